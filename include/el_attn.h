@@ -377,6 +377,132 @@ el_status el_attn_check_inputs(el_dtype dtype, int32_t d_model,
                                const void *H, int64_t H_batch_stride, const int32_t *lengths,
                                int32_t B, int32_t n, uint64_t *report, void *stream);
 
+/* ==== Beam search on a paged key/value cache ======================================================================
+ *
+ * What a search keeps next to the shared hidden states: projected keys and values of each beam's own continuation
+ * (section 3.2: "ordinary attention" over the part that is not shared), in pages, and the scores of the tokens that a
+ * step may go on with.  Context-free calls: every operand is passed, nothing is kept from call to call.
+ *
+ * A cache is a pool of `pages` pages of `page_size` positions.  Element (page, position, head, c) of K and of V is at
+ *     page * page_stride + position * position_stride + head * head_stride + c            (elements)
+ * so both [pages, page_size, kv_heads, d_head] and [pages, kv_heads, page_size, d_head] fit, and slices of either.
+ * Position t of sequence b is position t % page_size of page table[b * table_stride + t / page_size].  The table lives in
+ * device memory: several sequences may name the same page (a shared prefix, the full pages of a forked beam).  An entry
+ * outside [0, pages) names no page: its positions are neither read nor written and take no part in a softmax.
+ *
+ * Limits (UNSUPPORTED beyond): d_head <= 256, d_head a multiple of 16 bytes of elements.  Alignment (INVALID_ARG): K, V and
+ * every stride in bytes a multiple of 16; int32 and fp32 operands to 4 bytes.  Strides must not let two elements overlap.
+ * An argument error is found before any HIP call.
+ */
+typedef struct {
+    void *K, *V;              /* device, `dtype`                                                    */
+    int64_t page_stride;      /* elements, the same for K and V                                     */
+    int64_t position_stride;
+    int64_t head_stride;
+    int32_t pages, page_size; /* >= 1                                                               */
+    int32_t kv_heads, d_head;
+    int32_t dtype;            /* el_dtype of keys and values, queries and new tokens                */
+} el_attn_pages;
+
+/* How a score is formed from a query q and a key k at position t of a sequence of `len` positions, the last of which
+ * (len - 1) is the query's own:  s = scale q.k;  with a cap c > 0:  s = c tanh(s / c);  with slopes:
+ * s -= slopes[head] (len - 1 - t);  with a window w > 0: only positions t >= len - w. */
+typedef struct {
+    float scale;
+    float softcap;            /* >= 0; 0: none                                                      */
+    int32_t window;           /* >= 0; 0: none                                                      */
+    const float *slopes;      /* [heads] device, or NULL                                            */
+} el_attn_score_rule;
+
+/*
+ * Attention of one new token per query row over the sequence's pages.
+ *
+ *   table    [B, table_pages] int32 device, rows table_stride apart
+ *   lengths  [B] int32 device, each in [0, n] (a value outside is taken as the nearer end), or NULL: n
+ *   queries  rows b * beam + j, query_stride ELEMENTS apart, of `heads` heads of d_head each; device, `dtype`.  The `beam`
+ *            queries of a sequence read the same positions.  Query head i reads key head i / (heads / kv_heads)
+ *   out      [B * beam, heads * d_head] contiguous; `out_dtype`: EL_F32 or `dtype`
+ *   lse      [B * beam, heads] float32 or NULL: log sum_t exp(s_t), natural units
+ *   n        the largest length: at most table_pages * page_size
+ *
+ * With out_dtype EL_F32, (out, lse) is a segment as el_attn_decode_segment returns it, and el_attn_merge_segments joins
+ * it with segments over hidden states.  A row with no position (length 0, all pages absent, every score -inf) has output 0
+ * and lse -inf.  Storage behind a length or outside a window is never read into a result, whatever it holds.
+ *
+ * Accumulations and softmax statistics are fp32.  The result does not depend on what else runs, and is the same on
+ * every call.  `workspace`: el_attn_paged_workspace_bytes of device memory, 16-byte aligned, used by this call only, any
+ * contents; NULL where that is 0.
+ * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, heads no multiple of kv_heads, strides, a rule with a
+ * negative or non-finite number, n beyond the table), UNSUPPORTED (dtypes, d_head), WORKSPACE, HIP.
+ */
+size_t el_attn_paged_workspace_bytes(const el_attn_pages *cache, int32_t heads, int32_t B, int32_t beam, int32_t n);
+el_status el_attn_paged_attend(const el_attn_pages *cache,
+                               const int32_t *table, int64_t table_stride, int32_t table_pages, const int32_t *lengths,
+                               const void *queries, int64_t query_stride, int32_t heads, const el_attn_score_rule *rule,
+                               void *out, int32_t out_dtype, float *lse, int32_t B, int32_t beam, int32_t n,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * New tokens into the pages: K[position p of b] = K_new[b, i], V likewise, p = lengths[b] - counts[b] + i for i < counts[b],
+ * where lengths[b] counts the new tokens already (the same array that the attention after it reads).
+ *
+ *   K_new, V_new  [B, T, kv_heads, d_head], tokens token_stride and sequences batch_stride ELEMENTS apart (the same for
+ *                 both), a token's heads one behind the other; device, `dtype`; no part of the cache
+ *   lengths       [B] int32 device
+ *   counts        [B] int32 device, each in [0, T] (a value outside is taken as the nearer end), or NULL: T
+ *
+ * A token whose position is negative, or lies behind the table or in a page outside the pool, is dropped.  Where two
+ * sequences write the same position of the same page, either may win.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+el_status el_attn_paged_append(const el_attn_pages *cache,
+                               const int32_t *table, int64_t table_stride, int32_t table_pages,
+                               const int32_t *lengths, const int32_t *counts,
+                               const void *K_new, const void *V_new, int64_t batch_stride, int64_t token_stride,
+                               int32_t B, int32_t T, void *stream);
+
+/*
+ * Copies of pages, for a beam that forks: it takes its parent's full pages over in its own row of the table and needs a copy
+ * of the last, partly filled one only.  Positions [0, counts[i]) of page dst[i] become those of page src[i].
+ *
+ *   src, dst  [pairs] int32 device; a pair with either outside [0, pages), or src[i] == dst[i], is skipped
+ *   counts    [pairs] int32 device, each in [0, page_size] (a value outside is taken as the nearer end), or NULL: page_size
+ *
+ * A page may be the source of several pairs.  The caller sees to it that no page is the destination of two pairs, or the
+ * destination of one and the source of another.  Positions at or behind a count stay as they were.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_t *src, const int32_t *dst, const int32_t *counts,
+                             int32_t pairs, void *stream);
+
+/*
+ * Scores of the tokens that a row of logits x leaves open:
+ *
+ *   logprob[r]     = x[tokens[r]] - lse,  lse = log sum_v exp(x_v)
+ *   entropy[r]     = lse - sum_v p_v x_v,  p = exp(x - lse)
+ *   top_logprob[r, i], top_index[r, i]   for i < k: the k largest logits in descending order (of equal ones, the lowest index
+ *                    first), as log-probabilities, with their indices
+ *
+ *   logits   [rows, vocab], rows row_stride ELEMENTS apart (any, element alignment: an odd vocabulary is as good); device, `dtype`
+ *   tokens   [rows] int32 device, or NULL (with a NULL logprob).  A negative one marks a row without a token: log-probability 0.
+ *            One at or beyond vocab: NaN
+ *   logprob, entropy  [rows] float32, or NULL
+ *   top_logprob, top_index   [rows, k] float32 and int32; may be NULL where k is 0
+ *   k        0..el_attn_max_alternatives()
+ *
+ * A logit of -inf is a token that may not follow: probability 0, never an alternative.  Where fewer than k tokens may
+ * follow, the rest have log-probability -inf and index -1.  In a row where none may, the given token's log-probability is
+ * -inf and the entropy 0.  A NaN or +inf in a row makes its log-probabilities and entropy NaN; NaN is never an alternative.
+ * All sums are fp32 relative to the largest logit.  `workspace` as above, el_attn_score_workspace_bytes.
+ * Errors: INVALID_ARG (null operands, sizes < 1, k, row_stride < vocab, alignment), UNSUPPORTED (dtype), WORKSPACE, HIP.
+ */
+int32_t el_attn_max_alternatives(void);
+size_t el_attn_score_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
+el_status el_attn_score_tokens(el_dtype dtype, const void *logits, int64_t row_stride, int32_t rows, int32_t vocab,
+                               const int32_t *tokens, float *logprob, float *entropy,
+                               int32_t k, float *top_logprob, int32_t *top_index,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* Release the context and its packed weights (not the workspace, which the caller owns). */
 el_status el_attn_destroy(el_attn_ctx *ctx);
 

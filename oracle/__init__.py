@@ -13,6 +13,9 @@ module compiles it with gcc on first use and marshals numpy arrays to it.
                    over one key set, by definition (Eq. 1, Eq. 6/7), for the joint softmax of
                    section 3.2; ``join_segments_reference`` joins them and applies W^O.
 ``check_inputs_reference``  what a decode step assumes about its inputs, counted by definition.
+``paged_attend_reference``, ``paged_append_reference``, ``paged_copy_reference``  attention of one new token over pages
+                   of projected keys and values, and what moves them, position by position.
+``score_tokens_reference``  log-probability, entropy and best alternatives of rows of logits, by definition.
 ``gather_batch_reference``  the state gather between decode steps (section 3.1.1's
                    state, re-ordered / compacted by the search), by its definition.
 """
@@ -233,3 +236,110 @@ def check_inputs_reference(H, lengths, n=None):
             large += int((np.abs(row[fin]) > 65504.0).sum())
             seen += d_m
     return [bad_len, nonfinite, large, seen]
+
+
+def paged_attend_reference(K, V, table, lengths, queries, *, scale, n=None, softcap=0.0, window=0, slopes=None):
+    """Attention of one new token over pages of projected keys and values, one (row, head) at a time.
+
+    K, V [pages, page_size, kv_heads, d], queries [B, x, heads, d] as values of the stored elements; table [B, columns];
+    lengths [B], n the nearer end for what lies outside [0, n].  Positions in a page outside the pool do not exist.
+    Returns float64 out [B, x, heads, d] and lse [B, x, heads] (nothing attended: 0 and -inf), and for error bounds
+    {"spread": sum_t p_t |V_t| like out, "qk": max_t scale sum_c |q_c k_tc|, "s": the largest |score| or cap or bias that
+    a score is made of, "n": positions}, like lse.
+    """
+    pages, page_size, kv_heads, d = K.shape
+    B, x, heads, _ = queries.shape
+    n = table.shape[1] * page_size if n is None else n
+    out, lse = np.zeros((B, x, heads, d)), np.full((B, x, heads), -np.inf)
+    info = {"spread": np.zeros_like(out), "qk": np.zeros_like(lse), "s": np.zeros_like(lse), "n": np.zeros_like(lse)}
+    for b in range(B):
+        length = int(min(max(lengths[b], 0), n))
+        places = []
+        for t in range(max(0, length - window) if window else 0, length):
+            page = int(table[b, t // page_size])
+            if 0 <= page < pages:
+                places.append((t, page, t % page_size))
+        if not places:
+            continue
+        t, page, at = (np.array(c) for c in zip(*places))
+        for i in range(heads):
+            g = i // (heads // kv_heads)
+            k, v = K[page, at, g].astype(np.float64), V[page, at, g].astype(np.float64)
+            for j in range(x):
+                q = queries[b, j, i].astype(np.float64)
+                s = scale * (k @ q)
+                parts = [np.abs(s).max()]
+                info["qk"][b, j, i] = abs(scale) * (np.abs(k) @ np.abs(q)).max()
+                if softcap:
+                    s = softcap * np.tanh(s / softcap)
+                    parts.append(softcap)
+                if slopes is not None:
+                    bias = float(slopes[i]) * (length - 1 - t)
+                    s = s - bias
+                    parts += [np.abs(bias).max(), np.abs(s).max()]
+                m = s.max()
+                if m == -np.inf:
+                    continue
+                e = np.exp(s - m)
+                p = e / e.sum()
+                lse[b, j, i] = m + np.log(e.sum())
+                out[b, j, i] = (p[:, None] * v)[p > 0].sum(0)
+                info["spread"][b, j, i] = (p[:, None] * np.abs(v))[p > 0].sum(0)
+                info["s"][b, j, i], info["n"][b, j, i] = max(parts), len(places)
+    return out, lse, info
+
+
+def paged_append_reference(K, V, table, lengths, counts, K_new, V_new):
+    """K, V with token i < counts[b] of K_new, V_new [B, T, kv_heads, d] at position lengths[b] - counts[b] + i, token by
+    token; positions that do not exist are dropped."""
+    K, V = K.copy(), V.copy()
+    pages, page_size = K.shape[:2]
+    B, T = K_new.shape[:2]
+    for b in range(B):
+        count = T if counts is None else int(min(max(counts[b], 0), T))
+        for i in range(count):
+            t = int(lengths[b]) - count + i
+            if 0 <= t < table.shape[1] * page_size and 0 <= table[b, t // page_size] < pages:
+                K[table[b, t // page_size], t % page_size] = K_new[b, i]
+                V[table[b, t // page_size], t % page_size] = V_new[b, i]
+    return K, V
+
+
+def paged_copy_reference(K, V, src, dst, counts):
+    """K, V with positions [0, counts[i]) of page dst[i] taken from page src[i], pair by pair."""
+    K2, V2 = K.copy(), V.copy()
+    pages, page_size = K.shape[:2]
+    for i in range(len(src)):
+        if 0 <= src[i] < pages and 0 <= dst[i] < pages:
+            c = page_size if counts is None else int(min(max(counts[i], 0), page_size))
+            K2[dst[i], :c], V2[dst[i], :c] = K[src[i], :c], V[src[i], :c]
+    return K2, V2
+
+
+def score_tokens_reference(logits, tokens, k):
+    """(logprob, entropy, top_logprob, top_index) of float64 rows, and for error bounds sum_v p_v |x_v - max| per row."""
+    rows, vocab = logits.shape
+    logprob, entropy, away = np.zeros(rows), np.zeros(rows), np.zeros(rows)
+    top_logprob, top_index = np.full((rows, k), -np.inf), np.full((rows, k), -1, dtype=np.int64)
+    for r in range(rows):
+        x = logits[r].astype(np.float64)
+        allowed = x > -np.inf                                        # (False for NaN)
+        broken = bool(np.isnan(x).any() or (x == np.inf).any())
+        if broken:
+            lse = entropy[r] = np.nan
+        elif allowed.any():
+            m = x.max()
+            e = np.exp(x[allowed] - m)
+            lse = m + np.log(e.sum())
+            p = e / e.sum()
+            entropy[r] = lse - (p * x[allowed]).sum()
+            away[r] = (p * (m - x[allowed])).sum()
+        else:
+            lse = 0.0
+        if tokens is not None:
+            t = int(tokens[r])
+            logprob[r] = 0.0 if t < 0 else np.nan if t >= vocab else x[t] - lse
+        best = sorted((v for v in range(vocab) if allowed[v]), key=lambda v: (-x[v], v))[:k]
+        for i, v in enumerate(best):
+            top_logprob[r, i], top_index[r, i] = x[v] - lse, v
+    return logprob, entropy, top_logprob, top_index, away

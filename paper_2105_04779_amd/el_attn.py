@@ -26,6 +26,8 @@ EXPORTED_SYMBOLS = (
     "el_attn_core_timing_enable", "el_attn_core_timing_read",
     "el_attn_gather_batch", "el_attn_check_inputs",
     "el_attn_decode_segment", "el_attn_merge_segments", "el_attn_max_segments",
+    "el_attn_paged_workspace_bytes", "el_attn_paged_attend", "el_attn_paged_append", "el_attn_paged_copy",
+    "el_attn_max_alternatives", "el_attn_score_workspace_bytes", "el_attn_score_tokens",
     "el_attn_destroy", "el_attn_status_string", "el_attn_version",
 )
 
@@ -37,6 +39,21 @@ class ElAttnConfig(ctypes.Structure):
         ("max_batch", ctypes.c_int32), ("max_beam", ctypes.c_int32), ("max_n", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
     ]
+
+
+class ElAttnPages(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64), ("position_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32), ("d_head", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
+class ElAttnScoreRule(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p)]
 
 
 class ElAttnError(RuntimeError):
@@ -101,6 +118,21 @@ def _load():
     lib.el_attn_merge_segments.restype = ctypes.c_int
     lib.el_attn_max_segments.argtypes = []
     lib.el_attn_max_segments.restype = i32
+    pages, rule = ctypes.POINTER(ElAttnPages), ctypes.POINTER(ElAttnScoreRule)
+    lib.el_attn_paged_workspace_bytes.argtypes = [pages, i32, i32, i32, i32]
+    lib.el_attn_paged_workspace_bytes.restype = sz
+    lib.el_attn_paged_attend.argtypes = [pages, vp, i64, i32, vp, vp, i64, i32, rule, vp, i32, vp, i32, i32, i32, vp, sz, vp]
+    lib.el_attn_paged_attend.restype = ctypes.c_int
+    lib.el_attn_paged_append.argtypes = [pages, vp, i64, i32, vp, vp, vp, vp, i64, i64, i32, i32, vp]
+    lib.el_attn_paged_append.restype = ctypes.c_int
+    lib.el_attn_paged_copy.argtypes = [pages, vp, vp, vp, i32, vp]
+    lib.el_attn_paged_copy.restype = ctypes.c_int
+    lib.el_attn_max_alternatives.argtypes = []
+    lib.el_attn_max_alternatives.restype = i32
+    lib.el_attn_score_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.el_attn_score_workspace_bytes.restype = sz
+    lib.el_attn_score_tokens.argtypes = [ctypes.c_int, vp, i64, i32, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.el_attn_score_tokens.restype = ctypes.c_int
     lib.el_attn_destroy.argtypes = [vp]
     lib.el_attn_destroy.restype = ctypes.c_int
     lib.el_attn_status_string.argtypes = [ctypes.c_int]
@@ -218,6 +250,41 @@ def el_attn_max_segments() -> int:
     return int(lib.el_attn_max_segments())
 
 
+def el_attn_paged_workspace_bytes(cache: ElAttnPages, heads, B, beam, n) -> int:
+    return int(lib.el_attn_paged_workspace_bytes(cache, heads, B, beam, n))
+
+
+def el_attn_paged_attend(cache: ElAttnPages, table, table_stride, table_pages, lengths, queries, query_stride, heads,
+                         rule: ElAttnScoreRule, out, out_dtype, lse, B, beam, n, workspace=None, workspace_bytes=0,
+                         stream=None) -> int:
+    return lib.el_attn_paged_attend(cache, table, table_stride, table_pages, lengths, queries, query_stride, heads, rule,
+                                    out, out_dtype, lse, B, beam, n, workspace, workspace_bytes, stream)
+
+
+def el_attn_paged_append(cache: ElAttnPages, table, table_stride, table_pages, lengths, counts, K_new, V_new,
+                         batch_stride, token_stride, B, T, stream=None) -> int:
+    return lib.el_attn_paged_append(cache, table, table_stride, table_pages, lengths, counts, K_new, V_new,
+                                    batch_stride, token_stride, B, T, stream)
+
+
+def el_attn_paged_copy(cache: ElAttnPages, src, dst, counts, pairs, stream=None) -> int:
+    return lib.el_attn_paged_copy(cache, src, dst, counts, pairs, stream)
+
+
+def el_attn_max_alternatives() -> int:
+    return int(lib.el_attn_max_alternatives())
+
+
+def el_attn_score_workspace_bytes(rows, vocab, k) -> int:
+    return int(lib.el_attn_score_workspace_bytes(rows, vocab, k))
+
+
+def el_attn_score_tokens(dtype, logits, row_stride, rows, vocab, tokens, logprob, entropy, k, top_logprob, top_index,
+                         workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib.el_attn_score_tokens(dtype, logits, row_stride, rows, vocab, tokens, logprob, entropy, k,
+                                    top_logprob, top_index, workspace, workspace_bytes, stream)
+
+
 def el_attn_core_timing_enable(ctx, max_steps) -> int:
     return lib.el_attn_core_timing_enable(ctx, max_steps)
 
@@ -312,6 +379,193 @@ def check_inputs(H, lengths, report=None):
     if st != EL_OK:
         raise ElAttnError(st, "el_attn_check_inputs")
     return report
+
+
+def _dtype_code(t):
+    import torch
+    code = {torch.float32: EL_F32, torch.float16: EL_F16, torch.bfloat16: EL_BF16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"unsupported dtype {t.dtype}: float32, float16 or bfloat16")
+    return code
+
+
+def _check_operands(device, ints, floats):
+    """`ints`, `floats`: {name: tensor or None}.  All on `device`; index tensors int32; nothing that waits for a gradient
+    (none is computed)."""
+    import torch
+    for name, t in ints.items():
+        if t is not None and (t.dtype != torch.int32 or t.device != device):
+            raise ValueError(f"{name} must be an int32 tensor on {device}")
+    grad = torch.is_grad_enabled()
+    for name, t in floats.items():
+        if t is None:
+            continue
+        if t.device != device:
+            raise ValueError(f"{name} must be on {device}")
+        if grad and t.requires_grad:
+            raise ValueError(f"{name} requires a gradient, and none is computed: detach it or use torch.no_grad()")
+
+
+def _call(where, device, fn, *args):
+    """fn(*args, stream) on `device` (the operands'), on the stream that is current there."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        st = fn(*args, _stream_handle())
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _stream_handle())
+    if st != EL_OK:
+        raise ElAttnError(st, where)
+
+
+def _workspace(nbytes, device):
+    """Scratch memory of one call: torch's allocator keeps it for the stream (or the graph) that the call runs on."""
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+class PagedCache:
+    """Projected keys and values of one attention layer, in pages (see el_attn_pages): new tokens in, attention of one token
+    per query row out, pages copied for beams that fork.
+
+    K, V: device tensors [pages, page_size, kv_heads, d_head], the last dimension contiguous, with the same strides (a
+    transposed view of [pages, kv_heads, page_size, d_head] is as good).  The table [B, columns] int32 and the lengths
+    int32 [B] are the caller's, shared by all layers: position t of sequence b lies in page table[b, t // page_size];
+    an entry outside the pool (-1) holds no positions.
+    """
+
+    def __init__(self, K, V):
+        if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype or K.stride() != V.stride():
+            raise ValueError("K and V must be [pages, page_size, kv_heads, d_head] of one dtype and the same strides")
+        if not K.is_cuda or K.device != V.device:
+            raise ValueError("K and V must be on one device")
+        if K.stride(3) != 1:
+            raise ValueError("the last dimension of K and V must be contiguous")
+        if K.requires_grad or V.requires_grad:
+            raise ValueError("K and V are written in place: they must not require a gradient")
+        self.K, self.V = K, V
+        self.device = K.device
+        pages, self.page_size, self.kv_heads, self.d_head = K.shape
+        self.dtype = _dtype_code(K)
+        self._pages = ElAttnPages(_ptr(K), _ptr(V), K.stride(0), K.stride(1), K.stride(2),
+                                  pages, self.page_size, self.kv_heads, self.d_head, self.dtype)
+
+    def _table(self, table, B):
+        if table.dim() != 2 or table.shape[0] != B:
+            raise ValueError(f"table must be [{B}, columns]")
+        columns = table.shape[1]
+        if columns > 1 and table.stride(1) != 1:
+            raise ValueError("rows of the table must be contiguous")
+        return _ptr(table), table.stride(0) if B > 1 else columns, columns
+
+    def append(self, k, v, table, lengths, counts=None):
+        """New tokens k, v [B, T, kv_heads, d_head] (heads of a token contiguous, other strides free, the same for both) to
+        the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already."""
+        if k.dim() != 4 or k.shape != v.shape or k.shape[2:] != (self.kv_heads, self.d_head):
+            raise ValueError(f"k and v must be [B, T, {self.kv_heads}, {self.d_head}]")
+        if k.dtype != self.K.dtype or v.dtype != k.dtype:
+            raise ValueError(f"k and v must be {self.K.dtype}")
+        B, T = k.shape[:2]
+        strides = k.stride()
+        if strides[3] != 1 or (self.kv_heads > 1 and strides[2] != self.d_head) or v.stride() != strides:
+            raise ValueError("a token's heads must be contiguous, and k and v have the same strides")
+        _check_operands(self.device, {"table": table, "lengths": lengths, "counts": counts}, {"k": k, "v": v})
+        for name, t in (("lengths", lengths), ("counts", counts)):
+            if t is not None and (t.shape != (B,) or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous [{B}]")
+        row = self.kv_heads * self.d_head
+        _call("el_attn_paged_append", self.device, lib.el_attn_paged_append, self._pages, *self._table(table, B),
+              _ptr(lengths), _ptr(counts), _ptr(k), _ptr(v), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
+
+    def _attend(self, queries, table, lengths, n, scale, softcap, window, slopes, out, out_code, lse):
+        import torch
+        B, beam, heads, d = queries.shape
+        if lengths is not None and (lengths.shape != (B,) or not lengths.is_contiguous()):
+            raise ValueError(f"lengths must be contiguous [{B}]")
+        if slopes is not None and (slopes.shape != (heads,) or slopes.dtype != torch.float32 or not slopes.is_contiguous()):
+            raise ValueError(f"slopes must be contiguous float32 [{heads}]")
+        at, stride, columns = self._table(table, B)
+        if n is None:
+            n = columns * self.page_size
+        rule = ElAttnScoreRule(d ** -0.5 if scale is None else scale, softcap, window, _ptr(slopes))
+        q_stride = queries.stride(1) if beam > 1 else queries.stride(0) if B > 1 else heads * d
+        nbytes = lib.el_attn_paged_workspace_bytes(self._pages, heads, B, beam, n)
+        ws = _workspace(nbytes, self.device)
+        _call("el_attn_paged_attend", self.device, lib.el_attn_paged_attend, self._pages, at, stride, columns, _ptr(lengths),
+              _ptr(queries), q_stride, heads, rule, _ptr(out), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
+
+    def _check_queries(self, queries, table, lengths, slopes):
+        if queries.dim() != 4 or queries.shape[3] != self.d_head or queries.shape[2] % self.kv_heads != 0:
+            raise ValueError(f"queries must be [B, beam, heads, {self.d_head}], heads a multiple of {self.kv_heads}")
+        if queries.dtype != self.K.dtype:
+            raise ValueError(f"queries must be {self.K.dtype}")
+        B, beam, heads, d = queries.shape
+        if queries.stride(3) != 1 or (heads > 1 and queries.stride(2) != d):
+            raise ValueError("the heads of a query must be contiguous")
+        if B > 1 and beam > 1 and queries.stride(0) != beam * queries.stride(1):
+            raise ValueError("query rows must be evenly spaced")
+        _check_operands(self.device, {"table": table, "lengths": lengths}, {"queries": queries, "slopes": slopes})
+
+    def attend(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None,
+               out_dtype=None, out=None):
+        """Attention of queries [B, beam, heads, d_head] over each sequence's lengths[b] positions (None: n; n: the most that
+        any sequence has, default what the table holds).  Returns out [B, beam, heads, d_head] in `out_dtype` ("f32" or the
+        cache's own, the default).  See el_attn_score_rule for scale (default d_head ** -0.5), softcap, window and slopes."""
+        import torch
+        self._check_queries(queries, table, lengths, slopes)
+        code = self.dtype if out_dtype is None else DTYPE_CODES[out_dtype]
+        if out is None:
+            out = torch.empty(queries.shape, dtype=_torch_dtype(code), device=self.device)
+        elif out.shape != queries.shape or out.dtype != _torch_dtype(code) or not out.is_contiguous() or out.device != self.device:
+            raise ValueError(f"out must be a contiguous {_torch_dtype(code)} tensor of the queries' shape")
+        self._attend(queries, table, lengths, n, scale, softcap, window, slopes, out, code, None)
+        return out
+
+    def attend_segment(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None):
+        """The same as a segment (seg_A [B*beam, heads*d_head], seg_lse [B*beam, heads], float32) for
+        ElAttention.merge_segments."""
+        import torch
+        self._check_queries(queries, table, lengths, slopes)
+        B, beam, heads, d = queries.shape
+        A = torch.empty((B * beam, heads * d), dtype=torch.float32, device=self.device)
+        lse = torch.empty((B * beam, heads), dtype=torch.float32, device=self.device)
+        self._attend(queries, table, lengths, n, scale, softcap, window, slopes, A, EL_F32, lse)
+        return A, lse
+
+    def copy_pages(self, src, dst, counts=None):
+        """Positions [0, counts[i]) (default all) of page dst[i] become those of page src[i]; int32 device tensors.  No page
+        may be the destination of two pairs, or the destination of one and the source of another."""
+        pairs = src.shape[0] if src.dim() == 1 else -1
+        _check_operands(self.device, {"src": src, "dst": dst, "counts": counts}, {})
+        for t in (src, dst, counts):
+            if t is not None and (pairs < 0 or t.shape != (pairs,) or not t.is_contiguous()):
+                raise ValueError("src, dst and counts must be contiguous and of one length")
+        _call("el_attn_paged_copy", self.device, lib.el_attn_paged_copy, self._pages, _ptr(src), _ptr(dst), _ptr(counts), pairs)
+
+
+def score_tokens(logits, tokens=None, *, k=0):
+    """What rows of logits [rows, vocab] (rows strided, a row contiguous) say about the next token: (logprob, entropy,
+    top_logprob, top_index), float32 [rows], [rows], [rows, k] and int32 [rows, k].  logprob is that of tokens (int32 [rows];
+    None: logprob is None); the k best alternatives come in descending order.  See el_attn_score_tokens."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a device tensor [rows, vocab] with contiguous rows")
+    rows, vocab = logits.shape
+    device, code = logits.device, _dtype_code(logits)
+    _check_operands(device, {"tokens": tokens}, {"logits": logits})
+    if tokens is not None and (tokens.shape != (rows,) or not tokens.is_contiguous()):
+        raise ValueError(f"tokens must be contiguous [{rows}]")
+    if not 0 <= k <= el_attn_max_alternatives():
+        raise ValueError(f"k must lie in [0, {el_attn_max_alternatives()}]")
+    logprob = None if tokens is None else torch.empty(rows, dtype=torch.float32, device=device)
+    entropy = torch.empty(rows, dtype=torch.float32, device=device)
+    top_logprob = torch.empty((rows, k), dtype=torch.float32, device=device)
+    top_index = torch.empty((rows, k), dtype=torch.int32, device=device)
+    nbytes = lib.el_attn_score_workspace_bytes(rows, vocab, k)
+    ws = _workspace(nbytes, device)
+    _call("el_attn_score_tokens", device, lib.el_attn_score_tokens, code, _ptr(logits), logits.stride(0) if rows > 1 else vocab,
+          rows, vocab, _ptr(tokens), _ptr(logprob), _ptr(entropy), k, _ptr(top_logprob), _ptr(top_index), _ptr(ws), nbytes)
+    return logprob, entropy, top_logprob, top_index
 
 
 class ElAttention:

@@ -1,0 +1,150 @@
+"""GPU parity of the token scores against the fp64 reference.
+
+Error bound, u = 2^-24: a difference to the largest logit is rounded once and its exponential is good to 3 u (1 + |x - m|); sums of V
+positive terms in fp32 add at most V / 256 + 80 roundings; log S, lse and the results round a few times more at their own
+size.  So lse is off by u (3 (1 + A) + V / 256 + 80 + 4 |log S| + 2 |lse| + 2 |m|), A = sum p |x - m|, a log-probability by that
+and u |logprob|, and the entropy by the same with (1 + A) more for the weighted sum.  Indices are exact: the logits themselves are compared.
+"""
+import numpy as np
+import pytest
+
+import oracle
+from paper_2105_04779_amd import workloads as wl
+from helpers import record, to_device
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _check(tag, x, dtype, k, tokens="mixed", pad=0, offset=0):
+    import torch
+    from paper_2105_04779_amd import el_attn
+    rows, V = x.shape
+    g = np.random.default_rng(V)
+    x = wl.round_to_storage(x, dtype)
+    wide = np.full((rows, V + pad), np.float32(9e4 if dtype != "f16" else 6e4), dtype=np.float32)      # what is between rows would win
+    wide[:, :V] = x
+    flat = np.concatenate([np.full(offset, wide[0, -1] if pad else 0, np.float32), wide.reshape(-1)])
+    dev = to_device(wl.round_to_storage(flat, dtype), dtype)[offset:].view(rows, V + pad)[:, :V]
+    t = None if tokens is None else g.integers(0, V, rows).astype(np.int32) if isinstance(tokens, str) else np.asarray(tokens, np.int32)
+    got = el_attn.score_tokens(dev, None if t is None else torch.from_numpy(t).cuda(), k=k)
+    torch.cuda.synchronize()
+    logprob, entropy, top, index = (None if y is None else y.cpu().numpy() for y in got)
+    r_logprob, r_entropy, r_top, r_index, away = oracle.score_tokens_reference(x, t, k)
+    assert (logprob is None) == (t is None) and top.shape == index.shape == (rows, k)
+    assert np.array_equal(index, r_index), f"{tag}: indices differ in rows {np.nonzero((index != r_index).any(1))[0][:5]}"
+    finite = np.where(np.isfinite(x), x, 0).astype(np.float64)
+    m = np.array([r[np.isfinite(r)].max() if np.isfinite(r).any() else 0.0 for r in x.astype(np.float64)])
+    with np.errstate(all="ignore"):
+        log_s = np.array([np.log(np.exp(np.where(np.isfinite(r), r - b, -np.inf)).sum()) if np.isfinite(r).any() else 0.0
+                          for r, b in zip(x.astype(np.float64), m)])
+    D = U * (3 * (1 + away) + V / 256 + 80 + 4 * np.abs(log_s) + 2 * np.abs(m + log_s) + 2 * np.abs(m))
+    worst = 0.0
+
+    def close(name, y, ref, bound):
+        nonlocal worst
+        same = (np.isnan(y) & np.isnan(ref)) | (y == ref)
+        with np.errstate(invalid="ignore"):
+            ratio = np.where(same, 0.0, np.abs(y - ref) / bound)
+        worst = max(worst, float(np.max(ratio, initial=0.0)))
+        assert (ratio <= 1.0).all(), f"{tag}: {name} {np.nanmax(ratio)} of the bound"
+    if t is not None:
+        close("logprob", logprob, r_logprob, D + U * np.abs(np.nan_to_num(r_logprob, neginf=0.0)))
+    close("entropy", entropy, r_entropy, D * (2 + away))
+    close("top", top, r_top, D[:, None] + U * np.abs(np.nan_to_num(r_top, neginf=0.0)))
+    record(f"{tag}: {worst:.3f} of the bound")
+
+
+def _logits(seed, rows, V, scale=2.0):
+    return np.random.default_rng(seed).standard_normal((rows, V), dtype=np.float32) * np.float32(scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,V,k", [(1, 1, 1), (2, 2, 5), (3, 7, 7), (4, 63, 64), (1, 255, 3), (5, 257, 8), (3, 1000, 64), (4, 2049, 8), (2, 8191, 20),
+                                      (4, 16385, 10), (3, 50265, 8), (1, 131072, 64), (2, 200003, 50), (70, 4099, 4)])
+def test_sizes(dtype, rows, V, k):
+    _check(f"{dtype} {rows}x{V} k {k}", _logits(V, rows, V), dtype, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,offset", [(1, 0), (7, 3), (64, 1), (0, 5)])
+def test_rows_that_start_anywhere(dtype, pad, offset):
+    _check(f"{dtype} pad {pad} offset {offset}", _logits(3, 6, 5003), dtype, 12, pad=pad, offset=offset)
+    _check(f"{dtype} pad {pad} offset {offset} short", _logits(4, 6, 5), dtype, 3, pad=pad, offset=offset)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_ties_and_orders(dtype):
+    V = 40000
+    rows = [np.zeros(V), np.full(V, -3.5), np.linspace(0, 9, V), np.linspace(9, 0, V), np.where(np.arange(V) % 2, -0.0, 0.0),
+            np.where(np.arange(V) < V - 3, -60000.0, 1.0), np.where(np.arange(V) % 997 == 5, 2.0, 1.0), np.where(np.arange(V) >= V - 900, 4.0, -4.0),
+            np.repeat(np.linspace(5, 4, 10), V // 10)]
+    x = np.stack(rows).astype(np.float32)
+    for k in (1, 8, 64):
+        _check(f"ties {dtype} k {k}", x, dtype, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_banned_tokens(dtype):
+    g = np.random.default_rng(8)
+    x = _logits(9, 8, 30011)
+    x[0, :] = -np.inf                                                # none may follow
+    x[1, 1:] = -np.inf
+    x[2, :-1] = -np.inf
+    x[3, g.random(30011) < 0.999] = -np.inf                          # about 30
+    x[4, 20000:] = -np.inf
+    x[5, :20000] = -np.inf
+    x[6, :] = -np.inf
+    x[6, [3, 16390, 29000]] = [1.0, 1.0, 2.0]
+    for k in (1, 5, 40):
+        _check(f"banned {dtype} k {k}", x, dtype, k, tokens=[7, 0, 30010, 5, 25000, 25000, 3, 9])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_extreme_logits(dtype):
+    big = 60000.0
+    x = _logits(10, 7, 9001)
+    x[0, 77] = big                                                   # certain
+    x[1, :] = -big                                                   # large and equal
+    x[2, 5] = np.nan
+    x[3, 9] = np.inf
+    x[4] *= 50
+    x[5, 4000:] = -big                                               # the lowest of the type as a mask
+    x[6, :] = np.nan
+    _check(f"extreme {dtype}", x, dtype, 6, tokens=[77, 3, 5, 9, 1, 5000, 0])
+
+
+def test_tokens_that_are_none():
+    x = _logits(11, 5, 777)
+    _check("no token", x, "f32", 3, tokens=[-1, 776, 777, -2147483648, 2147483647])
+    _check("no tokens at all", x, "f32", 0, tokens=None)
+
+
+def test_rows_beyond_32_bits_of_elements():
+    """Three rows 2^31 elements apart, 8.6 GB of bf16."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    V, step = 5003, 1 << 31
+    flat = torch.zeros(2 * step + V, dtype=torch.bfloat16, device="cuda")
+    x = wl.round_to_storage(_logits(12, 3, V), "bf16")
+    rows = flat.as_strided((3, V), (step, 1))
+    rows.copy_(to_device(x, "bf16"))
+    t = torch.tensor([1, 2, 5002], dtype=torch.int32, device="cuda")
+    far, near = el_attn.score_tokens(rows, t, k=9), el_attn.score_tokens(to_device(x, "bf16"), t, k=9)
+    for a, b in zip(far, near):
+        assert torch.equal(a, b)
+
+
+def test_refusals():
+    import torch
+    from paper_2105_04779_amd import el_attn
+    x = torch.zeros((4, 100), device="cuda")
+    t = torch.zeros(4, dtype=torch.int32, device="cuda")
+    for call in (lambda: el_attn.score_tokens(x.double(), t), lambda: el_attn.score_tokens(x[0], t), lambda: el_attn.score_tokens(x.t(), t),
+                 lambda: el_attn.score_tokens(x, t.long()), lambda: el_attn.score_tokens(x, t[:2]), lambda: el_attn.score_tokens(x, t.cpu()),
+                 lambda: el_attn.score_tokens(x, t, k=65), lambda: el_attn.score_tokens(x, t, k=-1),
+                 lambda: el_attn.score_tokens(x.requires_grad_(), t)):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("taken")
