@@ -3,11 +3,31 @@
 //   s_t = scale q.K_t (capped, biased by distance),  out = sum_t softmax(s)_t V_t,  lse = log sum_t exp s_t
 //
 // over the positions that are there: below the length, inside the window, in a page of the pool.
+//
+// Bound by HBM: every key and value is read once and used by the query rows of its sequence that share the key head (beam x
+// heads / kv_heads of them, a handful), 2 flops a byte and row.  The kernel is built to keep that stream running:
+//   - A wavefront works alone on tiles of 32 positions (16 in fp32) of one sequence and key head, with a ring of tiles in LDS that
+//     is filled by direct requests (16 bytes a lane, no registers in flight) and waited for by count.  The page numbers
+//     of a tile are requested the same way, a ring's depth ahead, so that no request waits for the table.
+//   - Scores and weighted sum are matrix products, S^T = K Q^T and O^T += V^T P^T, with up to 16 query rows as columns.  S^T leaves
+//     the matrix unit with 4 neighbouring positions of one row in a lane; taken as the 8 inner indices of the second product (two
+//     groups of 16 positions), P never leaves the registers, and V's columns come from LDS transposed (ds_read_b64_tr_b16).
+//   - The running maximum and sum of the softmax are kept per wavefront and joined at the end, over the wavefronts of a workgroup
+//     through LDS and over the spans of a sequence by k_attend_join.
+// Work: the tiles of all sequences, cut into spans of T tiles, T such that the spans of all units (key heads, blocks of rows) are
+// about kWorkgroups, and never shorter than a tile a wavefront.  Every workgroup adds the lengths up by itself, so the cut
+// follows them without the host knowing them.
 #include <cmath>
+#include "mfma.h"
 #include "paged.h"
 
 namespace el {
 namespace {
+
+constexpr int kWaves = 2;            // wavefronts of a workgroup
+constexpr int kWorkgroups = 1024;    // spans x units aimed at: two rounds of the two workgroups that a compute unit holds
+constexpr int kCutMax = 1024;        // most sequences that are cut; beyond them the sequences alone fill the device twice
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArgs {
     PageView c;
@@ -16,76 +36,536 @@ struct AttendArgs {
     int64_t query_stride;                    // bytes
     const float *slopes;
     float scale, softcap;
-    int window, n, beam, heads, kv_heads, d;
+    int window, n, B, beam, heads, kv_heads, d;
+    int group, R, row_blocks, rows;          // heads / kv_heads; query rows of a key head; blocks of them; rows of a block, at most
+    int target, spans;                       // spans aimed at; spans at most
     void *out;
+    int out_dtype;
     float *lse;
+    int2 *pieces;                            // [B] first span and number of spans
+    float *part_o;                           // [span][unit][rows][d] weighted sums relative to part_ml's maximum
+    float2 *part_ml;                         // [span][unit][rows] (maximum, sum), powers of two
 };
 
-// One (query row, head) a workgroup, 256 positions at a time under the running maximum and sum of the softmax.
-template <typename T, typename TO>
-__global__ void __launch_bounds__(256) k_attend_rows(const AttendArgs a)
+// Tiles [x, y) of a sequence.
+__device__ __forceinline__ int2 tile_range(const AttendArgs &a, int b, int tile, int &len)
 {
-    __shared__ float q[kMaxHeadDim], p[256], red[8];
-    __shared__ int64_t off[256];
-    const int tid = threadIdx.x, w = tid >> 6;
-    const int head = blockIdx.x % a.heads, m = blockIdx.x / a.heads, b = m / a.beam;
-    const int64_t head_off = (int64_t)(head / (a.heads / a.kv_heads)) * a.c.head;
-    if (tid < a.d) q[tid] = to_f32(((const T *)(a.queries + m * a.query_stride))[(int64_t)head * a.d + tid]);
-    const int len = a.lengths ? min(max(a.lengths[b], 0), a.n) : a.n;
-    const float slope = a.slopes ? a.slopes[head] : 0.f;
-    float M = -INFINITY, L = 0.f, acc = 0.f;
-    for (int t0 = a.window ? max(0, len - a.window) : 0; t0 < len; t0 += 256) {
-        __syncthreads();
-        const int t = t0 + tid;
-        int64_t at = -1;
-        float s = -INFINITY;
-        if (t < len) {
-            const int slot = t / a.c.page_size, page = a.c.table[b * a.c.table_stride + slot];
-            if (page >= 0 && page < a.c.pages) {
-                at = page * a.c.page + (int64_t)(t - slot * a.c.page_size) * a.c.position + head_off;
-                const T *k = (const T *)(a.c.K + at);
-                s = 0.f;
-                for (int i = 0; i < a.d; ++i) s = fmaf(q[i], to_f32(k[i]), s);
-                s *= a.scale;
-                if (a.softcap > 0.f) s = a.softcap * tanhf(s / a.softcap);
-                if (a.slopes) s -= slope * (float)(len - 1 - t);
+    len = a.lengths ? min(max(a.lengths[b], 0), a.n) : a.n;
+    const int first = a.window ? max(0, len - a.window) : 0;
+    return int2{first / tile, (int)(((int64_t)len + tile - 1) / tile)};
+}
+
+struct Span { int b, index, count, first_span; int2 tiles; int len; };
+
+// The span of this workgroup: every wavefront finds it by itself.  False: there are fewer spans.
+__device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int tile, Span &s)
+{
+    const int lane = threadIdx.x & 63;
+    int T = INT32_MAX;
+    if (a.spans > a.B) {
+        long long total = 0;
+        for (int b = lane; b < a.B; b += 64) {
+            int len;
+            const int2 r = tile_range(a, b, tile, len);
+            total += r.y - r.x;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+        T = (int)max((long long)kWaves, (total + a.target - 1) / a.target);
+        int before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            const int b = b0 + lane;
+            int len = 0, c = 0;
+            int2 r{0, 0};
+            if (b < a.B) { r = tile_range(a, b, tile, len); c = max(1, (int)(((long long)(r.y - r.x) + T - 1) / T)); }
+            int incl = c;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(incl, o, 64); if (lane >= o) incl += v; }
+            const unsigned long long past = __ballot(before + incl > span);
+            if (past) {
+                const int at = __ffsll((long long)past) - 1;
+                s.b = b0 + at;
+                s.count = __builtin_amdgcn_readlane(c, at);
+                s.first_span = before + __builtin_amdgcn_readlane(incl, at) - s.count;
+                s.index = span - s.first_span;
+                s.len = __builtin_amdgcn_readlane(len, at);
+                const int x = __builtin_amdgcn_readlane(r.x, at), n = __builtin_amdgcn_readlane(r.y, at) - x;
+                const int each = (n + s.count - 1) / s.count;
+                s.tiles = int2{min(x + s.index * each, x + n), min(x + (s.index + 1) * each, x + n)};
+                return true;
+            }
+            before += __builtin_amdgcn_readlane(incl, 63);
+        }
+        return false;
+    }
+    s.b = span; s.index = 0; s.count = 1; s.first_span = span;
+    s.tiles = tile_range(a, span, tile, s.len);
+    return true;
+}
+
+__device__ __forceinline__ void request16(unsigned lds_addr, const char *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_addr), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void request4(unsigned lds_addr, const int32_t *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds_addr), "v"(from) : "memory", "m0");
+}
+template <int N> __device__ __forceinline__ void wait_requests() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
+// Row `row` of a tile keeps its chunk c of 16 bytes at c ^ swizzle(row): operand reads of 16 rows at one chunk, and the transposing
+// reads of 16 rows at two, then spread over all banks.
+template <int ROWB> __device__ __forceinline__ int swizzle(int row) { return ROWB >= 256 ? row & 15 : (row >> 1) & 7; }
+
+__device__ __forceinline__ float max_over_groups(float v)          // over the four lanes that hold one query row
+{
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_over_groups(float v)
+{
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+__device__ __forceinline__ void store4(void *out, int64_t at, int dtype, f4 v)
+{
+    if (dtype == EL_F32) *(f4 *)((float *)out + at) = v;
+    else if (dtype == EL_F16) *(h4 *)((f16_t *)out + at) = __builtin_convertvector(v, h4);
+    else *(u2 *)((uint16_t *)out + at) = u2{__builtin_bit_cast(unsigned, __builtin_convertvector(f2{v[0], v[1]}, b2)),
+                                            __builtin_bit_cast(unsigned, __builtin_convertvector(f2{v[2], v[3]}, b2))};
+}
+
+// DT: storage type; DP: d_head, padded; RG: query rows in groups of 16.  Grid: spans x units, a unit's key head first.
+template <int DT, int DP, int RG>
+__global__ void __launch_bounds__(64 * kWaves, 1) k_attend(const AttendArgs a)
+{
+    constexpr bool F32 = DT == EL_F32, BF16 = DT == EL_BF16;
+    constexpr int ES = F32 ? 4 : 2, TP = F32 ? 16 : 32, ROWB = DP * ES, CPR = ROWB / 16, NI = TP * ROWB / 1024, RPI = 64 / CPR;
+    constexpr int NS = DP == 64 ? 4 : 2, TILEB = TP * ROWB, PENDING = (NS - 1) * (2 * NI + 1), DT16 = DP / 16;
+    constexpr int QC = F32 ? DP / 16 : DP / 32;                      // pieces of 16 bytes of a query row that a lane holds
+    // P in 16 bits: parts that add up to it.  fp16: two (22 bits), times 2^12, which keeps the low part of small ones out of the
+    // subnormal numbers; bf16: three (24 bits).  The products that they cost are hidden behind HBM.
+    constexpr int NP = F32 ? 1 : BF16 ? 3 : 2;
+    constexpr float SHIFT = DT == EL_F16 ? 12.f : 0.f;
+    __shared__ __attribute__((aligned(1024))) char ring[kWaves * NS * 2 * TILEB];
+    __shared__ __attribute__((aligned(256))) int Tb[kWaves][NS][64];
+    __shared__ float2 ml[kWaves][RG][16];
+
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int units = a.kv_heads * a.row_blocks, span = blockIdx.x / units, unit = blockIdx.x - span * units;
+    const int kvh = unit % a.kv_heads, row0 = unit / a.kv_heads * a.rows;
+    Span sp;
+    if (!find_span(a, span, TP, sp)) return;
+    if (a.spans > a.B && sp.index == 0 && unit == 0 && threadIdx.x == 0) a.pieces[sp.b] = int2{sp.first_span, sp.count};
+    const int64_t b = sp.b;
+    const int len = sp.len, first = a.window ? max(0, len - a.window) : 0;
+    const float to_exp2 = a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e;  // what a product is multiplied by: the cap's argument
+    const int nt = max(0, (sp.tiles.y - sp.tiles.x - w + kWaves - 1) / kWaves);     // tiles of this wavefront: x + w, x + w + kWaves, ..
+
+    // query rows: row r of the key head is beam r / group, head kvh * group + r % group
+    u4 q[RG][QC];
+    float slope[RG];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        const int r = row0 + 16 * rg + r16;
+        const bool here = 16 * rg + r16 < a.rows && r < a.R;
+        const int head = kvh * a.group + r % a.group;
+        const char *p = a.queries + (b * a.beam + r / a.group) * a.query_stride + (int64_t)head * a.d * ES;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+            q[rg][c] = u4{0, 0, 0, 0};
+            if (here && (4 * c + g) * 16 < a.d * ES) q[rg][c] = *(const u4 *)(p + (4 * c + g) * 16);
+        }
+        slope[rg] = here && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    }
+    f4 acc[RG][DT16];
+    float m[RG], l[RG];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        m[rg] = -INFINITY; l[rg] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT16; ++t) acc[rg][t] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    char *const mine = ring + w * (NS * 2 * TILEB);
+    EL_LDS(char) *const lds = (EL_LDS(char) *)mine;
+    const unsigned lds_at = (unsigned)(uintptr_t)lds, tb_at = (unsigned)(uintptr_t)(EL_LDS(int) *)&Tb[w][0][0];
+    const int chunks = a.d * ES / 16;
+    if (chunks < CPR) {                     // columns beyond d_head are never requested: zeros, which a query's zeros meet
+        for (int i = lane; i < NS * 2 * TILEB / 16; i += 64) *(u4 *)(mine + i * 16) = u4{0, 0, 0, 0};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    const int32_t *const table = a.c.table + b * a.c.table_stride;
+    const char *const Kh = a.c.K + kvh * a.c.head;
+    const int64_t k_to_v = a.c.V - a.c.K;
+    auto position = [&](int i) __attribute__((always_inline)) { return (int64_t)(sp.tiles.x + w + kWaves * i) * TP + (lane & (TP - 1)); };
+    auto request_pages = [&](int i) __attribute__((always_inline)) {
+        const int64_t last = (int64_t)len - 1, t = position(i) < last ? position(i) : last;
+        request4(tb_at + (i & (NS - 1)) * 256, table + (unsigned)t / (unsigned)a.c.page_size);
+    };
+    // Requests tile i; returns which of its positions are there.  One that is not is replaced by one that is: what storage without
+    // a meaning holds reaches nothing.
+    auto request_tile = [&](int i) __attribute__((always_inline)) -> unsigned {
+        const int64_t t = position(i);
+        const unsigned slot = (unsigned)(t < len ? t : 0) / (unsigned)a.c.page_size;
+        const int page = Tb[w][i & (NS - 1)][lane];
+        const bool valid = t >= first && t < len && page >= 0 && page < a.c.pages;
+        constexpr unsigned ALL = TP == 32 ? 0xffffffffu : 0xffffu;
+        const unsigned mask = (unsigned)__ballot(valid) & ALL;
+        int64_t off = valid ? page * a.c.page + (t - (int64_t)slot * a.c.page_size) * a.c.position : 0;
+        if (mask != ALL) {
+            const int some = mask ? __ffs((int)mask) - 1 : 0;
+            const int lo = __builtin_amdgcn_readlane((int)off, some), hi = __builtin_amdgcn_readlane((int)(off >> 32), some);
+            if (!valid) off = (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo);
+        }
+        const unsigned at = lds_at + (i & (NS - 1)) * (2 * TILEB);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int row = j * RPI + lane / CPR, c = (lane % CPR) ^ swizzle<ROWB>(row);
+            const int lo = __shfl((int)off, row, 64), hi = __shfl((int)(off >> 32), row, 64);
+            const char *from = Kh + (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo) + c * 16;
+            if (c < chunks) {               // (at least the first chunk of a row: the instruction is issued, and counted, always)
+                request16(at + j * 1024, from);
+                request16(at + TILEB + j * 1024, from + k_to_v);
             }
         }
-        off[tid] = at;
-        float mx = s;
-        for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-        if ((tid & 63) == 0) red[w] = mx;
-        __syncthreads();
-        mx = fmaxf(fmaxf(M, fmaxf(red[0], red[1])), fmaxf(red[2], red[3]));
-        const float ref = mx == -INFINITY ? 0.f : mx, pr = at < 0 ? 0.f : expf(s - ref);
-        float sum = pr;
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        p[tid] = pr;
-        if ((tid & 63) == 0) red[4 + w] = sum;
-        __syncthreads();
-        const float rescale = M == -INFINITY ? 0.f : expf(M - ref);
-        L = L * rescale + (red[4] + red[5] + red[6] + red[7]);
-        acc *= rescale;
-        if (tid < a.d)
-            for (int i = 0; i < min(256, len - t0); ++i)
-                if (off[i] >= 0) acc = fmaf(p[i], to_f32(((const T *)(a.c.V + off[i]))[tid]), acc);
-        M = mx;
+        return mask;
+    };
+
+    unsigned here[NS];
+    if (nt > 0) {
+        // (q and slope are in registers before the first request: a wait of the compiler's for them would wait for all that is under way)
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+#pragma unroll
+            for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(q[rg][c]));
+            asm volatile("" : "+v"(slope[rg]));
+        }
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) request_pages(i);
+        wait_requests<0>();
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) {
+            request_pages(i + NS - 1);
+            here[i] = 0;
+            if (i < nt) here[i] = request_tile(i);
+        }
     }
-    // (no position, or every score -inf: nothing, where the quotient would be 0 / 0; a NaN stays one)
+    for (int i = 0; i < nt; ++i) {
+        // Requests come back in order.  Behind the pages of tile i + NS - 1, and behind tile i, exactly NS - 1 tiles and their pages
+        // have been requested; at the end of the span, where there are fewer, everything is waited for.
+        request_pages(i + 2 * NS - 2);
+        here[NS - 1] = 0;
+        if (i + NS - 1 < nt) {
+            wait_requests<PENDING>();
+            here[NS - 1] = request_tile(i + NS - 1);
+            wait_requests<PENDING>();
+        } else {
+            wait_requests<0>();
+        }
+        const unsigned mask = here[0];
+#pragma unroll
+        for (int k = 0; k < NS - 1; ++k) here[k] = here[k + 1];
+        if (mask == 0) continue;
+        const EL_LDS(char) *const Kt = lds + (i & (NS - 1)) * (2 * TILEB), *const Vt = Kt + TILEB;
+        const int dist0 = len - 1 - (sp.tiles.x + w + kWaves * i) * TP;             // of the tile's first position
+
+        // ---- scores ----
+        constexpr int NA = TP / 16;
+        f4 s[RG][NA];
+#pragma unroll
+        for (int x = 0; x < NA; ++x) {
+            u4 k[QC];
+#pragma unroll
+            for (int c = 0; c < QC; ++c) k[c] = *(const EL_LDS(u4) *)(Kt + (16 * x + r16) * ROWB + (((4 * c + g) ^ swizzle<ROWB>(r16)) << 4));
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg) s[rg][x] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < QC; ++c)
+#pragma unroll
+                for (int rg = 0; rg < RG; ++rg) {
+                    if constexpr (F32) {
+                        const f4 kf = __builtin_bit_cast(f4, k[c]), qf = __builtin_bit_cast(f4, q[rg][c]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[rg][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], s[rg][x], 0, 0, 0);
+                    } else {
+                        s[rg][x] = Mma<BF16>::s16(k[c], q[rg][c], s[rg][x]);
+                    }
+                }
+        }
+        // ---- softmax: lane (g, r16) holds positions 16 x + 4 g + e of row r16; scores in powers of two ----
+        const unsigned bits = mask >> (4 * g);
+        float p[RG][NA][4];
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+#pragma unroll
+            for (int x = 0; x < NA; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[rg][x][e] = s[rg][x][e] * to_exp2;
+            if (a.softcap > 0.f) {
+#pragma unroll
+                for (int x = 0; x < NA; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[rg][x][e] = a.softcap * kLog2e * tanhf(p[rg][x][e]);
+            }
+            if (a.slopes) {
+#pragma unroll
+                for (int x = 0; x < NA; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[rg][x][e] -= slope[rg] * (float)(dist0 - 16 * x - 4 * g - e);
+            }
+            if (mask != (TP == 32 ? 0xffffffffu : 0xffffu)) {
+#pragma unroll
+                for (int x = 0; x < NA; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!((bits >> (16 * x + e)) & 1)) p[rg][x][e] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < NA; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, p[rg][x][e]);
+            mx = fmaxf(m[rg], max_over_groups(mx));
+            if (__ballot(mx > m[rg])) {
+                const float f = m[rg] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rg] - mx);
+                l[rg] *= f;
+#pragma unroll
+                for (int t = 0; t < DT16; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[rg][t][e] *= f;
+                m[rg] = mx;
+            }
+            const float ref = (m[rg] == -INFINITY ? 0.f : m[rg]) - SHIFT;
+#pragma unroll
+            for (int x = 0; x < NA; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[rg][x][e] = __builtin_amdgcn_exp2f(p[rg][x][e] - ref);
+                    l[rg] += p[rg][x][e];
+                }
+        }
+        // ---- weighted sum ----
+        if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int t = 0; t < DT16; ++t) {
+                    const int row = 4 * g + e;
+                    const float v = *(const EL_LDS(float) *)(Vt + row * ROWB + (((4 * t + (r16 >> 2)) ^ swizzle<ROWB>(row)) << 4) + (r16 & 3) * 4);
+#pragma unroll
+                    for (int rg = 0; rg < RG; ++rg) acc[rg][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rg][0][e], acc[rg][t], 0, 0, 0);
+                }
+        } else {
+            u4 pp[RG][NP];
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    float u = p[rg][y >> 1][2 * (y & 1)], v = p[rg][y >> 1][2 * (y & 1) + 1];
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        if constexpr (BF16) {
+                            const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector(f2{u, v}, b2));
+                            pp[rg][k][y] = h;
+                            u -= __uint_as_float(h << 16); v -= __uint_as_float(h & 0xffff0000u);
+                        } else {
+                            const h2 h = __builtin_convertvector(f2{u, v}, h2);
+                            pp[rg][k][y] = __builtin_bit_cast(unsigned, h);
+                            u -= (float)h[0]; v -= (float)h[1];
+                        }
+                    }
+                }
+            const int row = 4 * g + (r16 >> 2);
+#pragma unroll
+            for (int t = 0; t < DT16; ++t) {
+                const int at = row * ROWB + (((2 * t + ((r16 & 3) >> 1)) ^ swizzle<ROWB>(row)) << 4) + (r16 & 1) * 8;
+                const s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EL_LDS(s4) *)(Vt + at));
+                const s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EL_LDS(s4) *)(Vt + at + 16 * ROWB));
+                const u4 v = __builtin_bit_cast(u4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) acc[rg][t] = Mma<BF16>::s16(v, pp[rg][k], acc[rg][t]);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // every read of this slot is through before it is requested into
+    }
+
+    // ---- the wavefronts' results joined: each finishes every kWaves-th block of 16 columns ----
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        l[rg] = sum_over_groups(l[rg]);
+        if (g == 0) ml[w][rg][r16] = float2{m[rg], l[rg]};
+    }
+    __syncthreads();                                                 // (the ring is read and requested no more)
+    f4 *const X = (f4 *)ring;                                        // [wavefront][row group][block of columns][lane]
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+        for (int t = 0; t < DT16; ++t) X[((w * RG + rg) * DT16 + t) * 64 + lane] = acc[rg][t];
+    __syncthreads();
+    const bool whole = sp.count == 1;
+    const int64_t slot = (int64_t)blockIdx.x * a.rows;
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        const int rb = 16 * rg + r16, r = row0 + rb;
+        const bool mine_row = rb < a.rows && r < a.R;
+        float M = -INFINITY, L = 0.f, f[kWaves];
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) M = fmaxf(M, ml[k][rg][r16].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            f[k] = __builtin_amdgcn_exp2f(ml[k][rg][r16].x - ref);
+            L += f[k] * ml[k][rg][r16].y;
+        }
+        if (M == -INFINITY)                                          // no score, or none above -inf: 0, unless there is a NaN among them
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) { f[k] = 1.f; L = k == 0 ? ml[k][rg][r16].y : L + ml[k][rg][r16].y; }
+        const bool empty = M == -INFINITY && !(L != L);
+        const int64_t out_row = ((b * a.beam + r / a.group) * a.heads + kvh * a.group + r % a.group);
+        if (mine_row && w == 0 && g == 0) {
+            if (!whole) a.part_ml[slot + rb] = float2{M, L};
+            else if (a.lse) a.lse[out_row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - SHIFT) * kLn2;
+        }
+        const float inv = whole ? (empty ? 0.f : 1.f / L) : 1.f;
+#pragma unroll
+        for (int t0 = 0; t0 < DT16; t0 += kWaves) {
+            const int t = t0 + w, col = 16 * t + 4 * g;
+            f4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                const f4 x = X[((k * RG + rg) * DT16 + t) * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += f[k] * x[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = empty && whole ? 0.f : o[e] * inv;
+            if (mine_row && col < a.d) {
+                if (whole) store4(a.out, out_row * a.d + col, a.out_dtype, o);
+                else *(f4 *)(a.part_o + (slot + rb) * a.d + col) = o;
+            }
+        }
+    }
+}
+
+// Joins the spans of a sequence that was cut: one (sequence, query row, head) a workgroup.  Bound by latency: the statistics of all
+// spans in one round trip, the weighted sums in another.
+__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, float shift)
+{
+    extern __shared__ float weight[];                                // [spans]
+    __shared__ float red[4];
+    __shared__ f4 sums[256];
+    const int tid = threadIdx.x, b = blockIdx.x / (a.beam * a.heads), x = blockIdx.x - b * (a.beam * a.heads);
+    const int2 pc = a.pieces[b];
+    if (pc.y < 2) return;
+    const int j = x / a.heads, head = x - j * a.heads, kvh = head / a.group, r = j * a.group + head % a.group;
+    const int units = a.kv_heads * a.row_blocks, unit = r / a.rows * a.kv_heads + kvh, rb = r % a.rows;
+    auto slot = [&](int s) { return ((int64_t)(pc.x + s) * units + unit) * a.rows + rb; };
+    float M = -INFINITY;
+    for (int s = tid; s < pc.y; s += 256) M = fmaxf(M, a.part_ml[slot(s)].x);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    if ((tid & 63) == 0) red[tid >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = M == -INFINITY ? 0.f : M;
+    float L = 0.f;
+    for (int s = tid; s < pc.y; s += 256) {
+        const float2 v = a.part_ml[slot(s)];
+        // (a span without a position: sum 0.  A NaN score leaves its maximum at -inf and its sum at NaN, which stays)
+        const float f = v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(v.x - ref);
+        weight[s] = f;
+        L += f * v.y;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o, 64);
+    __syncthreads();
+    if ((tid & 63) == 0) red[tid >> 6] = L;
+    __syncthreads();
+    L = (red[0] + red[1]) + (red[2] + red[3]);
     const bool empty = M == -INFINITY && !(L != L);
-    if (tid < a.d) from_f32(empty ? 0.f : acc / L, (TO *)a.out + (int64_t)blockIdx.x * a.d + tid);
-    if (tid == 0 && a.lse) a.lse[blockIdx.x] = empty ? -INFINITY : M + logf(L);
+    const int64_t row = (int64_t)blockIdx.x;
+    if (tid == 0 && a.lse) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - shift) * kLn2;
+    const int d4 = a.d / 4, groups = 256 / d4, grp = tid / d4, col = tid - grp * d4;
+    f4 o{0.f, 0.f, 0.f, 0.f};
+    if (grp < groups)
+        for (int s = grp; s < pc.y; s += groups) {
+            const f4 v = *(const f4 *)(a.part_o + slot(s) * a.d + 4 * col);
+            const float f = weight[s];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += f * v[e];
+        }
+    sums[tid] = o;
+    __syncthreads();
+    if (tid < d4) {
+        for (int k = 1; k < groups; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += sums[k * d4 + tid][e];
+        const float inv = 1.f / L;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = empty ? 0.f : o[e] * inv;
+        store4(a.out, row * a.d + 4 * tid, a.out_dtype, o);
+    }
+}
+
+// What a call is launched with: host arithmetic.
+struct AttendPlan { int row_groups, row_blocks, rows, target, spans; size_t pieces_bytes, ml_bytes, workspace; };
+
+AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n)
+{
+    AttendPlan p;
+    const int R = beam * (heads / c.kv_heads);
+    // (two groups of rows share a tile's operand reads; in fp32 beyond 128 columns their registers do not suffice)
+    p.row_groups = R <= 16 || (c.dtype == EL_F32 && c.d_head > 128) ? 1 : 2;
+    p.row_blocks = (R + 16 * p.row_groups - 1) / (16 * p.row_groups);
+    p.rows = R < 16 * p.row_groups ? R : 16 * p.row_groups;
+    const int64_t units = (int64_t)c.kv_heads * p.row_blocks;
+    p.target = (int)(units < kWorkgroups ? kWorkgroups / units : 1);
+    const int tile = c.dtype == EL_F32 ? 16 : 32;
+    const int64_t tiles = ((int64_t)n + tile - 1) / tile, each = (tiles + kWaves - 1) / kWaves;     // spans of a sequence, at most
+    const int64_t cut = (int64_t)p.target + B, all = B * each;
+    p.spans = B > kCutMax ? B : (int)(cut < all ? cut : all);
+    p.pieces_bytes = p.ml_bytes = p.workspace = 0;
+    if (p.spans > B) {
+        const size_t rows = (size_t)p.spans * units * p.rows;
+        p.pieces_bytes = align_up((size_t)B * sizeof(int2), 256);
+        p.ml_bytes = align_up(rows * sizeof(float2), 256);
+        p.workspace = p.pieces_bytes + p.ml_bytes + rows * c.d_head * sizeof(float);
+    }
+    return p;
+}
+
+template <int DT>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)(p.spans * a.kv_heads * p.row_blocks)), block(64 * kWaves);
+#define EL_ATTEND(DP, RG) hipLaunchKernelGGL((k_attend<DT, DP, RG>), grid, block, 0, s, a)
+    if (a.d <= 64) { if (p.row_groups == 1) EL_ATTEND(64, 1); else EL_ATTEND(64, 2); }
+    else if (a.d <= 128) { if (p.row_groups == 1) EL_ATTEND(128, 1); else EL_ATTEND(128, 2); }
+    else if (DT == EL_F32 || p.row_groups == 1) EL_ATTEND(256, 1);
+    else if constexpr (DT != EL_F32) EL_ATTEND(256, 2);
+#undef EL_ATTEND
 }
 
 bool finite_non_negative(float x) { return x >= 0.f && x < INFINITY; }
+
+constexpr int64_t kMaxRows = (int64_t)1 << 23;                       // B x beam x heads: a launch has fewer than 2^32 threads
+
+bool valid_sizes(const el_attn_pages *c, int32_t heads, int32_t B, int32_t beam, int32_t n)
+{
+    return heads >= 1 && B >= 1 && beam >= 1 && n >= 1 && heads % c->kv_heads == 0 && (int64_t)B * beam <= kMaxRows && (int64_t)B * beam * heads <= kMaxRows;
+}
 
 } // namespace
 } // namespace el
 
 extern "C" size_t el_attn_paged_workspace_bytes(const el_attn_pages *cache, int32_t heads, int32_t B, int32_t beam, int32_t n)
 {
-    if (el::check_pages(cache) != EL_OK || heads < 1 || B < 1 || beam < 1 || n < 1) return 0;
-    return 0;
+    if (el::check_pages(cache) != EL_OK || !el::valid_sizes(cache, heads, B, beam, n)) return 0;
+    return el::plan_attend(*cache, heads, B, beam, n).workspace;
 }
 
 extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
@@ -97,23 +577,41 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     using namespace el;
     if (const el_status st = check_pages(cache); st != EL_OK) return st;
     if (const el_status st = check_table(table, table_stride, table_pages, B); st != EL_OK) return st;
-    if (!queries || !rule || !out || heads < 1 || beam < 1 || n < 1) return EL_ERR_INVALID_ARG;
+    if (!queries || !rule || !out || !valid_sizes(cache, heads, B, beam, n)) return EL_ERR_INVALID_ARG;
     if (out_dtype != EL_F32 && out_dtype != cache->dtype) return EL_ERR_UNSUPPORTED;
-    if (heads % cache->kv_heads != 0 || n > (int64_t)table_pages * cache->page_size) return EL_ERR_INVALID_ARG;
+    if (n > (int64_t)table_pages * cache->page_size) return EL_ERR_INVALID_ARG;
     if (!(fabsf(rule->scale) < INFINITY) || !finite_non_negative(rule->softcap) || rule->window < 0) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)dtype_size(cache->dtype), row = (int64_t)heads * cache->d_head, rows = (int64_t)B * beam;
     if (((uintptr_t)lengths | (uintptr_t)lse | (uintptr_t)rule->slopes) & 3 || ((uintptr_t)queries | (uintptr_t)out) & 15) return EL_ERR_INVALID_ARG;
     if (query_stride > ((int64_t)1 << 44) || query_stride * es % 16 != 0 || (rows > 1 && query_stride < row)) return EL_ERR_INVALID_ARG;
-    if (rows * heads > INT32_MAX) return EL_ERR_INVALID_ARG;
-    const AttendArgs a{page_view(*cache, table, table_stride, table_pages), lengths, (const char *)queries, query_stride * es, rule->slopes,
-                       rule->scale, rule->softcap, rule->window, n, beam, heads, cache->kv_heads, cache->d_head, out, lse};
-    const dim3 grid((unsigned)(rows * heads)), block(256);
+    const AttendPlan p = plan_attend(*cache, heads, B, beam, n);
+    if (p.workspace) {
+        if (!workspace || workspace_bytes < p.workspace) return EL_ERR_WORKSPACE;
+        if ((uintptr_t)workspace & 15) return EL_ERR_INVALID_ARG;
+    }
+    AttendArgs a{};
+    a.c = page_view(*cache, table, table_stride, table_pages);
+    a.lengths = lengths;
+    a.queries = (const char *)queries; a.query_stride = query_stride * es;
+    a.slopes = rule->slopes; a.scale = rule->scale; a.softcap = rule->softcap; a.window = rule->window;
+    a.n = n; a.B = B; a.beam = beam; a.heads = heads; a.kv_heads = cache->kv_heads; a.d = cache->d_head;
+    a.group = heads / cache->kv_heads; a.R = beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
+    a.target = p.target; a.spans = p.spans;
+    a.out = out; a.out_dtype = out_dtype; a.lse = lse;
+    if (p.workspace) {
+        a.pieces = (int2 *)workspace;
+        a.part_ml = (float2 *)((char *)workspace + p.pieces_bytes);
+        a.part_o = (float *)((char *)workspace + p.pieces_bytes + p.ml_bytes);
+    }
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
-    if (cache->dtype == EL_F32) hipLaunchKernelGGL((k_attend_rows<float, float>), grid, block, 0, s, a);
-    else if (cache->dtype == EL_F16 && out_dtype == EL_F16) hipLaunchKernelGGL((k_attend_rows<f16_t, f16_t>), grid, block, 0, s, a);
-    else if (cache->dtype == EL_F16) hipLaunchKernelGGL((k_attend_rows<f16_t, float>), grid, block, 0, s, a);
-    else if (out_dtype == EL_BF16) hipLaunchKernelGGL((k_attend_rows<bf16_t, bf16_t>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_attend_rows<bf16_t, float>), grid, block, 0, s, a);
-    return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
+    if (cache->dtype == EL_F32) launch_attend<EL_F32>(a, p, s);
+    else if (cache->dtype == EL_F16) launch_attend<EL_F16>(a, p, s);
+    else launch_attend<EL_BF16>(a, p, s);
+    if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
+    if (p.spans > B) {
+        hipLaunchKernelGGL(k_attend_join, dim3((unsigned)(rows * heads)), dim3(256), (p.target + 1) * sizeof(float), s, a, cache->dtype == EL_F16 ? 12.f : 0.f);
+        if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
+    }
+    return EL_OK;
 }
