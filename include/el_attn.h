@@ -433,7 +433,7 @@ typedef struct {
  * every call.  `workspace`: el_attn_paged_workspace_bytes of device memory, 16-byte aligned, used by this call only, any
  * contents; NULL where that is 0.
  * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, heads no multiple of kv_heads, strides, a rule with a
- * negative or non-finite number, n beyond the table), UNSUPPORTED (dtypes, d_head), WORKSPACE, HIP.
+ * negative or non-finite number, n beyond the table, B * beam * heads beyond 2^23), UNSUPPORTED (dtypes, d_head), WORKSPACE, HIP.
  */
 size_t el_attn_paged_workspace_bytes(const el_attn_pages *cache, int32_t heads, int32_t B, int32_t beam, int32_t n);
 el_status el_attn_paged_attend(const el_attn_pages *cache,
@@ -488,13 +488,15 @@ el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_t *src, con
  *            One at or beyond vocab: NaN
  *   logprob, entropy  [rows] float32, or NULL
  *   top_logprob, top_index   [rows, k] float32 and int32; may be NULL where k is 0
+ *   vocab    up to 2^19 (UNSUPPORTED beyond)
  *   k        0..el_attn_max_alternatives()
  *
  * A logit of -inf is a token that may not follow: probability 0, never an alternative.  Where fewer than k tokens may
  * follow, the rest have log-probability -inf and index -1.  In a row where none may, the given token's log-probability is
  * -inf and the entropy 0.  A NaN or +inf in a row makes its log-probabilities and entropy NaN; NaN is never an alternative.
  * All sums are fp32 relative to the largest logit.  `workspace` as above, el_attn_score_workspace_bytes.
- * Errors: INVALID_ARG (null operands, sizes < 1, k, row_stride < vocab, alignment), UNSUPPORTED (dtype), WORKSPACE, HIP.
+ * Errors: INVALID_ARG (null operands, sizes < 1, k, row_stride < vocab, alignment; rows beyond
+ * 2^23), UNSUPPORTED (dtype, vocab), WORKSPACE, HIP.
  */
 int32_t el_attn_max_alternatives(void);
 size_t el_attn_score_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);

@@ -107,7 +107,7 @@ extern "C" el_status el_attn_paged_append(const el_attn_pages *cache,
 {
     if (const el_status st = el::check_pages(cache); st != EL_OK) return st;
     if (const el_status st = el::check_table(table, table_stride, table_pages, B); st != EL_OK) return st;
-    if (!lengths || !K_new || !V_new || T < 1 || B > 65535) return EL_ERR_INVALID_ARG;                       // B: grid.y
+    if (!lengths || !K_new || !V_new || T < 1 || T > 1 << 23 || B > 65535) return EL_ERR_INVALID_ARG;        // (grid)
     if (((uintptr_t)lengths | (uintptr_t)counts) & 3 || ((uintptr_t)K_new | (uintptr_t)V_new) & 15) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)el::dtype_size(cache->dtype), most = (int64_t)1 << 44, row = (int64_t)cache->kv_heads * cache->d_head;
     if (token_stride > most || batch_stride > most || token_stride * es % 16 != 0 || batch_stride * es % 16 != 0) return EL_ERR_INVALID_ARG;
@@ -124,7 +124,7 @@ extern "C" el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_
                                         int32_t pairs, void *stream)
 {
     if (const el_status st = el::check_pages(cache); st != EL_OK) return st;
-    if (!src || !dst || pairs < 1) return EL_ERR_INVALID_ARG;
+    if (!src || !dst || pairs < 1 || pairs > 1 << 23) return EL_ERR_INVALID_ARG;
     if (((uintptr_t)src | (uintptr_t)dst | (uintptr_t)counts) & 3) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)el::dtype_size(cache->dtype);
     const el::CopyArgs a{el::page_view(*cache, nullptr, 0, 0), src, dst, counts, cache->kv_heads, (int)(cache->d_head * es / 16)};

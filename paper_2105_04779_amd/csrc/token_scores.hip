@@ -1,90 +1,340 @@
 // What a row of logits says about the next token: log-probability of a given one, entropy, the best alternatives.
 //
-//   lse = m + log S,  S = sum exp(x - m),  entropy = log S - T / S,  T = sum exp(x - m) (x - m),  m the largest logit
+//   lse = m + log S,  S = sum exp(x - m),  entropy = log S - W / S,  W = sum exp(x - m) (x - m),  m the largest logit
+//
+// Bound by HBM where rows are many: every logit is read once.  A workgroup holds a chunk of a row in registers, so maximum, sums
+// and alternatives are passes over registers.  Rows start anywhere (an odd vocabulary): chunks are cut at 16-byte boundaries of
+// memory, and the pieces of 16 bytes at a row's ends that are not all its own are read element by element.
+// Alternatives: the k-th largest of the 256 lanes' maxima has k elements at or above it, so whatever lies below it is none of the
+// chunk's k best; about as many as k are left, and are ranked by counting.  k_score_join joins the chunks of a row.
+#include <cfloat>
 #include <cmath>
-#include "el_internal.h"
+#include "mfma.h"
 
 namespace el {
 namespace {
 
 constexpr int kMaxAlternatives = 64;
+constexpr int kLanes = 256;
+constexpr int kCandidates = 1024;        // of a chunk that are ranked by counting; with more (ties) one is taken at a time
+constexpr int kFillWorkgroups = 512;     // chunks get smaller until about so many workgroups share the logits: two a compute unit
+constexpr int32_t kMaxVocab = 1 << 19;
+constexpr int kListMax = 65 * kMaxAlternatives;                      // entries of the lists that k_score_join holds in LDS: the largest vocabulary's in fp32
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+typedef unsigned long long Key;
 
 struct ScoreArgs {
     const char *logits;
-    int64_t row_stride;          // elements
-    int vocab, k;
+    int64_t row_stride;                  // bytes
+    int vocab, k, chunks;
     const int32_t *tokens;
     float *logprob, *entropy, *top_logprob;
     int32_t *top_index;
+    f4 *stats;                           // [row][chunk] m, S, W
+    Key *keys;                           // [row][chunk][k] descending; 0: none
 };
 
-// What orders alternatives: the value, then the lower index.  0: no alternative (-inf or NaN).
-__device__ __forceinline__ unsigned long long order_key(float x, int v)
+// What orders alternatives: the value, then the lower index.
+__device__ __forceinline__ unsigned order32(float x)
 {
-    if (!(x > -INFINITY)) return 0ull;
     const unsigned u = __float_as_uint(x + 0.f);                     // (-0 counts as 0)
-    return ((unsigned long long)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - (unsigned)v);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(unsigned long long key)
+__device__ __forceinline__ float value_of(unsigned order) { return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
+__device__ __forceinline__ Key key_of(float x, int v) { return ((Key)order32(x) << 32) | (0xffffffffu - (unsigned)v); }
+
+template <typename T> struct Piece;      // 16 bytes of logits
+template <> struct Piece<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ float at(u4 v, int i) { return __uint_as_float(v[i]); }
+    static __device__ __forceinline__ void set(u4 &v, int i, float x) { v[i] = __float_as_uint(x); }
+};
+template <> struct Piece<bf16_t> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ float at(u4 v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
+    static __device__ __forceinline__ void set(u4 &v, int i, float x)
+    {
+        const unsigned u = __float_as_uint(x) >> 16;                 // (a bf16 value: exact)
+        v[i >> 1] = i & 1 ? (v[i >> 1] & 0xffffu) | (u << 16) : (v[i >> 1] & 0xffff0000u) | u;
+    }
+};
+template <> struct Piece<f16_t> {
+    static constexpr int N = 8;
+    // (a bit cast of a vector's element itself takes element 0 whatever the index: through a copy)
+    static __device__ __forceinline__ float at(u4 v, int i) { const unsigned u = v[i >> 1]; return (float)__builtin_bit_cast(h2, u)[i & 1]; }
+    static __device__ __forceinline__ void set(u4 &v, int i, float x)
+    {
+        const unsigned u = v[i >> 1];
+        h2 h = __builtin_bit_cast(h2, u);
+        h[i & 1] = (_Float16)x;
+        v[i >> 1] = __builtin_bit_cast(unsigned, h);
+    }
+};
+
+struct Sums { float m, S, W; };
+__device__ __forceinline__ Sums join(Sums a, Sums b)
 {
-    const unsigned u = (unsigned)(key >> 32);
-    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+    const float m = fmaxf(a.m, b.m);
+    // (nothing above -inf on a side: its sums are 0, or NaN, and stay)
+    const float da = a.m == -INFINITY ? 0.f : a.m - m, db = b.m == -INFINITY ? 0.f : b.m - m;
+    const float fa = __builtin_amdgcn_exp2f(da * kLog2e), fb = __builtin_amdgcn_exp2f(db * kLog2e);
+    return Sums{m, fa * a.S + fb * b.S, fa * (a.W + da * a.S) + fb * (b.W + db * b.S)};
 }
 
-template <typename V, typename F>
-__device__ __forceinline__ V block_reduce(V v, V *red, F f)
-{
-    for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return f(f(red[0], red[1]), f(red[2], red[3]));
-}
-
-// One row a workgroup; one pass for the maximum, one for the sums, one for every alternative.
+// logprob and entropy of a row, by one lane; returns lse.
 template <typename T>
-__global__ void __launch_bounds__(256) k_score_rows(const ScoreArgs a)
+__device__ __forceinline__ float lse_of(Sums s) { return s.S == 0.f ? 0.f : s.m + __builtin_amdgcn_logf(s.S) * kLn2; }
+template <typename T>
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t r, Sums s)
 {
-    __shared__ float red[4];
-    __shared__ unsigned long long redk[4];
-    const int64_t r = blockIdx.x;
-    const T *x = (const T *)a.logits + r * a.row_stride;
-    auto add = [](float p, float q) { return p + q; };
-    float m = -INFINITY;
-    for (int v = threadIdx.x; v < a.vocab; v += 256) m = fmaxf(m, to_f32(x[v]));
-    m = block_reduce(m, red, [](float p, float q) { return fmaxf(p, q); });
+    const bool none = s.S == 0.f;                                    // no token may follow
+    if (a.entropy) a.entropy[r] = none ? 0.f : __builtin_amdgcn_logf(s.S) * kLn2 - s.W / s.S;
+    if (a.logprob) {
+        const int t = a.tokens[r];
+        a.logprob[r] = t < 0 ? 0.f : t >= a.vocab ? NAN : none ? -INFINITY : to_f32(((const T *)(a.logits + r * a.row_stride))[t]) - lse_of<T>(s);
+    }
+}
+__device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r, int i, Key key, float lse)
+{
+    a.top_logprob[r * a.k + i] = key ? value_of((unsigned)(key >> 32)) - lse : -INFINITY;
+    a.top_index[r * a.k + i] = key ? (int)(0xffffffffu - (unsigned)key) : -1;
+}
+
+// A chunk of NV pieces a lane of one row.  Grid: rows x chunks.
+template <typename T, int NV>
+__global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
+{
+    constexpr int N = Piece<T>::N;
+    __shared__ unsigned best[kLanes];
+    __shared__ Key cand[kCandidates];
+    __shared__ Sums part[4];
+    __shared__ int count;
+    __shared__ Key top[4];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t r = blockIdx.x / a.chunks;
+    const int chunk = blockIdx.x - (int)r * a.chunks;
+    const char *const row = a.logits + r * a.row_stride;
+    const int lead = (int)((uintptr_t)row & 15) / (int)sizeof(T);   // elements between a 16-byte boundary and the row's first
+    const char *const base = row - lead * (int)sizeof(T);
+    const int first = (chunk * NV * kLanes + tid) * N - lead;       // index of this lane's first element; its pieces are kLanes apart
+    if (tid == 0) count = 0;
+
+    u4 v[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int64_t e = (int64_t)first + (int64_t)j * kLanes * N;
+        if (e >= 0 && e + N <= a.vocab) {
+            v[j] = __builtin_nontemporal_load((const u4 *)(base + (e + lead) * (int)sizeof(T)));
+        } else {                                                     // (-inf where there is no element)
+            v[j] = u4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < N; ++i) Piece<T>::set(v[j], i, e + i >= 0 && e + i < a.vocab ? to_f32(((const T *)row)[e + i]) : -INFINITY);
+        }
+    }
+    float most[NV], m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        most[j] = Piece<T>::at(v[j], 0);
+#pragma unroll
+        for (int i = 1; i < N; ++i) most[j] = fmaxf(most[j], Piece<T>::at(v[j], i));
+        m = fmaxf(m, most[j]);
+    }
+    best[tid] = m > -INFINITY ? order32(m) : 0u;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     const float ref = m == -INFINITY ? 0.f : m;
     float S = 0.f, W = 0.f;
-    for (int v = threadIdx.x; v < a.vocab; v += 256) {
-        const float d = to_f32(x[v]) - ref, e = expf(d);
-        S += e;
-        W += e * fmaxf(d, -1e4f);                                    // (a banned token: 0, not 0 * inf)
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float d = Piece<T>::at(v[j], i) - ref, e = __builtin_amdgcn_exp2f(d * kLog2e);
+            S += e;
+            W += e * fmaxf(d, -1e4f);                                // (a banned token: 0, not 0 * inf)
+        }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { S += __shfl_xor(S, o, 64); W += __shfl_xor(W, o, 64); }
+    if (lane == 0) part[w] = Sums{m, S, W};
+    __syncthreads();
+    const bool whole = a.chunks == 1;
+    const Sums s = join(join(part[0], part[1]), join(part[2], part[3]));
+    if (tid == 0) {
+        if (whole) write_row<T>(a, r, s);
+        else a.stats[blockIdx.x] = f4{s.m, s.S, s.W, 0.f};
     }
-    S = block_reduce(S, red, add);
-    W = block_reduce(W, red, add);
-    const bool none = S == 0.f;
-    const float lse = none ? 0.f : ref + logf(S);
-    if (threadIdx.x == 0) {
-        if (a.entropy) a.entropy[r] = none ? 0.f : logf(S) - W / S;
-        if (a.logprob) {
-            const int t = a.tokens[r];
-            a.logprob[r] = t < 0 ? 0.f : t >= a.vocab ? NAN : none ? -INFINITY : to_f32(x[t]) - lse;
+    if (a.k == 0) return;
+    const float lse = lse_of<T>(s);
+    auto emit = [&](int i, Key key) __attribute__((always_inline)) {
+        if (whole) write_alternative(a, r, i, key, lse);
+        else a.keys[(int64_t)blockIdx.x * a.k + i] = key;
+    };
+    // the k-th largest of the lanes' maxima, by its upper 16 bits (0: fewer than k lanes have an alternative)
+    unsigned bound = 0;
+    {
+        const unsigned b0 = best[lane], b1 = best[lane + 64], b2 = best[lane + 128], b3 = best[lane + 192];
+#pragma unroll
+        for (int bit = 31; bit >= 16; --bit) {
+            const unsigned t = bound | (1u << bit);
+            const int n = __popcll(__ballot(b0 >= t)) + __popcll(__ballot(b1 >= t)) + __popcll(__ballot(b2 >= t)) + __popcll(__ballot(b3 >= t));
+            if (n >= a.k) bound = t;
         }
     }
-    unsigned long long last = ~0ull;
+    const float least = bound ? value_of(bound) : -FLT_MAX;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (!__ballot(most[j] >= least)) continue;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = Piece<T>::at(v[j], i);
+            if (x >= least) {
+                const int at = atomicAdd(&count, 1);
+                if (at < kCandidates) cand[at] = key_of(x, first + j * kLanes * N + i);
+            }
+        }
+    }
+    __syncthreads();
+    const int n = count;
+    if (n <= kCandidates) {
+        for (int c = tid; c < n; c += kLanes) {
+            const Key key = cand[c];
+            int rank = 0;
+            for (int o = 0; o < n; ++o) rank += cand[o] > key;
+            if (rank < a.k) emit(rank, key);
+        }
+        for (int c = n + tid; c < a.k; c += kLanes) emit(c, 0);
+        return;
+    }
+    Key last = ~(Key)0;
     for (int i = 0; i < a.k; ++i) {
-        unsigned long long best = 0;
-        for (int v = threadIdx.x; v < a.vocab; v += 256) {
-            const unsigned long long key = order_key(to_f32(x[v]), v);
-            if (key < last && key > best) best = key;
+        Key mine = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float x = Piece<T>::at(v[j], e);
+                const Key key = x >= least ? key_of(x, first + j * kLanes * N + e) : 0;
+                if (key < last && key > mine) mine = key;
+            }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const Key other = __shfl_xor(mine, o, 64);
+            mine = mine > other ? mine : other;
         }
-        best = block_reduce(best, redk, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; });
-        if (threadIdx.x == 0) {
-            a.top_logprob[r * a.k + i] = best ? key_value(best) - lse : -INFINITY;
-            a.top_index[r * a.k + i] = best ? (int)(0xffffffffu - (unsigned)best) : -1;
-        }
-        last = best;
+        __syncthreads();
+        if (lane == 0) top[w] = mine;
+        __syncthreads();
+        const Key x = top[0] > top[1] ? top[0] : top[1], y = top[2] > top[3] ? top[2] : top[3];
+        last = x > y ? x : y;
+        if (tid == 0) emit(i, last);
     }
+}
+
+// The chunks of a row joined: one row a workgroup.  An alternative's place is the number of larger ones, counted in every chunk's
+// descending list by bisection; what lies below some chunk's k-th is none.
+template <typename T>
+__global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
+{
+    extern __shared__ Key list[];                                    // [chunk][k]
+    __shared__ Sums part[4];
+    __shared__ Key floor4[4];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t r = blockIdx.x;
+    const int total = a.chunks * a.k;
+    const Key *const keys = a.keys + r * total;
+    Sums s{-INFINITY, 0.f, 0.f};
+    for (int c = tid; c < a.chunks; c += kLanes) {
+        const f4 v = a.stats[r * a.chunks + c];
+        s = join(s, Sums{v[0], v[1], v[2]});
+    }
+    Key least = 0;
+    for (int i = tid; i < total; i += kLanes) {
+        const Key key = keys[i];
+        list[i] = key;
+        if ((i + 1) % a.k == 0 && key > least) least = key;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        s = join(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)});
+        const Key other = __shfl_xor(least, o, 64);
+        least = least > other ? least : other;
+    }
+    if (lane == 0) { part[w] = s; floor4[w] = least; }
+    __syncthreads();
+    s = join(join(part[0], part[1]), join(part[2], part[3]));
+    if (tid == 0) write_row<T>(a, r, s);
+    if (a.k == 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) least = least > floor4[i] ? least : floor4[i];
+    const float lse = lse_of<T>(s);
+    for (int i = tid; i < total; i += kLanes) {
+        const Key key = list[i];
+        if (key == 0 || key < least) continue;
+        int rank = 0;
+        for (int c = 0; c < a.chunks && rank < a.k; ++c) {
+            int lo = 0, hi = a.k;                                    // the first of the list that is not larger
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (list[c * a.k + mid] > key) lo = mid + 1; else hi = mid;
+            }
+            rank += lo;
+        }
+        if (rank < a.k) write_alternative(a, r, rank, key, lse);
+    }
+    // places without an alternative: fewer than k in all chunks together
+    if (least == 0) {
+        int there = 0;
+        for (int c = 0; c < a.chunks; ++c) {
+            int lo = 0, hi = a.k;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (list[c * a.k + mid] > 0) lo = mid + 1; else hi = mid;
+            }
+            there += lo;
+        }
+        for (int i = there + tid; i < a.k; i += kLanes) write_alternative(a, r, i, 0, lse);
+    }
+}
+
+// How a call is cut: pieces a lane, chunks of a row.
+struct ScorePlan { int pieces, chunks; size_t stats_bytes, workspace; };
+
+ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
+{
+    const int n = 16 / element_size;
+    const int64_t pieces = ((int64_t)vocab + n - 1 + n - 1) / n;     // of a row that starts anywhere between two boundaries
+    ScorePlan p;
+    p.pieces = 8;
+    auto chunks = [&] { return (pieces + (int64_t)p.pieces * kLanes - 1) / ((int64_t)p.pieces * kLanes); };
+    while (p.pieces > 1 && rows * chunks() < kFillWorkgroups) {
+        p.pieces /= 2;
+        if (chunks() * k > kListMax) { p.pieces *= 2; break; }
+    }
+    p.chunks = (int)chunks();
+    p.stats_bytes = p.workspace = 0;
+    if (p.chunks > 1) {
+        p.stats_bytes = align_up((size_t)rows * p.chunks * sizeof(f4), 256);
+        p.workspace = p.stats_bytes + (size_t)rows * p.chunks * k * sizeof(Key);
+    }
+    return p;
+}
+
+template <typename T>
+void launch_score(const ScoreArgs &a, const ScorePlan &p, int rows, hipStream_t s)
+{
+    const dim3 grid((unsigned)(rows * p.chunks)), block(kLanes);
+    if (p.pieces == 8) hipLaunchKernelGGL((k_score_chunk<T, 8>), grid, block, 0, s, a);
+    else if (p.pieces == 4) hipLaunchKernelGGL((k_score_chunk<T, 4>), grid, block, 0, s, a);
+    else if (p.pieces == 2) hipLaunchKernelGGL((k_score_chunk<T, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_score_chunk<T, 1>), grid, block, 0, s, a);
+    if (p.chunks > 1) hipLaunchKernelGGL((k_score_join<T>), dim3(rows), block, (size_t)p.chunks * a.k * sizeof(Key), s, a);
+}
+
+constexpr int64_t kMaxChunks = (int64_t)1 << 23;                     // rows x chunks: a launch has fewer than 2^32 threads
+
+bool valid_sizes(int32_t rows, int32_t vocab, int32_t k)
+{
+    return rows >= 1 && vocab >= 1 && k >= 0 && k <= kMaxAlternatives && rows <= kMaxChunks;
 }
 
 } // namespace
@@ -94,8 +344,10 @@ extern "C" int32_t el_attn_max_alternatives(void) { return el::kMaxAlternatives;
 
 extern "C" size_t el_attn_score_workspace_bytes(int32_t rows, int32_t vocab, int32_t k)
 {
-    if (rows < 1 || vocab < 1 || k < 0 || k > el::kMaxAlternatives) return 0;
-    return 0;
+    using namespace el;
+    if (!valid_sizes(rows, vocab, k) || vocab > kMaxVocab) return 0;
+    const size_t two = plan_score(2, rows, vocab, k).workspace, four = plan_score(4, rows, vocab, k).workspace;
+    return two > four ? two : four;
 }
 
 extern "C" el_status el_attn_score_tokens(el_dtype dtype, const void *logits, int64_t row_stride, int32_t rows, int32_t vocab,
@@ -105,16 +357,25 @@ extern "C" el_status el_attn_score_tokens(el_dtype dtype, const void *logits, in
 {
     using namespace el;
     if (dtype != EL_F32 && dtype != EL_F16 && dtype != EL_BF16) return EL_ERR_UNSUPPORTED;
-    if (!logits || rows < 1 || vocab < 1 || k < 0 || k > kMaxAlternatives) return EL_ERR_INVALID_ARG;
+    if (!logits || !valid_sizes(rows, vocab, k)) return EL_ERR_INVALID_ARG;
+    if (vocab > kMaxVocab) return EL_ERR_UNSUPPORTED;
     if ((logprob && !tokens) || (k > 0 && (!top_logprob || !top_index))) return EL_ERR_INVALID_ARG;
     if ((rows > 1 && row_stride < vocab) || row_stride > ((int64_t)1 << 44)) return EL_ERR_INVALID_ARG;
-    if ((uintptr_t)logits % dtype_size(dtype) != 0) return EL_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)dtype_size(dtype);
+    if ((uintptr_t)logits % (size_t)es != 0) return EL_ERR_INVALID_ARG;
     if (((uintptr_t)tokens | (uintptr_t)logprob | (uintptr_t)entropy | (uintptr_t)top_logprob | (uintptr_t)top_index) & 3) return EL_ERR_INVALID_ARG;
-    const ScoreArgs a{(const char *)logits, row_stride, vocab, k, tokens, logprob, entropy, top_logprob, top_index};
+    const ScorePlan p = plan_score((int)es, rows, vocab, k);
+    if ((int64_t)rows * p.chunks > kMaxChunks) return EL_ERR_INVALID_ARG;
+    if (p.workspace) {
+        if (!workspace || workspace_bytes < p.workspace) return EL_ERR_WORKSPACE;
+        if ((uintptr_t)workspace & 15) return EL_ERR_INVALID_ARG;
+    }
+    const ScoreArgs a{(const char *)logits, row_stride * es, vocab, k, p.chunks, tokens, logprob, entropy, top_logprob, top_index,
+                      (f4 *)workspace, (Key *)((char *)workspace + p.stats_bytes)};
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
-    if (dtype == EL_F32) hipLaunchKernelGGL((k_score_rows<float>), dim3(rows), dim3(256), 0, s, a);
-    else if (dtype == EL_F16) hipLaunchKernelGGL((k_score_rows<f16_t>), dim3(rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_score_rows<bf16_t>), dim3(rows), dim3(256), 0, s, a);
+    if (dtype == EL_F32) launch_score<float>(a, p, rows, s);
+    else if (dtype == EL_F16) launch_score<f16_t>(a, p, rows, s);
+    else launch_score<bf16_t>(a, p, rows, s);
     return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
 }
