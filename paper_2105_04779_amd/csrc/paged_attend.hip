@@ -12,20 +12,22 @@
 //   - Scores and weighted sum are matrix products, S^T = K Q^T and O^T += V^T P^T, with up to 16 query rows as columns.  S^T leaves
 //     the matrix unit with 4 neighbouring positions of one row in a lane; taken as the 8 inner indices of the second product (two
 //     groups of 16 positions), P never leaves the registers, and V's columns come from LDS transposed (ds_read_b64_tr_b16).
-//   - The running maximum and sum of the softmax are kept per wavefront and joined at the end, over the wavefronts of a workgroup
-//     through LDS and over the spans of a sequence by k_attend_join.
-// Work: the tiles of all sequences, cut into spans of T tiles, T such that the spans of all units (key heads, blocks of rows) are
-// about kWorkgroups, and never shorter than a tile a wavefront.  Every workgroup adds the lengths up by itself, so the cut
-// follows them without the host knowing them.
+//   - The running maximum and sum of the softmax are kept per wavefront; k_attend_join joins the pieces of a sequence.
+// Work: the tiles of all sequences form one list, cut into as many equal spans as wavefronts (spans x units) fit the device at
+// once.  A span that goes on to the next sequence closes a piece and starts another.  Every wavefront adds the lengths up by
+// itself, so the cut follows them without the host knowing them.  Where sequences alone fill the device and are short, a
+// wavefront takes one whole, and nothing is joined.
 #include <cmath>
+#include <type_traits>
 #include "mfma.h"
 #include "paged.h"
 
 namespace el {
 namespace {
 
-constexpr int kWaves = 2;            // wavefronts of a workgroup
-constexpr int kWorkgroups = 1024;    // spans x units aimed at: two rounds of the two workgroups that a compute unit holds
+constexpr int kCrossing = 1;
+constexpr int kComputeUnits = 256;
+constexpr int kShort = 2048;         // positions that one wavefront may be left with where sequences alone fill the device
 constexpr int kCutMax = 1024;        // most sequences that are cut; beyond them the sequences alone fill the device twice
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -38,69 +40,81 @@ struct AttendArgs {
     float scale, softcap;
     int window, n, B, beam, heads, kv_heads, d;
     int group, R, row_blocks, rows;          // heads / kv_heads; query rows of a key head; blocks of them; rows of a block, at most
-    int target, spans;                       // spans aimed at; spans at most
+    int spans;                               // spans that the tiles of all sequences are cut into, at most; 0: a span is a sequence
     void *out;
     int out_dtype;
     float *lse;
-    int2 *pieces;                            // [B] first span and number of spans
-    float *part_o;                           // [span][unit][rows][d] weighted sums relative to part_ml's maximum
-    float2 *part_ml;                         // [span][unit][rows] (maximum, sum), powers of two
+    int2 *pieces;                            // [B] first slot and number of slots of a sequence's pieces
+    float *part_o;                           // [slot][unit][rows][d] weighted sums relative to part_ml's maximum
+    float2 *part_ml;                         // [slot][unit][rows] (maximum, sum), powers of two
 };
 
-// Tiles [x, y) of a sequence.
-__device__ __forceinline__ int2 tile_range(const AttendArgs &a, int b, int tile, int &len)
+// Tiles [x, y) of a sequence of `len` positions.
+__device__ __forceinline__ int length_of(const AttendArgs &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.n) : a.n; }
+__device__ __forceinline__ int2 tile_range(const AttendArgs &a, int len, int tile)
 {
-    len = a.lengths ? min(max(a.lengths[b], 0), a.n) : a.n;
     const int first = a.window ? max(0, len - a.window) : 0;
     return int2{first / tile, (int)(((int64_t)len + tile - 1) / tile)};
 }
 
-struct Span { int b, index, count, first_span; int2 tiles; int len; };
+// Where a span starts in the list of all sequences' tiles: sequence b, whose tiles are [before, before + ..) of the list.
+struct Start { int b, before, at, end, T; bool aligned; };
 
-// The span of this workgroup: every wavefront finds it by itself.  False: there are fewer spans.
-__device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int tile, Span &s)
+// Sums over the lanes up to this one, on the vector ALU.
+template <int CTRL, int ROWS> __device__ __forceinline__ int add_dpp(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int running_sum(int v)
 {
-    const int lane = threadIdx.x & 63;
-    int T = INT32_MAX;
-    if (a.spans > a.B) {
-        long long total = 0;
-        for (int b = lane; b < a.B; b += 64) {
-            int len;
-            const int2 r = tile_range(a, b, tile, len);
-            total += r.y - r.x;
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-        T = (int)max((long long)kWaves, (total + a.target - 1) / a.target);
-        int before = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 64) {
-            const int b = b0 + lane;
-            int len = 0, c = 0;
-            int2 r{0, 0};
-            if (b < a.B) { r = tile_range(a, b, tile, len); c = max(1, (int)(((long long)(r.y - r.x) + T - 1) / T)); }
-            int incl = c;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(incl, o, 64); if (lane >= o) incl += v; }
-            const unsigned long long past = __ballot(before + incl > span);
-            if (past) {
-                const int at = __ffsll((long long)past) - 1;
-                s.b = b0 + at;
-                s.count = __builtin_amdgcn_readlane(c, at);
-                s.first_span = before + __builtin_amdgcn_readlane(incl, at) - s.count;
-                s.index = span - s.first_span;
-                s.len = __builtin_amdgcn_readlane(len, at);
-                const int x = __builtin_amdgcn_readlane(r.x, at), n = __builtin_amdgcn_readlane(r.y, at) - x;
-                const int each = (n + s.count - 1) / s.count;
-                s.tiles = int2{min(x + s.index * each, x + n), min(x + (s.index + 1) * each, x + n)};
-                return true;
-            }
-            before += __builtin_amdgcn_readlane(incl, 63);
-        }
-        return false;
+    v = add_dpp<0x111, 0xf>(v);             // row_shr 1, 2, 4, 8: within 16 lanes
+    v = add_dpp<0x112, 0xf>(v);
+    v = add_dpp<0x114, 0xf>(v);
+    v = add_dpp<0x118, 0xf>(v);
+    v = add_dpp<0x142, 0xa>(v);             // the last lane of rows 0 and 2 to rows 1 and 3, then of lane 31 to the upper half
+    return add_dpp<0x143, 0xc>(v);
+}
+__device__ __forceinline__ int sum_lanes(int v) { return __builtin_amdgcn_readlane(running_sum(v), 63); }
+
+// Every wavefront adds the lengths up by itself.  False: the list is shorter.
+__device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int tile, Start &s)
+{
+    const int lane = threadIdx.x;
+    int total = 0, tiles = 0;
+    for (int b = lane; b < a.B; b += 64) {
+        const int2 r = tile_range(a, length_of(a, b), tile);
+        tiles = r.y - r.x;
+        total += tiles;
     }
-    s.b = span; s.index = 0; s.count = 1; s.first_span = span;
-    s.tiles = tile_range(a, span, tile, s.len);
-    return true;
+    if (a.B <= 64 && lane >= a.B) tiles = 0;
+    total = sum_lanes(total);
+    s.T = max(1, (int)(((int64_t)total + a.spans - 1) / a.spans));
+    s.aligned = false;
+    if (a.B <= 64) {
+        // a span that goes on to another sequence costs about kCrossing tiles more (the way through length, pages and first tile): where
+        // spans no longer than that suffice that start with a sequence anew, they are taken
+        for (int T = s.T; T <= s.T + kCrossing && !s.aligned; ++T) {
+            const int spans = sum_lanes((tiles + T - 1) / T);
+            if (spans <= a.spans) { s.aligned = true; s.T = T; tiles = (tiles + T - 1) / T * T; total = spans * T; }
+        }
+    }
+    if ((int64_t)span * s.T >= total) return false;
+    s.at = span * s.T;
+    s.end = (int)min((int64_t)s.at + s.T, (int64_t)total);
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        if (a.B > 64) {
+            tiles = 0;
+            if (b0 + lane < a.B) { const int2 r = tile_range(a, length_of(a, b0 + lane), tile); tiles = r.y - r.x; }
+        }
+        const int incl = running_sum(tiles);
+        const unsigned long long past = __ballot(before + incl > s.at);
+        if (past) {
+            const int first = __ffsll((long long)past) - 1;
+            s.b = b0 + first;
+            s.before = before + __builtin_amdgcn_readlane(incl, first) - __builtin_amdgcn_readlane(tiles, first);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    return false;
 }
 
 __device__ __forceinline__ void request16(unsigned lds_addr, const char *from)
@@ -116,6 +130,13 @@ template <int N> __device__ __forceinline__ void wait_requests() { asm volatile(
 // Row `row` of a tile keeps its chunk c of 16 bytes at c ^ swizzle(row): operand reads of 16 rows at one chunk, and the transposing
 // reads of 16 rows at two, then spread over all banks.
 template <int ROWB> __device__ __forceinline__ int swizzle(int row) { return ROWB >= 256 ? row & 15 : (row >> 1) & 7; }
+
+// The product with 16 inner indices, 4 of them in a lane.
+template <bool BF16> __device__ __forceinline__ f4 k16(s4 a, u2 b, f4 c)
+{
+    if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s4, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(h4, a), __builtin_bit_cast(h4, b), c, 0, 0, 0);
+}
 
 __device__ __forceinline__ float max_over_groups(float v)          // over the four lanes that hold one query row
 {
@@ -136,33 +157,116 @@ __device__ __forceinline__ void store4(void *out, int64_t at, int dtype, f4 v)
                                             __builtin_bit_cast(unsigned, __builtin_convertvector(f2{v[2], v[3]}, b2))};
 }
 
-// DT: storage type; DP: d_head, padded; RG: query rows in groups of 16.  Grid: spans x units, a unit's key head first.
-template <int DT, int DP, int RG>
-__global__ void __launch_bounds__(64 * kWaves, 1) k_attend(const AttendArgs a)
+// What a wavefront is built for: storage type, d_head padded, query rows in groups of 16.
+template <int DT_, int DP_, int RG_> struct Form {
+    static constexpr int DT = DT_, DP = DP_, RG = RG_;
+    static constexpr bool F32 = DT == EL_F32, BF16 = DT == EL_BF16;
+    static constexpr int ES = F32 ? 4 : 2, ROWB = DP * ES;
+    static constexpr int TP = F32 || DP == 256 ? 16 : 32;            // positions of a tile
+    static constexpr int TILEB = TP * ROWB;                          // bytes of a tile's keys
+    // Tiles in the ring: one used, one under way.  More wavefronts a compute unit beat deeper rings: with three and four tiles 64 sequences of
+    // 1024 to 4096 positions (8 key heads of 128) take 154 and 200 us for 136, 512 of up to 256 (16 of 64) 65 and 80 for 54.
+    static constexpr int NS = 2;
+    static constexpr int LDS = NS * (2 * TILEB + 256);
+    static constexpr int PER_CU = 163840 / LDS < (RG == 2 ? 8 : 12) ? 163840 / LDS : RG == 2 ? 8 : 12;   // wavefronts that a compute unit holds
+};
+
+template <class F>
+__global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const AttendArgs a)
 {
-    constexpr bool F32 = DT == EL_F32, BF16 = DT == EL_BF16;
-    constexpr int ES = F32 ? 4 : 2, TP = F32 ? 16 : 32, ROWB = DP * ES, CPR = ROWB / 16, NI = TP * ROWB / 1024, RPI = 64 / CPR;
-    constexpr int NS = DP == 64 ? 4 : 2, TILEB = TP * ROWB, PENDING = (NS - 1) * (2 * NI + 1), DT16 = DP / 16;
+    constexpr bool F32 = F::F32, BF16 = F::BF16;
+    constexpr int DT = F::DT, DP = F::DP, RG = F::RG, ES = F::ES, TP = F::TP, ROWB = F::ROWB, NS = F::NS, TILEB = F::TILEB;
+    constexpr int CPR = ROWB / 16, NI = TILEB / 1024, RPI = 64 / CPR, PENDING = (NS - 1) * (2 * NI + 1), DT16 = DP / 16;
     constexpr int QC = F32 ? DP / 16 : DP / 32;                      // pieces of 16 bytes of a query row that a lane holds
     // P in 16 bits: parts that add up to it.  fp16: two (22 bits), times 2^12, which keeps the low part of small ones out of the
     // subnormal numbers; bf16: three (24 bits).  The products that they cost are hidden behind HBM.
     constexpr int NP = F32 ? 1 : BF16 ? 3 : 2;
     constexpr float SHIFT = DT == EL_F16 ? 12.f : 0.f;
-    __shared__ __attribute__((aligned(1024))) char ring[kWaves * NS * 2 * TILEB];
-    __shared__ __attribute__((aligned(256))) int Tb[kWaves][NS][64];
-    __shared__ float2 ml[kWaves][RG][16];
+    __shared__ __attribute__((aligned(1024))) char ring[NS * 2 * TILEB];
+    __shared__ __attribute__((aligned(256))) int Tb[NS][64];
 
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const int units = a.kv_heads * a.row_blocks, span = blockIdx.x / units, unit = blockIdx.x - span * units;
     const int kvh = unit % a.kv_heads, row0 = unit / a.kv_heads * a.rows;
-    Span sp;
-    if (!find_span(a, span, TP, sp)) return;
-    if (a.spans > a.B && sp.index == 0 && unit == 0 && threadIdx.x == 0) a.pieces[sp.b] = int2{sp.first_span, sp.count};
-    const int64_t b = sp.b;
-    const int len = sp.len, first = a.window ? max(0, len - a.window) : 0;
+    EL_LDS(char) *const lds = (EL_LDS(char) *)ring;
+    const unsigned lds_at = (unsigned)(uintptr_t)lds, tb_at = (unsigned)(uintptr_t)(EL_LDS(int) *)&Tb[0][0];
+    const int chunks = a.d * ES / 16;
+    if (chunks < CPR) {                     // columns beyond d_head are never requested: zeros, which a query's zeros meet
+        for (int i = threadIdx.x; i < NS * 2 * TILEB / 16; i += 64) *(u4 *)(ring + i * 16) = u4{0, 0, 0, 0};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    const char *const Kh = a.c.K + kvh * a.c.head;
+    const int64_t k_to_v = a.c.V - a.c.K;
     const float to_exp2 = a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e;  // what a product is multiplied by: the cap's argument
-    const int nt = max(0, (sp.tiles.y - sp.tiles.x - w + kWaves - 1) / kWaves);     // tiles of this wavefront: x + w, x + w + kWaves, ..
 
+    Start st{span, 0, 0, 0, 1, false};
+    if (a.spans && !find_span(a, span, TP, st)) return;
+    // the pieces of this span: the tiles of one sequence after the other
+    for (;;) {
+    int lane = threadIdx.x;
+    asm volatile("" : "+v"(lane));          // (what follows from it is worked out anew for a piece, instead of being held over all of them)
+    const int r16 = lane & 15, g = lane >> 4;
+    const int64_t b = st.b;
+    const int len = length_of(a, st.b), first = a.window ? max(0, len - a.window) : 0;
+    const int2 range = tile_range(a, len, TP);
+    const int tiles = range.y - range.x;
+    if (a.spans && tiles == 0) { ++st.b; continue; }                 // (there is a tile to come: st.b stays below B)
+    int t0 = range.x, nt = tiles, pieces = 1;
+    if (a.spans) {
+        t0 += st.at - st.before;
+        nt = min(range.y - t0, st.end - st.at);
+        pieces = (st.before + tiles - 1) / st.T - st.before / st.T + 1;       // (aligned: st.before is a multiple of T)
+        if (t0 == range.x && unit == 0 && lane == 0) a.pieces[b] = int2{span + st.b, pieces};
+    }
+
+    f4 acc[RG][DT16];
+    float m[RG], l[RG];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        m[rg] = -INFINITY; l[rg] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT16; ++t) acc[rg][t] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int32_t *const table = a.c.table + b * a.c.table_stride;
+    auto slot_of = [&](int i) __attribute__((always_inline)) { return (int)((unsigned)i % NS); };
+    auto position = [&](int i) __attribute__((always_inline)) { return (int64_t)(t0 + i) * TP + (lane & (TP - 1)); };
+    auto request_pages = [&](int i) __attribute__((always_inline)) {
+        const int64_t last = (int64_t)len - 1, t = position(i) < last ? position(i) : last;
+        request4(tb_at + slot_of(i) * 256, table + (unsigned)t / (unsigned)a.c.page_size);
+    };
+    // Requests tile i; returns which of its positions are there.  One that is not is replaced by one that is: what storage without
+    // a meaning holds reaches nothing.
+    auto request_tile = [&](int i) __attribute__((always_inline)) -> unsigned {
+        const int64_t t = position(i);
+        const unsigned slot = (unsigned)(t < len ? t : 0) / (unsigned)a.c.page_size;
+        const int page = Tb[slot_of(i)][lane];
+        const bool valid = t >= first && t < len && page >= 0 && page < a.c.pages;
+        constexpr unsigned ALL = TP == 32 ? 0xffffffffu : 0xffffu;
+        const unsigned mask = (unsigned)__ballot(valid) & ALL;
+        int64_t off = valid ? page * a.c.page + (t - (int64_t)slot * a.c.page_size) * a.c.position : 0;
+        if (mask != ALL) {
+            const int some = mask ? __ffs((int)mask) - 1 : 0;
+            const int lo = __builtin_amdgcn_readlane((int)off, some), hi = __builtin_amdgcn_readlane((int)(off >> 32), some);
+            if (!valid) off = (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo);
+        }
+        const unsigned at = lds_at + slot_of(i) * (2 * TILEB);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int row = j * RPI + lane / CPR, c = (lane % CPR) ^ swizzle<ROWB>(row);
+            const int lo = __shfl((int)off, row, 64), hi = __shfl((int)(off >> 32), row, 64);
+            const char *from = Kh + (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo) + c * 16;
+            if (c < chunks) {               // (at least the first chunk of a row: the instruction is issued, and counted, always)
+                request16(at + j * 1024, from);
+                request16(at + TILEB + j * 1024, from + k_to_v);
+            }
+        }
+        return mask;
+    };
+
+    if (nt > 0) {
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) request_pages(i);
+    }
     // query rows: row r of the key head is beam r / group, head kvh * group + r % group
     u4 q[RG][QC];
     float slope[RG];
@@ -179,71 +283,15 @@ __global__ void __launch_bounds__(64 * kWaves, 1) k_attend(const AttendArgs a)
         }
         slope[rg] = here && a.slopes ? a.slopes[head] * kLog2e : 0.f;
     }
-    f4 acc[RG][DT16];
-    float m[RG], l[RG];
+    // (in registers before the first tile is requested: a wait of the compiler's for them would wait for all that is under way)
 #pragma unroll
     for (int rg = 0; rg < RG; ++rg) {
-        m[rg] = -INFINITY; l[rg] = 0.f;
 #pragma unroll
-        for (int t = 0; t < DT16; ++t) acc[rg][t] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(q[rg][c]));
+        asm volatile("" : "+v"(slope[rg]));
     }
-
-    char *const mine = ring + w * (NS * 2 * TILEB);
-    EL_LDS(char) *const lds = (EL_LDS(char) *)mine;
-    const unsigned lds_at = (unsigned)(uintptr_t)lds, tb_at = (unsigned)(uintptr_t)(EL_LDS(int) *)&Tb[w][0][0];
-    const int chunks = a.d * ES / 16;
-    if (chunks < CPR) {                     // columns beyond d_head are never requested: zeros, which a query's zeros meet
-        for (int i = lane; i < NS * 2 * TILEB / 16; i += 64) *(u4 *)(mine + i * 16) = u4{0, 0, 0, 0};
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    const int32_t *const table = a.c.table + b * a.c.table_stride;
-    const char *const Kh = a.c.K + kvh * a.c.head;
-    const int64_t k_to_v = a.c.V - a.c.K;
-    auto position = [&](int i) __attribute__((always_inline)) { return (int64_t)(sp.tiles.x + w + kWaves * i) * TP + (lane & (TP - 1)); };
-    auto request_pages = [&](int i) __attribute__((always_inline)) {
-        const int64_t last = (int64_t)len - 1, t = position(i) < last ? position(i) : last;
-        request4(tb_at + (i & (NS - 1)) * 256, table + (unsigned)t / (unsigned)a.c.page_size);
-    };
-    // Requests tile i; returns which of its positions are there.  One that is not is replaced by one that is: what storage without
-    // a meaning holds reaches nothing.
-    auto request_tile = [&](int i) __attribute__((always_inline)) -> unsigned {
-        const int64_t t = position(i);
-        const unsigned slot = (unsigned)(t < len ? t : 0) / (unsigned)a.c.page_size;
-        const int page = Tb[w][i & (NS - 1)][lane];
-        const bool valid = t >= first && t < len && page >= 0 && page < a.c.pages;
-        constexpr unsigned ALL = TP == 32 ? 0xffffffffu : 0xffffu;
-        const unsigned mask = (unsigned)__ballot(valid) & ALL;
-        int64_t off = valid ? page * a.c.page + (t - (int64_t)slot * a.c.page_size) * a.c.position : 0;
-        if (mask != ALL) {
-            const int some = mask ? __ffs((int)mask) - 1 : 0;
-            const int lo = __builtin_amdgcn_readlane((int)off, some), hi = __builtin_amdgcn_readlane((int)(off >> 32), some);
-            if (!valid) off = (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo);
-        }
-        const unsigned at = lds_at + (i & (NS - 1)) * (2 * TILEB);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const int row = j * RPI + lane / CPR, c = (lane % CPR) ^ swizzle<ROWB>(row);
-            const int lo = __shfl((int)off, row, 64), hi = __shfl((int)(off >> 32), row, 64);
-            const char *from = Kh + (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo) + c * 16;
-            if (c < chunks) {               // (at least the first chunk of a row: the instruction is issued, and counted, always)
-                request16(at + j * 1024, from);
-                request16(at + TILEB + j * 1024, from + k_to_v);
-            }
-        }
-        return mask;
-    };
-
     unsigned here[NS];
     if (nt > 0) {
-        // (q and slope are in registers before the first request: a wait of the compiler's for them would wait for all that is under way)
-#pragma unroll
-        for (int rg = 0; rg < RG; ++rg) {
-#pragma unroll
-            for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(q[rg][c]));
-            asm volatile("" : "+v"(slope[rg]));
-        }
-#pragma unroll
-        for (int i = 0; i < NS - 1; ++i) request_pages(i);
         wait_requests<0>();
 #pragma unroll
         for (int i = 0; i < NS - 1; ++i) {
@@ -268,8 +316,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) k_attend(const AttendArgs a)
 #pragma unroll
         for (int k = 0; k < NS - 1; ++k) here[k] = here[k + 1];
         if (mask == 0) continue;
-        const EL_LDS(char) *const Kt = lds + (i & (NS - 1)) * (2 * TILEB), *const Vt = Kt + TILEB;
-        const int dist0 = len - 1 - (sp.tiles.x + w + kWaves * i) * TP;             // of the tile's first position
+        const EL_LDS(char) *const Kt = lds + slot_of(i) * (2 * TILEB), *const Vt = Kt + TILEB;
+        const int dist0 = len - 1 - (t0 + i) * TP;             // of the tile's first position
 
         // ---- scores ----
         constexpr int NA = TP / 16;
@@ -362,7 +410,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) k_attend(const AttendArgs a)
 #pragma unroll
             for (int rg = 0; rg < RG; ++rg)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
+                for (int y = 0; y < 2 * NA; ++y) {
                     float u = p[rg][y >> 1][2 * (y & 1)], v = p[rg][y >> 1][2 * (y & 1) + 1];
 #pragma unroll
                     for (int k = 0; k < NP; ++k) {
@@ -382,84 +430,73 @@ __global__ void __launch_bounds__(64 * kWaves, 1) k_attend(const AttendArgs a)
             for (int t = 0; t < DT16; ++t) {
                 const int at = row * ROWB + (((2 * t + ((r16 & 3) >> 1)) ^ swizzle<ROWB>(row)) << 4) + (r16 & 1) * 8;
                 const s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EL_LDS(s4) *)(Vt + at));
-                const s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EL_LDS(s4) *)(Vt + at + 16 * ROWB));
-                const u4 v = __builtin_bit_cast(u4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                if constexpr (TP == 16) {
 #pragma unroll
-                for (int rg = 0; rg < RG; ++rg)
+                    for (int rg = 0; rg < RG; ++rg)
 #pragma unroll
-                    for (int k = 0; k < NP; ++k) acc[rg][t] = Mma<BF16>::s16(v, pp[rg][k], acc[rg][t]);
+                        for (int k = 0; k < NP; ++k) acc[rg][t] = k16<BF16>(v0, u2{pp[rg][k][0], pp[rg][k][1]}, acc[rg][t]);
+                } else {
+                    const s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EL_LDS(s4) *)(Vt + at + 16 * ROWB));
+                    const u4 v = __builtin_bit_cast(u4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+                        for (int k = 0; k < NP; ++k) acc[rg][t] = Mma<BF16>::s16(v, pp[rg][k], acc[rg][t]);
+                }
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // every read of this slot is through before it is requested into
     }
 
-    // ---- the wavefronts' results joined: each finishes every kWaves-th block of 16 columns ----
-#pragma unroll
-    for (int rg = 0; rg < RG; ++rg) {
-        l[rg] = sum_over_groups(l[rg]);
-        if (g == 0) ml[w][rg][r16] = float2{m[rg], l[rg]};
-    }
-    __syncthreads();                                                 // (the ring is read and requested no more)
-    f4 *const X = (f4 *)ring;                                        // [wavefront][row group][block of columns][lane]
-#pragma unroll
-    for (int rg = 0; rg < RG; ++rg)
-#pragma unroll
-        for (int t = 0; t < DT16; ++t) X[((w * RG + rg) * DT16 + t) * 64 + lane] = acc[rg][t];
-    __syncthreads();
-    const bool whole = sp.count == 1;
-    const int64_t slot = (int64_t)blockIdx.x * a.rows;
+    const bool whole = pieces == 1;
+    const int64_t slot = ((int64_t)(span + st.b) * units + unit) * a.rows;
 #pragma unroll
     for (int rg = 0; rg < RG; ++rg) {
         const int rb = 16 * rg + r16, r = row0 + rb;
-        const bool mine_row = rb < a.rows && r < a.R;
-        float M = -INFINITY, L = 0.f, f[kWaves];
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) M = fmaxf(M, ml[k][rg][r16].x);
-        const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
-            f[k] = __builtin_amdgcn_exp2f(ml[k][rg][r16].x - ref);
-            L += f[k] * ml[k][rg][r16].y;
-        }
-        if (M == -INFINITY)                                          // no score, or none above -inf: 0, unless there is a NaN among them
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) { f[k] = 1.f; L = k == 0 ? ml[k][rg][r16].y : L + ml[k][rg][r16].y; }
-        const bool empty = M == -INFINITY && !(L != L);
-        const int64_t out_row = ((b * a.beam + r / a.group) * a.heads + kvh * a.group + r % a.group);
-        if (mine_row && w == 0 && g == 0) {
+        const float M = m[rg], L = sum_over_groups(l[rg]);
+        if (rb >= a.rows || r >= a.R) continue;
+        // no score, or none above -inf: 0, unless there is a NaN among them
+        const bool empty = whole && M == -INFINITY && !(L != L);
+        const int64_t out_row = (b * a.beam + r / a.group) * a.heads + kvh * a.group + r % a.group;
+        if (g == 0) {
             if (!whole) a.part_ml[slot + rb] = float2{M, L};
             else if (a.lse) a.lse[out_row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - SHIFT) * kLn2;
         }
-        const float inv = whole ? (empty ? 0.f : 1.f / L) : 1.f;
+        const float inv = whole ? 1.f / L : 1.f;
 #pragma unroll
-        for (int t0 = 0; t0 < DT16; t0 += kWaves) {
-            const int t = t0 + w, col = 16 * t + 4 * g;
-            f4 o{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < DT16; ++t) {
+            const int col = 16 * t + 4 * g;
+            if (col >= a.d) continue;
+            f4 o;
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-                const f4 x = X[((k * RG + rg) * DT16 + t) * 64 + lane];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += f[k] * x[e];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = empty && whole ? 0.f : o[e] * inv;
-            if (mine_row && col < a.d) {
-                if (whole) store4(a.out, out_row * a.d + col, a.out_dtype, o);
-                else *(f4 *)(a.part_o + (slot + rb) * a.d + col) = o;
-            }
+            for (int e = 0; e < 4; ++e) o[e] = empty ? 0.f : acc[rg][t][e] * inv;
+            if (whole) store4(a.out, out_row * a.d + col, a.out_dtype, o);
+            else *(f4 *)(a.part_o + (slot + rb) * a.d + col) = o;
         }
+    }
+    if (!a.spans) return;
+    st.at += nt;
+    if (st.aligned || st.at >= st.end) return;
+    st.before += tiles;
+    ++st.b;
     }
 }
 
-// Joins the spans of a sequence that was cut: one (sequence, query row, head) a workgroup.  Bound by latency: the statistics of all
-// spans in one round trip, the weighted sums in another.
-__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, float shift)
+// Joins the pieces of a sequence that was cut: one (sequence, query row, head) a workgroup.  Bound by latency: the statistics of all
+// pieces in one round trip, the weighted sums in another.
+__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int tile, float shift)
 {
-    extern __shared__ float weight[];                                // [spans]
+    extern __shared__ float weight[];                                // [pieces]
     __shared__ float red[4];
     __shared__ f4 sums[256];
     const int tid = threadIdx.x, b = blockIdx.x / (a.beam * a.heads), x = blockIdx.x - b * (a.beam * a.heads);
-    const int2 pc = a.pieces[b];
+    const int2 pc = a.pieces[b];                                     // (not written for a sequence without a tile)
+    const int2 range = tile_range(a, length_of(a, b), tile);
+    if (range.y == range.x) {
+        if (tid < a.d / 4) store4(a.out, (int64_t)blockIdx.x * a.d + 4 * tid, a.out_dtype, f4{0.f, 0.f, 0.f, 0.f});
+        if (tid == 0 && a.lse) a.lse[blockIdx.x] = -INFINITY;
+        return;
+    }
     if (pc.y < 2) return;
     const int j = x / a.heads, head = x - j * a.heads, kvh = head / a.group, r = j * a.group + head % a.group;
     const int units = a.kv_heads * a.row_blocks, unit = r / a.rows * a.kv_heads + kvh, rb = r % a.rows;
@@ -492,6 +529,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, float s
     const int d4 = a.d / 4, groups = 256 / d4, grp = tid / d4, col = tid - grp * d4;
     f4 o{0.f, 0.f, 0.f, 0.f};
     if (grp < groups)
+#pragma unroll 8
         for (int s = grp; s < pc.y; s += groups) {
             const f4 v = *(const f4 *)(a.part_o + slot(s) * a.d + 4 * col);
             const float f = weight[s];
@@ -512,25 +550,44 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, float s
 }
 
 // What a call is launched with: host arithmetic.
-struct AttendPlan { int row_groups, row_blocks, rows, target, spans; size_t pieces_bytes, ml_bytes, workspace; };
+struct AttendPlan { int padded, row_groups, row_blocks, rows, tile, spans, grid; size_t pieces_bytes, ml_bytes, workspace; };
+
+template <class Fn>
+void with_form(int dtype, int padded, int row_groups, Fn fn)
+{
+    auto width = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (padded == 64) { if (row_groups == 1) fn(Form<DT, 64, 1>{}); else fn(Form<DT, 64, 2>{}); }
+        else if (padded == 128) { if (row_groups == 1) fn(Form<DT, 128, 1>{}); else fn(Form<DT, 128, 2>{}); }
+        else if (row_groups == 1) fn(Form<DT, 256, 1>{});
+        else if constexpr (DT != EL_F32) fn(Form<DT, 256, 2>{});
+    };
+    if (dtype == EL_F32) width(std::integral_constant<int, EL_F32>{});
+    else if (dtype == EL_F16) width(std::integral_constant<int, EL_F16>{});
+    else width(std::integral_constant<int, EL_BF16>{});
+}
 
 AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n)
 {
     AttendPlan p;
     const int R = beam * (heads / c.kv_heads);
+    p.padded = c.d_head <= 64 ? 64 : c.d_head <= 128 ? 128 : 256;
     // (two groups of rows share a tile's operand reads; in fp32 beyond 128 columns their registers do not suffice)
-    p.row_groups = R <= 16 || (c.dtype == EL_F32 && c.d_head > 128) ? 1 : 2;
+    p.row_groups = R <= 16 || (c.dtype == EL_F32 && p.padded == 256) ? 1 : 2;
     p.row_blocks = (R + 16 * p.row_groups - 1) / (16 * p.row_groups);
     p.rows = R < 16 * p.row_groups ? R : 16 * p.row_groups;
     const int64_t units = (int64_t)c.kv_heads * p.row_blocks;
-    p.target = (int)(units < kWorkgroups ? kWorkgroups / units : 1);
-    const int tile = c.dtype == EL_F32 ? 16 : 32;
-    const int64_t tiles = ((int64_t)n + tile - 1) / tile, each = (tiles + kWaves - 1) / kWaves;     // spans of a sequence, at most
-    const int64_t cut = (int64_t)p.target + B, all = B * each;
-    p.spans = B > kCutMax ? B : (int)(cut < all ? cut : all);
+    int slots = 0;
+    with_form(c.dtype, p.padded, p.row_groups, [&](auto f) { p.tile = f.TP; slots = kComputeUnits * f.PER_CU; });
+    const int64_t tiles = ((int64_t)n + p.tile - 1) / p.tile, all = B * tiles, target = units < slots ? slots / units : 1;
+    // whole sequences: where there are wavefronts enough without a cut and none can be left with much, where the lengths
+    // would take long to add up, and where there is one tile each
+    const bool whole = B > kCutMax || tiles == 1 || all > 1 << 30 || (n <= kShort && B * units >= slots);
+    p.spans = whole ? 0 : (int)(target < all ? target : all);
+    p.grid = (int)((whole ? B : p.spans) * units);
     p.pieces_bytes = p.ml_bytes = p.workspace = 0;
-    if (p.spans > B) {
-        const size_t rows = (size_t)p.spans * units * p.rows;
+    if (p.spans) {
+        const size_t rows = ((size_t)p.spans + B) * units * p.rows;
         p.pieces_bytes = align_up((size_t)B * sizeof(int2), 256);
         p.ml_bytes = align_up(rows * sizeof(float2), 256);
         p.workspace = p.pieces_bytes + p.ml_bytes + rows * c.d_head * sizeof(float);
@@ -538,16 +595,10 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     return p;
 }
 
-template <int DT>
-void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s)
+void launch_attend(const AttendArgs &a, const AttendPlan &p, int dtype, hipStream_t s)
 {
-    const dim3 grid((unsigned)(p.spans * a.kv_heads * p.row_blocks)), block(64 * kWaves);
-#define EL_ATTEND(DP, RG) hipLaunchKernelGGL((k_attend<DT, DP, RG>), grid, block, 0, s, a)
-    if (a.d <= 64) { if (p.row_groups == 1) EL_ATTEND(64, 1); else EL_ATTEND(64, 2); }
-    else if (a.d <= 128) { if (p.row_groups == 1) EL_ATTEND(128, 1); else EL_ATTEND(128, 2); }
-    else if (DT == EL_F32 || p.row_groups == 1) EL_ATTEND(256, 1);
-    else if constexpr (DT != EL_F32) EL_ATTEND(256, 2);
-#undef EL_ATTEND
+    const dim3 grid((unsigned)p.grid);
+    with_form(dtype, p.padded, p.row_groups, [&](auto f) { hipLaunchKernelGGL(k_attend<decltype(f)>, grid, dim3(64), 0, s, a); });
 }
 
 bool finite_non_negative(float x) { return x >= 0.f && x < INFINITY; }
@@ -596,7 +647,7 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     a.slopes = rule->slopes; a.scale = rule->scale; a.softcap = rule->softcap; a.window = rule->window;
     a.n = n; a.B = B; a.beam = beam; a.heads = heads; a.kv_heads = cache->kv_heads; a.d = cache->d_head;
     a.group = heads / cache->kv_heads; a.R = beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
-    a.target = p.target; a.spans = p.spans;
+    a.spans = p.spans;
     a.out = out; a.out_dtype = out_dtype; a.lse = lse;
     if (p.workspace) {
         a.pieces = (int2 *)workspace;
@@ -605,12 +656,10 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     }
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
-    if (cache->dtype == EL_F32) launch_attend<EL_F32>(a, p, s);
-    else if (cache->dtype == EL_F16) launch_attend<EL_F16>(a, p, s);
-    else launch_attend<EL_BF16>(a, p, s);
+    launch_attend(a, p, cache->dtype, s);
     if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
-    if (p.spans > B) {
-        hipLaunchKernelGGL(k_attend_join, dim3((unsigned)(rows * heads)), dim3(256), (p.target + 1) * sizeof(float), s, a, cache->dtype == EL_F16 ? 12.f : 0.f);
+    if (p.spans) {
+        hipLaunchKernelGGL(k_attend_join, dim3((unsigned)(rows * heads)), dim3(256), p.spans * sizeof(float), s, a, p.tile, cache->dtype == EL_F16 ? 12.f : 0.f);
         if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
     }
     return EL_OK;
