@@ -72,6 +72,20 @@ template <> struct Piece<f16_t> {
     }
 };
 
+// How many of the first n keys of a list that goes on with at least 7 zeros are larger: 8 in flight at a time.
+__device__ __forceinline__ int rank_in(const Key *list, int n, Key key)
+{
+    int rank = 0;
+    for (int o = 0; o < n; o += 8) {
+        Key other[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) other[i] = list[o + i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rank += other[i] > key;
+    }
+    return rank;
+}
+
 struct Sums { float m, S, W; };
 __device__ __forceinline__ Sums join(Sums a, Sums b)
 {
@@ -82,18 +96,24 @@ __device__ __forceinline__ Sums join(Sums a, Sums b)
     return Sums{m, fa * a.S + fb * b.S, fa * (a.W + da * a.S) + fb * (b.W + db * b.S)};
 }
 
-// logprob and entropy of a row, by one lane; returns lse.
-template <typename T>
 __device__ __forceinline__ float lse_of(Sums s) { return s.S == 0.f ? 0.f : s.m + __builtin_amdgcn_logf(s.S) * kLn2; }
+
+// The given token's logit; where there is none, NaN (beyond the vocabulary) or +inf (no token given).
 template <typename T>
-__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t r, Sums s)
+__device__ __forceinline__ float given_logit(const ScoreArgs &a, int64_t r)
+{
+    if (!a.logprob) return 0.f;
+    const int t = a.tokens[r];
+    if (t < 0 || t >= a.vocab) return t < 0 ? INFINITY : NAN;
+    const float x = to_f32(((const T *)(a.logits + r * a.row_stride))[t]);
+    return x == INFINITY ? NAN : x;                                  // (a logit of +inf has no log-probability)
+}
+// logprob and entropy of a row, by one lane.
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t r, Sums s, float given)
 {
     const bool none = s.S == 0.f;                                    // no token may follow
     if (a.entropy) a.entropy[r] = none ? 0.f : __builtin_amdgcn_logf(s.S) * kLn2 - s.W / s.S;
-    if (a.logprob) {
-        const int t = a.tokens[r];
-        a.logprob[r] = t < 0 ? 0.f : t >= a.vocab ? NAN : none ? -INFINITY : to_f32(((const T *)(a.logits + r * a.row_stride))[t]) - lse_of<T>(s);
-    }
+    if (a.logprob) a.logprob[r] = given == INFINITY ? 0.f : given - lse_of(s);
 }
 __device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r, int i, Key key, float lse)
 {
@@ -107,7 +127,7 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
 {
     constexpr int N = Piece<T>::N;
     __shared__ unsigned best[kLanes];
-    __shared__ Key cand[kCandidates];
+    __shared__ __attribute__((aligned(16))) Key cand[kCandidates + 8];
     __shared__ Sums part[4];
     __shared__ int count;
     __shared__ Key top[4];
@@ -119,6 +139,8 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     const char *const base = row - lead * (int)sizeof(T);
     const int first = (chunk * NV * kLanes + tid) * N - lead;       // index of this lane's first element; its pieces are kLanes apart
     if (tid == 0) count = 0;
+    if (a.k)
+        for (int i = tid; i < kCandidates + 8; i += kLanes) cand[i] = 0;
 
     u4 v[NV];
 #pragma unroll
@@ -132,6 +154,7 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
             for (int i = 0; i < N; ++i) Piece<T>::set(v[j], i, e + i >= 0 && e + i < a.vocab ? to_f32(((const T *)row)[e + i]) : -INFINITY);
         }
     }
+    const float given = a.chunks == 1 && tid == 0 ? given_logit<T>(a, r) : 0.f;
     float most[NV], m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -160,11 +183,11 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     const bool whole = a.chunks == 1;
     const Sums s = join(join(part[0], part[1]), join(part[2], part[3]));
     if (tid == 0) {
-        if (whole) write_row<T>(a, r, s);
+        if (whole) write_row(a, r, s, given);
         else a.stats[blockIdx.x] = f4{s.m, s.S, s.W, 0.f};
     }
     if (a.k == 0) return;
-    const float lse = lse_of<T>(s);
+    const float lse = lse_of(s);
     auto emit = [&](int i, Key key) __attribute__((always_inline)) {
         if (whole) write_alternative(a, r, i, key, lse);
         else a.keys[(int64_t)blockIdx.x * a.k + i] = key;
@@ -198,8 +221,7 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     if (n <= kCandidates) {
         for (int c = tid; c < n; c += kLanes) {
             const Key key = cand[c];
-            int rank = 0;
-            for (int o = 0; o < n; ++o) rank += cand[o] > key;
+            const int rank = rank_in(cand, n, key);
             if (rank < a.k) emit(rank, key);
         }
         for (int c = n + tid; c < a.k; c += kLanes) emit(c, 0);
@@ -230,70 +252,62 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     }
 }
 
-// The chunks of a row joined: one row a workgroup.  An alternative's place is the number of larger ones, counted in every chunk's
-// descending list by bisection; what lies below some chunk's k-th is none.
+// The chunks of a row joined: one row a workgroup.  Every chunk's list is descending, so what lies below the largest of their last
+// entries is none of the k best; the rest, some tens, is collected and ranked by counting.  Bound by latency: everything is requested at
+// once.
 template <typename T>
 __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
 {
-    extern __shared__ Key list[];                                    // [chunk][k]
+    extern __shared__ __attribute__((aligned(16))) Key list[];       // [chunks * k + 8] what is left, and zeros
     __shared__ Sums part[4];
-    __shared__ Key floor4[4];
+    __shared__ Key last[4];
+    __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t r = blockIdx.x;
     const int total = a.chunks * a.k;
     const Key *const keys = a.keys + r * total;
+    Key key[4], least = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) key[j] = tid + j * kLanes < total ? keys[tid + j * kLanes] : 0;
+    const float given = tid == 0 ? given_logit<T>(a, r) : 0.f;
     Sums s{-INFINITY, 0.f, 0.f};
     for (int c = tid; c < a.chunks; c += kLanes) {
         const f4 v = a.stats[r * a.chunks + c];
         s = join(s, Sums{v[0], v[1], v[2]});
+        if (a.k) { const Key k = keys[(int64_t)c * a.k + a.k - 1]; least = k > least ? k : least; }
     }
-    Key least = 0;
-    for (int i = tid; i < total; i += kLanes) {
-        const Key key = keys[i];
-        list[i] = key;
-        if ((i + 1) % a.k == 0 && key > least) least = key;
-    }
+    if (tid == 0) count = 0;
+    for (int i = tid; i < total + 8; i += kLanes) list[i] = 0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
         s = join(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)});
         const Key other = __shfl_xor(least, o, 64);
         least = least > other ? least : other;
     }
-    if (lane == 0) { part[w] = s; floor4[w] = least; }
+    if (lane == 0) { part[w] = s; last[w] = least; }
     __syncthreads();
     s = join(join(part[0], part[1]), join(part[2], part[3]));
-    if (tid == 0) write_row<T>(a, r, s);
+    if (tid == 0) write_row(a, r, s, given);
     if (a.k == 0) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) least = least > floor4[i] ? least : floor4[i];
-    const float lse = lse_of<T>(s);
-    for (int i = tid; i < total; i += kLanes) {
-        const Key key = list[i];
-        if (key == 0 || key < least) continue;
-        int rank = 0;
-        for (int c = 0; c < a.chunks && rank < a.k; ++c) {
-            int lo = 0, hi = a.k;                                    // the first of the list that is not larger
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (list[c * a.k + mid] > key) lo = mid + 1; else hi = mid;
-            }
-            rank += lo;
-        }
-        if (rank < a.k) write_alternative(a, r, rank, key, lse);
+    for (int i = 0; i < 4; ++i) least = least > last[i] ? least : last[i];
+    if (least == 0) least = 1;                                       // (0: no alternative)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (key[j] >= least) list[atomicAdd(&count, 1)] = key[j];
+    for (int i = tid + 4 * kLanes; i < total; i += kLanes) {
+        const Key k = keys[i];
+        if (k >= least) list[atomicAdd(&count, 1)] = k;
     }
-    // places without an alternative: fewer than k in all chunks together
-    if (least == 0) {
-        int there = 0;
-        for (int c = 0; c < a.chunks; ++c) {
-            int lo = 0, hi = a.k;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (list[c * a.k + mid] > 0) lo = mid + 1; else hi = mid;
-            }
-            there += lo;
-        }
-        for (int i = there + tid; i < a.k; i += kLanes) write_alternative(a, r, i, 0, lse);
+    __syncthreads();
+    const int n = count;
+    const float lse = lse_of(s);
+    for (int c = tid; c < n; c += kLanes) {
+        const Key k = list[c];
+        const int rank = rank_in(list, n, k);
+        if (rank < a.k) write_alternative(a, r, rank, k, lse);
     }
+    for (int i = n + tid; i < a.k; i += kLanes) write_alternative(a, r, i, 0, lse);
 }
 
 // How a call is cut: pieces a lane, chunks of a row.
@@ -327,7 +341,7 @@ void launch_score(const ScoreArgs &a, const ScorePlan &p, int rows, hipStream_t 
     else if (p.pieces == 4) hipLaunchKernelGGL((k_score_chunk<T, 4>), grid, block, 0, s, a);
     else if (p.pieces == 2) hipLaunchKernelGGL((k_score_chunk<T, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_score_chunk<T, 1>), grid, block, 0, s, a);
-    if (p.chunks > 1) hipLaunchKernelGGL((k_score_join<T>), dim3(rows), block, (size_t)p.chunks * a.k * sizeof(Key), s, a);
+    if (p.chunks > 1) hipLaunchKernelGGL((k_score_join<T>), dim3(rows), block, ((size_t)p.chunks * a.k + 8) * sizeof(Key), s, a);
 }
 
 constexpr int64_t kMaxChunks = (int64_t)1 << 23;                     // rows x chunks: a launch has fewer than 2^32 threads
