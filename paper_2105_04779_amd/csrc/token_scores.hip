@@ -1,7 +1,8 @@
 // What a row of logits says about the next token: log-probability of a given one, entropy, the best alternatives.
 //
-//   lse = m + log S,  S = sum exp(x - m),  entropy = log S - W / S,  W = sum exp(x - m) (x - m),  m the largest logit
+//   lse = (m + log2 S) ln 2,  S = sum 2^y,  entropy = (log2 S - W / S) ln 2,  W = sum 2^y y,  y = x log2(e) - m
 //
+// with m the largest logit times log2(e), rounded: whatever it is, it is what y is relative to.
 // Bound by HBM where rows are many: every logit is read once.  A workgroup holds a chunk of a row in registers, so maximum, sums
 // and alternatives are passes over registers.  Rows start anywhere (an odd vocabulary): chunks are cut at 16-byte boundaries of
 // memory, and the pieces of 16 bytes at a row's ends that are not all its own are read element by element.
@@ -27,7 +28,7 @@ typedef unsigned long long Key;
 struct ScoreArgs {
     const char *logits;
     int64_t row_stride;                  // bytes
-    int vocab, k, chunks;
+    int vocab, k, chunks, pieces;        // pieces of 16 bytes of a chunk
     const int32_t *tokens;
     float *logprob, *entropy, *top_logprob;
     int32_t *top_index;
@@ -92,11 +93,11 @@ __device__ __forceinline__ Sums join(Sums a, Sums b)
     const float m = fmaxf(a.m, b.m);
     // (nothing above -inf on a side: its sums are 0, or NaN, and stay)
     const float da = a.m == -INFINITY ? 0.f : a.m - m, db = b.m == -INFINITY ? 0.f : b.m - m;
-    const float fa = __builtin_amdgcn_exp2f(da * kLog2e), fb = __builtin_amdgcn_exp2f(db * kLog2e);
+    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
     return Sums{m, fa * a.S + fb * b.S, fa * (a.W + da * a.S) + fb * (b.W + db * b.S)};
 }
 
-__device__ __forceinline__ float lse_of(Sums s) { return s.S == 0.f ? 0.f : s.m + __builtin_amdgcn_logf(s.S) * kLn2; }
+__device__ __forceinline__ float lse_of(Sums s) { return s.S == 0.f ? 0.f : (s.m + __builtin_amdgcn_logf(s.S)) * kLn2; }
 
 // The given token's logit; where there is none, NaN (beyond the vocabulary) or +inf (no token given).
 template <typename T>
@@ -112,7 +113,7 @@ __device__ __forceinline__ float given_logit(const ScoreArgs &a, int64_t r)
 __device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t r, Sums s, float given)
 {
     const bool none = s.S == 0.f;                                    // no token may follow
-    if (a.entropy) a.entropy[r] = none ? 0.f : __builtin_amdgcn_logf(s.S) * kLn2 - s.W / s.S;
+    if (a.entropy) a.entropy[r] = none ? 0.f : (__builtin_amdgcn_logf(s.S) - s.W / s.S) * kLn2;
     if (a.logprob) a.logprob[r] = given == INFINITY ? 0.f : given - lse_of(s);
 }
 __device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r, int i, Key key, float lse)
@@ -121,7 +122,7 @@ __device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r,
     a.top_index[r * a.k + i] = key ? (int)(0xffffffffu - (unsigned)key) : -1;
 }
 
-// A chunk of NV pieces a lane of one row.  Grid: rows x chunks.
+// A chunk of up to NV pieces a lane of one row.  Grid: rows x chunks.
 template <typename T, int NV>
 __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
 {
@@ -137,7 +138,7 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     const char *const row = a.logits + r * a.row_stride;
     const int lead = (int)((uintptr_t)row & 15) / (int)sizeof(T);   // elements between a 16-byte boundary and the row's first
     const char *const base = row - lead * (int)sizeof(T);
-    const int first = (chunk * NV * kLanes + tid) * N - lead;       // index of this lane's first element; its pieces are kLanes apart
+    const int first = (chunk * a.pieces + tid) * N - lead;          // index of this lane's first element; its pieces are kLanes apart
     if (tid == 0) count = 0;
     if (a.k)
         for (int i = tid; i < kCandidates + 8; i += kLanes) cand[i] = 0;
@@ -145,19 +146,20 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     u4 v[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int64_t e = (int64_t)first + (int64_t)j * kLanes * N;
-        if (e >= 0 && e + N <= a.vocab) {
-            v[j] = __builtin_nontemporal_load((const u4 *)(base + (e + lead) * (int)sizeof(T)));
+        const int e = first + j * kLanes * N, end = j * kLanes + tid < a.pieces ? a.vocab : 0;      // (a chunk's last pieces: -inf in the lanes behind)
+        if (e >= 0 && e + N <= end) {
+            v[j] = __builtin_nontemporal_load((const u4 *)(base + (int64_t)(e + lead) * (int)sizeof(T)));
         } else {                                                     // (-inf where there is no element)
             v[j] = u4{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < N; ++i) Piece<T>::set(v[j], i, e + i >= 0 && e + i < a.vocab ? to_f32(((const T *)row)[e + i]) : -INFINITY);
+            for (int i = 0; i < N; ++i) Piece<T>::set(v[j], i, e + i >= 0 && e + i < end ? to_f32(((const T *)row)[e + i]) : -INFINITY);
         }
     }
     const float given = a.chunks == 1 && tid == 0 ? given_logit<T>(a, r) : 0.f;
     float most[NV], m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        most[j] = -INFINITY;
         most[j] = Piece<T>::at(v[j], 0);
 #pragma unroll
         for (int i = 1; i < N; ++i) most[j] = fmaxf(most[j], Piece<T>::at(v[j], i));
@@ -166,16 +168,18 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     best[tid] = m > -INFINITY ? order32(m) : 0u;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    m *= kLog2e;
     const float ref = m == -INFINITY ? 0.f : m;
     float S = 0.f, W = 0.f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float d = Piece<T>::at(v[j], i) - ref, e = __builtin_amdgcn_exp2f(d * kLog2e);
+            const float y = fmaf(Piece<T>::at(v[j], i), kLog2e, -ref), e = __builtin_amdgcn_exp2f(y);
             S += e;
-            W += e * fmaxf(d, -1e4f);                                // (a banned token: 0, not 0 * inf)
+            W = fmaf(e, fmaxf(y, -1e4f), W);                         // (a banned token: 0, not 0 * inf)
         }
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) { S += __shfl_xor(S, o, 64); W += __shfl_xor(W, o, 64); }
     if (lane == 0) part[w] = Sums{m, S, W};
@@ -231,13 +235,14 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     for (int i = 0; i < a.k; ++i) {
         Key mine = 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+    #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float x = Piece<T>::at(v[j], e);
                 const Key key = x >= least ? key_of(x, first + j * kLanes * N + e) : 0;
                 if (key < last && key > mine) mine = key;
             }
+        }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             const Key other = __shfl_xor(mine, o, 64);
@@ -311,20 +316,18 @@ __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
 }
 
 // How a call is cut: pieces a lane, chunks of a row.
-struct ScorePlan { int pieces, chunks; size_t stats_bytes, workspace; };
+struct ScorePlan { int form, chunks, pieces; size_t stats_bytes, workspace; };
 
 ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
 {
     const int n = 16 / element_size;
-    const int64_t pieces = ((int64_t)vocab + n - 1 + n - 1) / n;     // of a row that starts anywhere between two boundaries
+    const int pieces = (int)(((int64_t)vocab + n - 1 + n - 1) / n);  // of a row that starts anywhere between two boundaries
     ScorePlan p;
-    p.pieces = 8;
-    auto chunks = [&] { return (pieces + (int64_t)p.pieces * kLanes - 1) / ((int64_t)p.pieces * kLanes); };
-    while (p.pieces > 1 && rows * chunks() < kFillWorkgroups) {
-        p.pieces /= 2;
-        if (chunks() * k > kListMax) { p.pieces *= 2; break; }
-    }
-    p.chunks = (int)chunks();
+    p.form = 8;
+    auto chunks = [&](int form) { return (pieces + form * kLanes - 1) / (form * kLanes); };
+    while (p.form > 1 && (int64_t)rows * chunks(p.form) < kFillWorkgroups && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
+    p.chunks = chunks(p.form);
+    p.pieces = (pieces + p.chunks - 1) / p.chunks;                   // chunks of one size
     p.stats_bytes = p.workspace = 0;
     if (p.chunks > 1) {
         p.stats_bytes = align_up((size_t)rows * p.chunks * sizeof(f4), 256);
@@ -337,9 +340,9 @@ template <typename T>
 void launch_score(const ScoreArgs &a, const ScorePlan &p, int rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(rows * p.chunks)), block(kLanes);
-    if (p.pieces == 8) hipLaunchKernelGGL((k_score_chunk<T, 8>), grid, block, 0, s, a);
-    else if (p.pieces == 4) hipLaunchKernelGGL((k_score_chunk<T, 4>), grid, block, 0, s, a);
-    else if (p.pieces == 2) hipLaunchKernelGGL((k_score_chunk<T, 2>), grid, block, 0, s, a);
+    if (p.form == 8) hipLaunchKernelGGL((k_score_chunk<T, 8>), grid, block, 0, s, a);
+    else if (p.form == 4) hipLaunchKernelGGL((k_score_chunk<T, 4>), grid, block, 0, s, a);
+    else if (p.form == 2) hipLaunchKernelGGL((k_score_chunk<T, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_score_chunk<T, 1>), grid, block, 0, s, a);
     if (p.chunks > 1) hipLaunchKernelGGL((k_score_join<T>), dim3(rows), block, ((size_t)p.chunks * a.k + 8) * sizeof(Key), s, a);
 }
@@ -384,7 +387,7 @@ extern "C" el_status el_attn_score_tokens(el_dtype dtype, const void *logits, in
         if (!workspace || workspace_bytes < p.workspace) return EL_ERR_WORKSPACE;
         if ((uintptr_t)workspace & 15) return EL_ERR_INVALID_ARG;
     }
-    const ScoreArgs a{(const char *)logits, row_stride * es, vocab, k, p.chunks, tokens, logprob, entropy, top_logprob, top_index,
+    const ScoreArgs a{(const char *)logits, row_stride * es, vocab, k, p.chunks, p.pieces, tokens, logprob, entropy, top_logprob, top_index,
                       (f4 *)workspace, (Key *)((char *)workspace + p.stats_bytes)};
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
