@@ -27,6 +27,11 @@ namespace {
 
 constexpr int kCrossing = 1;
 constexpr int kComputeUnits = 256;
+// Tiles of a wavefront up to which a workgroup of several takes a whole sequence, without a second launch.  us on the device, cut and joined /
+// whole: bf16, 16 heads of 64, 1 sequence of 613 9.9 / 9.5, 8 of 300 to 400 10.9 / 8.5, 16 of 400 to 800 17.0 / 13.3; 8 key heads of 128, 32 of
+// 200 to 500 19.8 / 15.7, 1 of 500 (four tiles each) 11.0 / 12.6; fp32, 4 of 300 to 500 10.7 / 13.2.  Outside a graph the second launch and its
+// scratch memory cost the host 5 us more than what the last two lose.  With eight tiles they lose 3 to 6 us.
+constexpr int kFew = 4;
 constexpr int kShort = 2048;         // positions that one wavefront may be left with where sequences alone fill the device
 constexpr int kCutMax = 1024;        // most sequences that are cut; beyond them the sequences alone fill the device twice
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -40,6 +45,7 @@ struct AttendArgs {
     float scale, softcap;
     int window, n, B, beam, heads, kv_heads, d;
     int group, R, row_blocks, rows;          // heads / kv_heads; query rows of a key head; blocks of them; rows of a block, at most
+    int waves;                               // of a workgroup: a power of 2; more than one only where they share a whole sequence
     int spans;                               // spans that the tiles of all sequences are cut into, at most; 0: a span is a sequence
     void *out;
     int out_dtype;
@@ -167,12 +173,13 @@ template <int DT_, int DP_, int RG_> struct Form {
     // Tiles in the ring: one used, one under way.  More wavefronts a compute unit beat deeper rings: with three and four tiles 64 sequences of
     // 1024 to 4096 positions (8 key heads of 128) take 154 and 200 us for 136, 512 of up to 256 (16 of 64) 65 and 80 for 54.
     static constexpr int NS = 2;
-    static constexpr int LDS = NS * (2 * TILEB + 256);
+    static constexpr int RING = NS * 2 * TILEB, LDS = RING + NS * 256;             // of a wavefront: tiles, page numbers
     static constexpr int PER_CU = 163840 / LDS < (RG == 2 ? 8 : 12) ? 163840 / LDS : RG == 2 ? 8 : 12;   // wavefronts that a compute unit holds
+    static constexpr int WAVES = PER_CU >= 8 ? 8 : PER_CU >= 4 ? 4 : 2;            // of a workgroup, at most
 };
 
 template <class F>
-__global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const AttendArgs a)
+__global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(const AttendArgs a)
 {
     constexpr bool F32 = F::F32, BF16 = F::BF16;
     constexpr int DT = F::DT, DP = F::DP, RG = F::RG, ES = F::ES, TP = F::TP, ROWB = F::ROWB, NS = F::NS, TILEB = F::TILEB;
@@ -182,16 +189,18 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
     // subnormal numbers; bf16: three (24 bits).  The products that they cost are hidden behind HBM.
     constexpr int NP = F32 ? 1 : BF16 ? 3 : 2;
     constexpr float SHIFT = DT == EL_F16 ? 12.f : 0.f;
-    __shared__ __attribute__((aligned(1024))) char ring[NS * 2 * TILEB];
-    __shared__ __attribute__((aligned(256))) int Tb[NS][64];
+    extern __shared__ __attribute__((aligned(1024))) char shared[];  // [wavefront] ring of tiles; then [wavefront] page numbers of NS tiles
 
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char *const ring = shared + wave * F::RING;
+    int *const Tb = (int *)(shared + a.waves * F::RING + wave * (NS * 256));
     const int units = a.kv_heads * a.row_blocks, span = blockIdx.x / units, unit = blockIdx.x - span * units;
     const int kvh = unit % a.kv_heads, row0 = unit / a.kv_heads * a.rows;
     EL_LDS(char) *const lds = (EL_LDS(char) *)ring;
-    const unsigned lds_at = (unsigned)(uintptr_t)lds, tb_at = (unsigned)(uintptr_t)(EL_LDS(int) *)&Tb[0][0];
+    const unsigned lds_at = (unsigned)(uintptr_t)lds, tb_at = (unsigned)(uintptr_t)(EL_LDS(int) *)Tb;
     const int chunks = a.d * ES / 16;
     if (chunks < CPR) {                     // columns beyond d_head are never requested: zeros, which a query's zeros meet
-        for (int i = threadIdx.x; i < NS * 2 * TILEB / 16; i += 64) *(u4 *)(ring + i * 16) = u4{0, 0, 0, 0};
+        for (int i = threadIdx.x & 63; i < F::RING / 16; i += 64) *(u4 *)(ring + i * 16) = u4{0, 0, 0, 0};
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     const char *const Kh = a.c.K + kvh * a.c.head;
@@ -202,7 +211,7 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
     if (a.spans && !find_span(a, span, TP, st)) return;
     // the pieces of this span: the tiles of one sequence after the other
     for (;;) {
-    int lane = threadIdx.x;
+    int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));          // (what follows from it is worked out anew for a piece, instead of being held over all of them)
     const int r16 = lane & 15, g = lane >> 4;
     const int64_t b = st.b;
@@ -216,6 +225,10 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
         nt = min(range.y - t0, st.end - st.at);
         pieces = (st.before + tiles - 1) / st.T - st.before / st.T + 1;       // (aligned: st.before is a multiple of T)
         if (t0 == range.x && unit == 0 && lane == 0) a.pieces[b] = int2{span + st.b, pieces};
+    } else {                                                         // the workgroup's wavefronts share the sequence
+        const int each = (tiles + a.waves - 1) / a.waves, skip = min(wave * each, tiles);
+        t0 += skip;
+        nt = min(each, tiles - skip);
     }
 
     f4 acc[RG][DT16];
@@ -239,7 +252,7 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
     auto request_tile = [&](int i) __attribute__((always_inline)) -> unsigned {
         const int64_t t = position(i);
         const unsigned slot = (unsigned)(t < len ? t : 0) / (unsigned)a.c.page_size;
-        const int page = Tb[slot_of(i)][lane];
+        const int page = Tb[slot_of(i) * 64 + lane];
         const bool valid = t >= first && t < len && page >= 0 && page < a.c.pages;
         constexpr unsigned ALL = TP == 32 ? 0xffffffffu : 0xffffu;
         const unsigned mask = (unsigned)__ballot(valid) & ALL;
@@ -250,12 +263,14 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
             if (!valid) off = (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo);
         }
         const unsigned at = lds_at + slot_of(i) * (2 * TILEB);
+        int have = chunks;
+        asm volatile("" : "+s"(have));      // (compared anew for a tile: NI masks of lanes held over the loop are more registers than there are)
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
             const int row = j * RPI + lane / CPR, c = (lane % CPR) ^ swizzle<ROWB>(row);
             const int lo = __shfl((int)off, row, 64), hi = __shfl((int)(off >> 32), row, 64);
             const char *from = Kh + (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo) + c * 16;
-            if (c < chunks) {               // (at least the first chunk of a row: the instruction is issued, and counted, always)
+            if (c < have) {                 // (at least the first chunk of a row: the instruction is issued, and counted, always)
                 request16(at + j * 1024, from);
                 request16(at + TILEB + j * 1024, from + k_to_v);
             }
@@ -448,17 +463,59 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // every read of this slot is through before it is requested into
     }
 
+    int waves = a.waves, w = wave;
+    asm volatile("" : "+s"(waves), "+s"(w));                         // (as above)
     const bool whole = pieces == 1;
     const int64_t slot = ((int64_t)(span + st.b) * units + unit) * a.rows;
 #pragma unroll
+    for (int rg = 0; rg < RG; ++rg) l[rg] = sum_over_groups(l[rg]);
+    if (waves > 1) {
+        // the wavefronts' results joined: each finishes every waves-th block of 16 columns
+        float2 *const ml = (float2 *)Tb;                             // (of this wavefront: its own ring is through)
+        f4 *const X = (f4 *)ring;
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+            if (g == 0) ml[16 * rg + r16] = float2{m[rg], l[rg]};
+#pragma unroll
+            for (int t = 0; t < DT16; ++t) X[(rg * DT16 + t) * 64 + lane] = acc[rg][t];
+        }
+        __syncthreads();
+        float2 *const ml0 = (float2 *)(shared + waves * F::RING);
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+            float M = -INFINITY, L = 0.f;
+            for (int k = 0; k < waves; ++k) M = fmaxf(M, ml0[k * (NS * 32) + 16 * rg + r16].x);
+            // (a wavefront without a position: sum 0.  A NaN score leaves its maximum at -inf and its sum at NaN, which stays)
+            auto factor = [&](int k) __attribute__((always_inline)) {
+                const float mk = ml0[k * (NS * 32) + 16 * rg + r16].x;
+                return mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - M);
+            };
+#pragma unroll
+            for (int t = 0; t < DT16; ++t) acc[rg][t] = f4{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < waves; ++k) {
+                const float f = factor(k);
+                L += f * ml0[k * (NS * 32) + 16 * rg + r16].y;
+                const f4 *const Xk = (const f4 *)(shared + k * F::RING);
+#pragma unroll
+                for (int t = 0; t < DT16; ++t) {
+                    if ((t & (waves - 1)) != w) continue;
+                    const f4 x = Xk[(rg * DT16 + t) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[rg][t][e] += f * x[e];
+                }
+            }
+            m[rg] = M; l[rg] = L;
+        }
+    }
+#pragma unroll
     for (int rg = 0; rg < RG; ++rg) {
         const int rb = 16 * rg + r16, r = row0 + rb;
-        const float M = m[rg], L = sum_over_groups(l[rg]);
         if (rb >= a.rows || r >= a.R) continue;
+        const float M = m[rg], L = l[rg];
         // no score, or none above -inf: 0, unless there is a NaN among them
         const bool empty = whole && M == -INFINITY && !(L != L);
         const int64_t out_row = (b * a.beam + r / a.group) * a.heads + kvh * a.group + r % a.group;
-        if (g == 0) {
+        if (g == 0 && w == 0) {
             if (!whole) a.part_ml[slot + rb] = float2{M, L};
             else if (a.lse) a.lse[out_row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - SHIFT) * kLn2;
         }
@@ -466,7 +523,7 @@ __global__ void __launch_bounds__(64, (F::PER_CU + 3) / 4) k_attend(const Attend
 #pragma unroll
         for (int t = 0; t < DT16; ++t) {
             const int col = 16 * t + 4 * g;
-            if (col >= a.d) continue;
+            if (col >= a.d || (t & (waves - 1)) != w) continue;
             f4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = empty ? 0.f : acc[rg][t][e] * inv;
@@ -550,7 +607,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int til
 }
 
 // What a call is launched with: host arithmetic.
-struct AttendPlan { int padded, row_groups, row_blocks, rows, tile, spans, grid; size_t pieces_bytes, ml_bytes, workspace; };
+struct AttendPlan { int padded, row_groups, row_blocks, rows, tile, waves, spans, grid, lds; size_t pieces_bytes, ml_bytes, workspace; };
 
 template <class Fn>
 void with_form(int dtype, int padded, int row_groups, Fn fn)
@@ -577,14 +634,19 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     p.row_blocks = (R + 16 * p.row_groups - 1) / (16 * p.row_groups);
     p.rows = R < 16 * p.row_groups ? R : 16 * p.row_groups;
     const int64_t units = (int64_t)c.kv_heads * p.row_blocks;
-    int slots = 0;
-    with_form(c.dtype, p.padded, p.row_groups, [&](auto f) { p.tile = f.TP; slots = kComputeUnits * f.PER_CU; });
+    int slots = 0, most = 1, lds = 0;
+    with_form(c.dtype, p.padded, p.row_groups, [&](auto f) { p.tile = f.TP; slots = kComputeUnits * f.PER_CU; most = f.WAVES; lds = f.LDS; });
     const int64_t tiles = ((int64_t)n + p.tile - 1) / p.tile, all = B * tiles, target = units < slots ? slots / units : 1;
-    // whole sequences: where there are wavefronts enough without a cut and none can be left with much, where the lengths
-    // would take long to add up, and where there is one tile each
-    const bool whole = B > kCutMax || tiles == 1 || all > 1 << 30 || (n <= kShort && B * units >= slots);
+    p.waves = 1;
+    while (p.waves < most && 2 * p.waves * B * units <= slots && 2 * p.waves <= tiles) p.waves *= 2;
+    // whole sequences: where they alone fill the device and none is long, where the lengths would take long to add up, and where a few
+    // tiles are all that a wavefront gets
+    const bool few = tiles <= (int64_t)kFew * p.waves;
+    const bool whole = few || B > kCutMax || all > 1 << 30 || (n <= kShort && B * units >= slots);
+    if (!few) p.waves = 1;
     p.spans = whole ? 0 : (int)(target < all ? target : all);
     p.grid = (int)((whole ? B : p.spans) * units);
+    p.lds = p.waves * lds;
     p.pieces_bytes = p.ml_bytes = p.workspace = 0;
     if (p.spans) {
         const size_t rows = ((size_t)p.spans + B) * units * p.rows;
@@ -598,7 +660,7 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
 void launch_attend(const AttendArgs &a, const AttendPlan &p, int dtype, hipStream_t s)
 {
     const dim3 grid((unsigned)p.grid);
-    with_form(dtype, p.padded, p.row_groups, [&](auto f) { hipLaunchKernelGGL(k_attend<decltype(f)>, grid, dim3(64), 0, s, a); });
+    with_form(dtype, p.padded, p.row_groups, [&](auto f) { hipLaunchKernelGGL(k_attend<decltype(f)>, grid, dim3(64 * p.waves), p.lds, s, a); });
 }
 
 bool finite_non_negative(float x) { return x >= 0.f && x < INFINITY; }
@@ -647,7 +709,7 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     a.slopes = rule->slopes; a.scale = rule->scale; a.softcap = rule->softcap; a.window = rule->window;
     a.n = n; a.B = B; a.beam = beam; a.heads = heads; a.kv_heads = cache->kv_heads; a.d = cache->d_head;
     a.group = heads / cache->kv_heads; a.R = beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
-    a.spans = p.spans;
+    a.waves = p.waves; a.spans = p.spans;
     a.out = out; a.out_dtype = out_dtype; a.lse = lse;
     if (p.workspace) {
         a.pieces = (int2 *)workspace;
