@@ -389,20 +389,20 @@ def _dtype_code(t):
     return code
 
 
-def _check_operands(device, ints, floats):
-    """`ints`, `floats`: {name: tensor or None}.  All on `device`; index tensors int32; nothing that waits for a gradient
-    (none is computed)."""
+def _check_index(name, t, device, shape):
+    """An index operand: contiguous int32 of that shape on `device`."""
     import torch
-    for name, t in ints.items():
-        if t is not None and (t.dtype != torch.int32 or t.device != device):
-            raise ValueError(f"{name} must be an int32 tensor on {device}")
-    grad = torch.is_grad_enabled()
-    for name, t in floats.items():
-        if t is None:
-            continue
-        if t.device != device:
-            raise ValueError(f"{name} must be on {device}")
-        if grad and t.requires_grad:
+    if t.dtype is not torch.int32 or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+
+
+def _check_values(name, t, device, dtype):
+    """A floating operand on `device`, one that nobody waits for a gradient of: none is computed."""
+    if t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
+    if t.requires_grad:
+        import torch
+        if torch.is_grad_enabled():
             raise ValueError(f"{name} requires a gradient, and none is computed: detach it or use torch.no_grad()")
 
 
@@ -418,10 +418,7 @@ def _call(where, device, fn, *args):
         raise ElAttnError(st, where)
 
 
-def _workspace(nbytes, device):
-    """Scratch memory of one call: torch's allocator keeps it for the stream (or the graph) that the call runs on."""
-    import torch
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+_INT32_MAX = 2 ** 31 - 1
 
 
 class PagedCache:
@@ -431,101 +428,108 @@ class PagedCache:
     K, V: device tensors [pages, page_size, kv_heads, d_head], the last dimension contiguous, with the same strides (a
     transposed view of [pages, kv_heads, page_size, d_head] is as good).  The table [B, columns] int32 and the lengths
     int32 [B] are the caller's, shared by all layers: position t of sequence b lies in page table[b, t // page_size];
-    an entry outside the pool (-1) holds no positions.
+    an entry outside the pool (-1) holds no positions.  Scratch memory comes from torch per call, so calls on several streams
+    and captured graphs keep apart.
     """
 
     def __init__(self, K, V):
+        import torch
+        self._torch = torch
         if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype or K.stride() != V.stride():
             raise ValueError("K and V must be [pages, page_size, kv_heads, d_head] of one dtype and the same strides")
         if not K.is_cuda or K.device != V.device:
             raise ValueError("K and V must be on one device")
-        if K.stride(3) != 1:
-            raise ValueError("the last dimension of K and V must be contiguous")
+        if K.stride(3) != 1 or max(K.shape) > _INT32_MAX:
+            raise ValueError("the last dimension of K and V must be contiguous, and every dimension below 2^31")
         if K.requires_grad or V.requires_grad:
             raise ValueError("K and V are written in place: they must not require a gradient")
         self.K, self.V = K, V
         self.device = K.device
         pages, self.page_size, self.kv_heads, self.d_head = K.shape
         self.dtype = _dtype_code(K)
+        self._element = K.dtype
         self._pages = ElAttnPages(_ptr(K), _ptr(V), K.stride(0), K.stride(1), K.stride(2),
                                   pages, self.page_size, self.kv_heads, self.d_head, self.dtype)
 
     def _table(self, table, B):
-        if table.dim() != 2 or table.shape[0] != B:
-            raise ValueError(f"table must be [{B}, columns]")
-        columns = table.shape[1]
-        if columns > 1 and table.stride(1) != 1:
-            raise ValueError("rows of the table must be contiguous")
-        return _ptr(table), table.stride(0) if B > 1 else columns, columns
+        """(address, row stride, columns) of a table for B sequences."""
+        shape, strides = table.shape, table.stride()
+        if len(shape) != 2 or shape[0] != B or (shape[1] > 1 and strides[1] != 1):
+            raise ValueError(f"table must be [{B}, columns] with contiguous rows")
+        if table.dtype is not self._torch.int32 or table.device != self.device:
+            raise ValueError(f"table must be an int32 tensor on {self.device}")
+        return table.data_ptr(), strides[0] if B > 1 else shape[1], shape[1]
 
     def append(self, k, v, table, lengths, counts=None):
         """New tokens k, v [B, T, kv_heads, d_head] (heads of a token contiguous, other strides free, the same for both) to
         the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already."""
-        if k.dim() != 4 or k.shape != v.shape or k.shape[2:] != (self.kv_heads, self.d_head):
+        shape, strides, device = k.shape, k.stride(), self.device
+        if len(shape) != 4 or shape != v.shape or shape[2] != self.kv_heads or shape[3] != self.d_head:
             raise ValueError(f"k and v must be [B, T, {self.kv_heads}, {self.d_head}]")
-        if k.dtype != self.K.dtype or v.dtype != k.dtype:
-            raise ValueError(f"k and v must be {self.K.dtype}")
-        B, T = k.shape[:2]
-        strides = k.stride()
         if strides[3] != 1 or (self.kv_heads > 1 and strides[2] != self.d_head) or v.stride() != strides:
             raise ValueError("a token's heads must be contiguous, and k and v have the same strides")
-        _check_operands(self.device, {"table": table, "lengths": lengths, "counts": counts}, {"k": k, "v": v})
-        for name, t in (("lengths", lengths), ("counts", counts)):
-            if t is not None and (t.shape != (B,) or not t.is_contiguous()):
-                raise ValueError(f"{name} must be contiguous [{B}]")
+        _check_values("k", k, device, self._element)
+        _check_values("v", v, device, self._element)
+        B, T = shape[0], shape[1]
+        _check_index("lengths", lengths, device, (B,))
+        if counts is not None:
+            _check_index("counts", counts, device, (B,))
         row = self.kv_heads * self.d_head
-        _call("el_attn_paged_append", self.device, lib.el_attn_paged_append, self._pages, *self._table(table, B),
-              _ptr(lengths), _ptr(counts), _ptr(k), _ptr(v), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
+        at, stride, columns = self._table(table, B)
+        _call("el_attn_paged_append", device, lib.el_attn_paged_append, self._pages, at, stride, columns, lengths.data_ptr(),
+              _ptr(counts), k.data_ptr(), v.data_ptr(), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
 
     def _attend(self, queries, table, lengths, n, scale, softcap, window, slopes, out, out_code, lse):
-        import torch
-        B, beam, heads, d = queries.shape
-        if lengths is not None and (lengths.shape != (B,) or not lengths.is_contiguous()):
-            raise ValueError(f"lengths must be contiguous [{B}]")
-        if slopes is not None and (slopes.shape != (heads,) or slopes.dtype != torch.float32 or not slopes.is_contiguous()):
-            raise ValueError(f"slopes must be contiguous float32 [{heads}]")
+        """`queries` has been found to be [B, beam, heads, d_head] of this cache's type."""
+        (B, beam, heads, d), strides, device = queries.shape, queries.stride(), self.device
+        if strides[3] != 1 or (heads > 1 and strides[2] != d):
+            raise ValueError("the heads of a query must be contiguous")
+        if B > 1 and beam > 1 and strides[0] != beam * strides[1]:
+            raise ValueError("query rows must be evenly spaced")
+        if lengths is not None:
+            _check_index("lengths", lengths, device, (B,))
+        if slopes is not None:
+            _check_values("slopes", slopes, device, self._torch.float32)
+            if slopes.shape != (heads,) or not slopes.is_contiguous():
+                raise ValueError(f"slopes must be contiguous [{heads}]")
         at, stride, columns = self._table(table, B)
         if n is None:
-            n = columns * self.page_size
+            n = min(columns * self.page_size, _INT32_MAX)
+        if abs(n) > _INT32_MAX or abs(window) > _INT32_MAX:
+            raise ValueError("n and window must be 32-bit numbers")
         rule = ElAttnScoreRule(d ** -0.5 if scale is None else scale, softcap, window, _ptr(slopes))
-        q_stride = queries.stride(1) if beam > 1 else queries.stride(0) if B > 1 else heads * d
         nbytes = lib.el_attn_paged_workspace_bytes(self._pages, heads, B, beam, n)
-        ws = _workspace(nbytes, self.device)
-        _call("el_attn_paged_attend", self.device, lib.el_attn_paged_attend, self._pages, at, stride, columns, _ptr(lengths),
-              _ptr(queries), q_stride, heads, rule, _ptr(out), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
+        ws = self._torch.empty(nbytes, dtype=self._torch.uint8, device=device) if nbytes else None
+        _call("el_attn_paged_attend", device, lib.el_attn_paged_attend, self._pages, at, stride, columns, _ptr(lengths),
+              queries.data_ptr(), strides[1] if beam > 1 else strides[0] if B > 1 else heads * d, heads, rule,
+              out.data_ptr(), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
 
-    def _check_queries(self, queries, table, lengths, slopes):
-        if queries.dim() != 4 or queries.shape[3] != self.d_head or queries.shape[2] % self.kv_heads != 0:
+    def _check_queries(self, queries):
+        shape = queries.shape
+        if len(shape) != 4 or shape[3] != self.d_head or shape[2] % self.kv_heads != 0:
             raise ValueError(f"queries must be [B, beam, heads, {self.d_head}], heads a multiple of {self.kv_heads}")
-        if queries.dtype != self.K.dtype:
-            raise ValueError(f"queries must be {self.K.dtype}")
-        B, beam, heads, d = queries.shape
-        if queries.stride(3) != 1 or (heads > 1 and queries.stride(2) != d):
-            raise ValueError("the heads of a query must be contiguous")
-        if B > 1 and beam > 1 and queries.stride(0) != beam * queries.stride(1):
-            raise ValueError("query rows must be evenly spaced")
-        _check_operands(self.device, {"table": table, "lengths": lengths}, {"queries": queries, "slopes": slopes})
+        _check_values("queries", queries, self.device, self._element)
 
     def attend(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None,
                out_dtype=None, out=None):
         """Attention of queries [B, beam, heads, d_head] over each sequence's lengths[b] positions (None: n; n: the most that
         any sequence has, default what the table holds).  Returns out [B, beam, heads, d_head] in `out_dtype` ("f32" or the
         cache's own, the default).  See el_attn_score_rule for scale (default d_head ** -0.5), softcap, window and slopes."""
-        import torch
-        self._check_queries(queries, table, lengths, slopes)
+        self._check_queries(queries)
         code = self.dtype if out_dtype is None else DTYPE_CODES[out_dtype]
+        element = self._element if code == self.dtype else _torch_dtype(code)
         if out is None:
-            out = torch.empty(queries.shape, dtype=_torch_dtype(code), device=self.device)
-        elif out.shape != queries.shape or out.dtype != _torch_dtype(code) or not out.is_contiguous() or out.device != self.device:
-            raise ValueError(f"out must be a contiguous {_torch_dtype(code)} tensor of the queries' shape")
+            out = self._torch.empty(queries.shape, dtype=element, device=self.device)
+        elif out.shape != queries.shape or out.dtype != element or not out.is_contiguous() or out.device != self.device:
+            raise ValueError(f"out must be a contiguous {element} tensor of the queries' shape")
         self._attend(queries, table, lengths, n, scale, softcap, window, slopes, out, code, None)
         return out
 
     def attend_segment(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None):
         """The same as a segment (seg_A [B*beam, heads*d_head], seg_lse [B*beam, heads], float32) for
         ElAttention.merge_segments."""
-        import torch
-        self._check_queries(queries, table, lengths, slopes)
+        torch = self._torch
+        self._check_queries(queries)
         B, beam, heads, d = queries.shape
         A = torch.empty((B * beam, heads * d), dtype=torch.float32, device=self.device)
         lse = torch.empty((B * beam, heads), dtype=torch.float32, device=self.device)
@@ -535,12 +539,13 @@ class PagedCache:
     def copy_pages(self, src, dst, counts=None):
         """Positions [0, counts[i]) (default all) of page dst[i] become those of page src[i]; int32 device tensors.  No page
         may be the destination of two pairs, or the destination of one and the source of another."""
-        pairs = src.shape[0] if src.dim() == 1 else -1
-        _check_operands(self.device, {"src": src, "dst": dst, "counts": counts}, {})
-        for t in (src, dst, counts):
-            if t is not None and (pairs < 0 or t.shape != (pairs,) or not t.is_contiguous()):
-                raise ValueError("src, dst and counts must be contiguous and of one length")
-        _call("el_attn_paged_copy", self.device, lib.el_attn_paged_copy, self._pages, _ptr(src), _ptr(dst), _ptr(counts), pairs)
+        device, shape = self.device, (src.numel(),)
+        _check_index("src", src, device, shape)
+        _check_index("dst", dst, device, shape)
+        if counts is not None:
+            _check_index("counts", counts, device, shape)
+        _call("el_attn_paged_copy", device, lib.el_attn_paged_copy, self._pages, src.data_ptr(), dst.data_ptr(), _ptr(counts),
+              shape[0])
 
 
 def score_tokens(logits, tokens=None, *, k=0):
@@ -548,24 +553,29 @@ def score_tokens(logits, tokens=None, *, k=0):
     top_logprob, top_index), float32 [rows], [rows], [rows, k] and int32 [rows, k].  logprob is that of tokens (int32 [rows];
     None: logprob is None); the k best alternatives come in descending order.  See el_attn_score_tokens."""
     import torch
-    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    shape = logits.shape
+    if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and logits.stride(1) != 1) or max(shape) > _INT32_MAX:
         raise ValueError("logits must be a device tensor [rows, vocab] with contiguous rows")
-    rows, vocab = logits.shape
+    rows, vocab = shape
     device, code = logits.device, _dtype_code(logits)
-    _check_operands(device, {"tokens": tokens}, {"logits": logits})
-    if tokens is not None and (tokens.shape != (rows,) or not tokens.is_contiguous()):
-        raise ValueError(f"tokens must be contiguous [{rows}]")
-    if not 0 <= k <= el_attn_max_alternatives():
-        raise ValueError(f"k must lie in [0, {el_attn_max_alternatives()}]")
-    logprob = None if tokens is None else torch.empty(rows, dtype=torch.float32, device=device)
-    entropy = torch.empty(rows, dtype=torch.float32, device=device)
-    top_logprob = torch.empty((rows, k), dtype=torch.float32, device=device)
+    _check_values("logits", logits, device, logits.dtype)
+    if tokens is not None:
+        _check_index("tokens", tokens, device, (rows,))
+    if not 0 <= k <= _MAX_ALTERNATIVES:
+        raise ValueError(f"k must lie in [0, {_MAX_ALTERNATIVES}]")
+    f32 = torch.float32
+    logprob = None if tokens is None else torch.empty(rows, dtype=f32, device=device)
+    entropy = torch.empty(rows, dtype=f32, device=device)
+    top_logprob = torch.empty((rows, k), dtype=f32, device=device)
     top_index = torch.empty((rows, k), dtype=torch.int32, device=device)
     nbytes = lib.el_attn_score_workspace_bytes(rows, vocab, k)
-    ws = _workspace(nbytes, device)
-    _call("el_attn_score_tokens", device, lib.el_attn_score_tokens, code, _ptr(logits), logits.stride(0) if rows > 1 else vocab,
-          rows, vocab, _ptr(tokens), _ptr(logprob), _ptr(entropy), k, _ptr(top_logprob), _ptr(top_index), _ptr(ws), nbytes)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _call("el_attn_score_tokens", device, lib.el_attn_score_tokens, code, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab,
+          rows, vocab, _ptr(tokens), _ptr(logprob), entropy.data_ptr(), k, top_logprob.data_ptr(), top_index.data_ptr(), _ptr(ws), nbytes)
     return logprob, entropy, top_logprob, top_index
+
+
+_MAX_ALTERNATIVES = el_attn_max_alternatives()
 
 
 class ElAttention:
