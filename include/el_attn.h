@@ -470,7 +470,7 @@ el_status el_attn_paged_append(const el_attn_pages *cache,
  *
  * A page may be the source of several pairs.  The caller sees to it that no page is the destination of two pairs, or the
  * destination of one and the source of another.  Positions at or behind a count stay as they were.
- * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (also a page of 32 GB or more), HIP.
  */
 el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_t *src, const int32_t *dst, const int32_t *counts,
                              int32_t pairs, void *stream);

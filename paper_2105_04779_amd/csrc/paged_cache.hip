@@ -78,21 +78,38 @@ __global__ void __launch_bounds__(256) k_append(const AppendArgs a)
 struct CopyArgs {
     PageView c;
     const int32_t *src, *dst, *counts;
-    int kv_heads, chunks;
+    unsigned kv_heads, chunks;
+    int heads_first;                         // a head's positions lie closer together than a position's heads
 };
 
-// One pair a workgroup.
+// Grid: (pairs, slices of a page).  Bound by HBM: four pieces of K and of V on their way per lane.
 __global__ void __launch_bounds__(256) k_copy(const CopyArgs a)
 {
     const int src = a.src[blockIdx.x], dst = a.dst[blockIdx.x];
     if (src < 0 || src >= a.c.pages || dst < 0 || dst >= a.c.pages || src == dst) return;
-    const int count = a.counts ? min(max(a.counts[blockIdx.x], 0), a.c.page_size) : a.c.page_size;
-    const int64_t row = (int64_t)a.kv_heads * a.chunks;
-    for (int64_t k = threadIdx.x; k < count * row; k += 256) {
-        const int64_t t = k / row, r = k - t * row, h = r / a.chunks;
-        const int64_t at = t * a.c.position + h * a.c.head + (r - h * a.chunks) * 16;
-        *(u4v *)(a.c.K + dst * a.c.page + at) = *(const u4v *)(a.c.K + src * a.c.page + at);
-        *(u4v *)(a.c.V + dst * a.c.page + at) = *(const u4v *)(a.c.V + src * a.c.page + at);
+    const unsigned count = a.counts ? min(max(a.counts[blockIdx.x], 0), a.c.page_size) : a.c.page_size;
+    const unsigned total = count * a.kv_heads * a.chunks, inner = (a.heads_first ? count : a.kv_heads) * a.chunks;
+    const int64_t outer_step = a.heads_first ? a.c.head : a.c.position, inner_step = a.heads_first ? a.c.position : a.c.head;
+    const char *const Ks = a.c.K + src * a.c.page, *const Vs = a.c.V + src * a.c.page;
+    char *const Kd = a.c.K + dst * a.c.page, *const Vd = a.c.V + dst * a.c.page;
+    // pieces in the order of memory, as far as the strides allow
+    auto place = [&](unsigned k) {
+        const unsigned o = k / inner, r = k - o * inner, i = r / a.chunks;
+        return o * outer_step + i * inner_step + (r - i * a.chunks) * 16;
+    };
+    constexpr int AHEAD = 4;
+    for (unsigned k0 = blockIdx.y * (256 * AHEAD); k0 < total; k0 += gridDim.y * (256 * AHEAD)) {
+        u4v kk[AHEAD], vv[AHEAD];
+        int64_t at[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const unsigned k = k0 + j * 256 + threadIdx.x;
+            at[j] = k < total ? place(k) : -1;
+            if (at[j] >= 0) { kk[j] = *(const u4v *)(Ks + at[j]); vv[j] = *(const u4v *)(Vs + at[j]); }
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (at[j] >= 0) { *(u4v *)(Kd + at[j]) = kk[j]; *(u4v *)(Vd + at[j]) = vv[j]; }
     }
 }
 
@@ -127,8 +144,14 @@ extern "C" el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_
     if (!src || !dst || pairs < 1 || pairs > 1 << 23) return EL_ERR_INVALID_ARG;
     if (((uintptr_t)src | (uintptr_t)dst | (uintptr_t)counts) & 3) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)el::dtype_size(cache->dtype);
-    const el::CopyArgs a{el::page_view(*cache, nullptr, 0, 0), src, dst, counts, cache->kv_heads, (int)(cache->d_head * es / 16)};
+    const int64_t chunks = cache->d_head * es / 16, pieces = (int64_t)cache->page_size * cache->kv_heads * chunks;
+    if (pieces > INT32_MAX) return EL_ERR_UNSUPPORTED;
+    const el::CopyArgs a{el::page_view(*cache, nullptr, 0, 0), src, dst, counts, (unsigned)cache->kv_heads, (unsigned)chunks,
+                         cache->position_stride < cache->head_stride};
+    // slices: eight workgroups a compute unit where the pages have work for them
+    const int64_t most = (pieces + 1023) / 1024, want = (2048 + pairs - 1) / pairs;
+    const dim3 grid(pairs, (unsigned)(most < want ? most : want));
     (void)hipGetLastError();
-    hipLaunchKernelGGL(el::k_copy, dim3(pairs), dim3(256), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(el::k_copy, grid, dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
 }

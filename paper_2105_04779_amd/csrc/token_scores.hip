@@ -5,7 +5,7 @@
 // with m the largest logit times log2(e), rounded: whatever it is, it is what y is relative to.
 // Bound by HBM where rows are many: every logit is read once.  A workgroup holds a chunk of a row in registers, so maximum, sums
 // and alternatives are passes over registers.  Rows start anywhere (an odd vocabulary): chunks are cut at 16-byte boundaries of
-// memory, and the pieces of 16 bytes at a row's ends that are not all its own are read element by element.
+// memory, and the elements at a row's ends that do not fill 16 bytes are a lane's each.
 // Alternatives: the k-th largest of the 256 lanes' maxima has k elements at or above it, so whatever lies below it is none of the
 // chunk's k best; about as many as k are left, and are ranked by counting.  k_score_join joins the chunks of a row.
 #include <cfloat>
@@ -49,28 +49,18 @@ template <typename T> struct Piece;      // 16 bytes of logits
 template <> struct Piece<float> {
     static constexpr int N = 4;
     static __device__ __forceinline__ float at(u4 v, int i) { return __uint_as_float(v[i]); }
-    static __device__ __forceinline__ void set(u4 &v, int i, float x) { v[i] = __float_as_uint(x); }
+    static __device__ __forceinline__ u4 none() { return u4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }      // all -inf
 };
 template <> struct Piece<bf16_t> {
     static constexpr int N = 8;
     static __device__ __forceinline__ float at(u4 v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
-    static __device__ __forceinline__ void set(u4 &v, int i, float x)
-    {
-        const unsigned u = __float_as_uint(x) >> 16;                 // (a bf16 value: exact)
-        v[i >> 1] = i & 1 ? (v[i >> 1] & 0xffffu) | (u << 16) : (v[i >> 1] & 0xffff0000u) | u;
-    }
+    static __device__ __forceinline__ u4 none() { return u4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
 };
 template <> struct Piece<f16_t> {
     static constexpr int N = 8;
     // (a bit cast of a vector's element itself takes element 0 whatever the index: through a copy)
     static __device__ __forceinline__ float at(u4 v, int i) { const unsigned u = v[i >> 1]; return (float)__builtin_bit_cast(h2, u)[i & 1]; }
-    static __device__ __forceinline__ void set(u4 &v, int i, float x)
-    {
-        const unsigned u = v[i >> 1];
-        h2 h = __builtin_bit_cast(h2, u);
-        h[i & 1] = (_Float16)x;
-        v[i >> 1] = __builtin_bit_cast(unsigned, h);
-    }
+    static __device__ __forceinline__ u4 none() { return u4{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u}; }
 };
 
 // How many of the first n keys of a list that goes on with at least 7 zeros are larger: 8 in flight at a time.
@@ -122,6 +112,61 @@ __device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r,
     a.top_index[r * a.k + i] = key ? (int)(0xffffffffu - (unsigned)key) : -1;
 }
 
+// Where a row's `full` pieces of 16 bytes lie: the first behind `head` elements, at a 16-byte boundary.
+struct Row { const char *row; int head, full; };
+template <typename T>
+__device__ __forceinline__ Row row_at(const ScoreArgs &a, int64_t r)
+{
+    const char *const row = a.logits + r * a.row_stride;
+    const int head = min((int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T), a.vocab);
+    return Row{row, head, (a.vocab - head) / Piece<T>::N};
+}
+// Piece p, if it is below `end`; -inf otherwise.
+template <typename T>
+__device__ __forceinline__ u4 load_piece(const Row &x, int p, int end)
+{
+    if (p < end) return __builtin_nontemporal_load((const u4 *)(x.row + x.head * (int)sizeof(T)) + p);
+    return Piece<T>::none();
+}
+// The elements around the pieces, fewer than 2 N, are one lane's each: index of lane t's, or -1.
+template <typename T>
+__device__ __forceinline__ int edge_of(const Row &x, int t, int vocab)
+{
+    const int i = t < x.head ? t : t + x.full * Piece<T>::N;
+    return t < 2 * Piece<T>::N && i < vocab ? i : -1;
+}
+
+template <typename T>
+__device__ __forceinline__ float largest(u4 v)
+{
+    float m = Piece<T>::at(v, 0);
+#pragma unroll
+    for (int i = 1; i < Piece<T>::N; ++i) m = fmaxf(m, Piece<T>::at(v, i));
+    return m;
+}
+__device__ __forceinline__ void add_term(float x, float ref, float &S, float &W)
+{
+    const float y = fmaf(x, kLog2e, -ref), e = __builtin_amdgcn_exp2f(y);
+    S += e;
+    W = fmaf(e, fmaxf(y, -1e4f), W);                                 // (a banned token: 0, not 0 * inf)
+}
+
+// The k-th largest of the numbers of `COUNT` x 64 lanes, by its upper 16 bits (0: fewer than k are above 0).
+template <int COUNT>
+__device__ __forceinline__ unsigned kth_of(const unsigned (&mine)[COUNT], int k)
+{
+    unsigned bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const unsigned t = bound | (1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) n += __popcll(__ballot(mine[i] >= t));
+        if (n >= k) bound = t;
+    }
+    return bound;
+}
+
 // A chunk of up to NV pieces a lane of one row.  Grid: rows x chunks.
 template <typename T, int NV>
 __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
@@ -135,10 +180,9 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t r = blockIdx.x / a.chunks;
     const int chunk = blockIdx.x - (int)r * a.chunks;
-    const char *const row = a.logits + r * a.row_stride;
-    const int lead = (int)((uintptr_t)row & 15) / (int)sizeof(T);   // elements between a 16-byte boundary and the row's first
-    const char *const base = row - lead * (int)sizeof(T);
-    const int first = (chunk * a.pieces + tid) * N - lead;          // index of this lane's first element; its pieces are kLanes apart
+    const Row row = row_at<T>(a, r);
+    const int used = NV < 16 ? NV : (a.pieces + kLanes - 1) / kLanes;          // (uniform) pieces that some lane has
+    const int from = chunk * a.pieces + tid, end = min((chunk + 1) * a.pieces, row.full);           // this lane's pieces: kLanes apart
     if (tid == 0) count = 0;
     if (a.k)
         for (int i = tid; i < kCandidates + 8; i += kLanes) cand[i] = 0;
@@ -146,24 +190,20 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     u4 v[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int e = first + j * kLanes * N, end = j * kLanes + tid < a.pieces ? a.vocab : 0;      // (a chunk's last pieces: -inf in the lanes behind)
-        if (e >= 0 && e + N <= end) {
-            v[j] = __builtin_nontemporal_load((const u4 *)(base + (int64_t)(e + lead) * (int)sizeof(T)));
-        } else {                                                     // (-inf where there is no element)
-            v[j] = u4{0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < N; ++i) Piece<T>::set(v[j], i, e + i >= 0 && e + i < end ? to_f32(((const T *)row)[e + i]) : -INFINITY);
-        }
+        v[j] = Piece<T>::none();
+        if (j < used) v[j] = load_piece<T>(row, from + j * kLanes, end);
     }
+    const int edge = chunk == 0 ? edge_of<T>(row, tid, a.vocab) : -1;
+    const float x_edge = edge >= 0 ? to_f32(((const T *)row.row)[edge]) : -INFINITY;
     const float given = a.chunks == 1 && tid == 0 ? given_logit<T>(a, r) : 0.f;
-    float most[NV], m = -INFINITY;
+    float most[NV], m = x_edge;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         most[j] = -INFINITY;
-        most[j] = Piece<T>::at(v[j], 0);
-#pragma unroll
-        for (int i = 1; i < N; ++i) most[j] = fmaxf(most[j], Piece<T>::at(v[j], i));
+        if (j >= used) continue;
+        most[j] = largest<T>(v[j]);
         m = fmaxf(m, most[j]);
+        asm volatile("" : "+v"(v[j]));                               // (one piece unpacked at a time)
     }
     best[tid] = m > -INFINITY ? order32(m) : 0u;
 #pragma unroll
@@ -171,14 +211,13 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     m *= kLog2e;
     const float ref = m == -INFINITY ? 0.f : m;
     float S = 0.f, W = 0.f;
+    add_term(x_edge, ref, S, W);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        if (j >= used) continue;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = fmaf(Piece<T>::at(v[j], i), kLog2e, -ref), e = __builtin_amdgcn_exp2f(y);
-            S += e;
-            W = fmaf(e, fmaxf(y, -1e4f), W);                         // (a banned token: 0, not 0 * inf)
-        }
+        for (int i = 0; i < N; ++i) add_term(Piece<T>::at(v[j], i), ref, S, W);
+        asm volatile("" : "+v"(v[j]));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) { S += __shfl_xor(S, o, 64); W += __shfl_xor(W, o, 64); }
@@ -196,29 +235,21 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
         if (whole) write_alternative(a, r, i, key, lse);
         else a.keys[(int64_t)blockIdx.x * a.k + i] = key;
     };
-    // the k-th largest of the lanes' maxima, by its upper 16 bits (0: fewer than k lanes have an alternative)
-    unsigned bound = 0;
-    {
-        const unsigned b0 = best[lane], b1 = best[lane + 64], b2 = best[lane + 128], b3 = best[lane + 192];
-#pragma unroll
-        for (int bit = 31; bit >= 16; --bit) {
-            const unsigned t = bound | (1u << bit);
-            const int n = __popcll(__ballot(b0 >= t)) + __popcll(__ballot(b1 >= t)) + __popcll(__ballot(b2 >= t)) + __popcll(__ballot(b3 >= t));
-            if (n >= a.k) bound = t;
-        }
-    }
+    const unsigned maxima[4] = {best[lane], best[lane + 64], best[lane + 128], best[lane + 192]};
+    const unsigned bound = kth_of(maxima, a.k);
     const float least = bound ? value_of(bound) : -FLT_MAX;
+    auto collect = [&](float x, int index) __attribute__((always_inline)) {
+        if (x >= least) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kCandidates) cand[at] = key_of(x, index);
+        }
+    };
+    collect(x_edge, edge);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         if (!__ballot(most[j] >= least)) continue;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float x = Piece<T>::at(v[j], i);
-            if (x >= least) {
-                const int at = atomicAdd(&count, 1);
-                if (at < kCandidates) cand[at] = key_of(x, first + j * kLanes * N + i);
-            }
-        }
+        for (int i = 0; i < N; ++i) collect(Piece<T>::at(v[j], i), row.head + (from + j * kLanes) * N + i);
     }
     __syncthreads();
     const int n = count;
@@ -234,14 +265,16 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     Key last = ~(Key)0;
     for (int i = 0; i < a.k; ++i) {
         Key mine = 0;
+        auto better = [&](float x, int index) __attribute__((always_inline)) {
+            const Key key = x >= least ? key_of(x, index) : 0;
+            if (key < last && key > mine) mine = key;
+        };
+        better(x_edge, edge);
+#pragma unroll 1
+        for (int j = 0; j < NV; ++j) {                               // (read again: rare, and registers are short)
+            const u4 again = load_piece<T>(row, from + j * kLanes, end);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-    #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float x = Piece<T>::at(v[j], e);
-                const Key key = x >= least ? key_of(x, first + j * kLanes * N + e) : 0;
-                if (key < last && key > mine) mine = key;
-            }
+            for (int e = 0; e < N; ++e) better(Piece<T>::at(again, e), row.head + (from + j * kLanes) * N + e);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
@@ -321,12 +354,15 @@ struct ScorePlan { int form, chunks, pieces; size_t stats_bytes, workspace; };
 ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
 {
     const int n = 16 / element_size;
-    const int pieces = (int)(((int64_t)vocab + n - 1 + n - 1) / n);  // of a row that starts anywhere between two boundaries
+    const int pieces = vocab < n ? 1 : vocab / n;                    // full ones of a row, at most
     ScorePlan p;
-    p.form = 8;
+    p.form = 16;
     auto chunks = [&](int form) { return (pieces + form * kLanes - 1) / (form * kLanes); };
-    while (p.form > 1 && (int64_t)rows * chunks(p.form) < kFillWorkgroups && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
+    // The more a workgroup holds, the fewer lists there are to join: 1024 rows of 128003 in fp32, 20 alternatives, 111 us with 8 pieces a
+    // lane, 95 with 16, which take two rounds of workgroups; 1024 of 50265 in bf16 29 / 25.
+    while (p.form > 1 && (int64_t)rows * chunks(p.form) < (p.form > 8 ? 2 * kFillWorkgroups : kFillWorkgroups) && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
     p.chunks = chunks(p.form);
+    while (p.form > 1 && chunks(p.form / 2) == p.chunks) p.form /= 2;
     p.pieces = (pieces + p.chunks - 1) / p.chunks;                   // chunks of one size
     p.stats_bytes = p.workspace = 0;
     if (p.chunks > 1) {
@@ -340,7 +376,8 @@ template <typename T>
 void launch_score(const ScoreArgs &a, const ScorePlan &p, int rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(rows * p.chunks)), block(kLanes);
-    if (p.form == 8) hipLaunchKernelGGL((k_score_chunk<T, 8>), grid, block, 0, s, a);
+    if (p.form == 16) hipLaunchKernelGGL((k_score_chunk<T, 16>), grid, block, 0, s, a);
+    else if (p.form == 8) hipLaunchKernelGGL((k_score_chunk<T, 8>), grid, block, 0, s, a);
     else if (p.form == 4) hipLaunchKernelGGL((k_score_chunk<T, 4>), grid, block, 0, s, a);
     else if (p.form == 2) hipLaunchKernelGGL((k_score_chunk<T, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_score_chunk<T, 1>), grid, block, 0, s, a);
