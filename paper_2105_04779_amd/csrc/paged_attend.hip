@@ -26,6 +26,7 @@ namespace el {
 namespace {
 
 constexpr int kCrossing = 1;
+constexpr int64_t kManyPieces = 16;  // of a sequence, from which the join takes four wavefronts a row
 constexpr int kComputeUnits = 256;
 // Tiles of a wavefront up to which a workgroup of several takes a whole sequence, without a second launch.  us on the device, cut and joined /
 // whole: bf16, 16 heads of 64, 1 sequence of 613 9.9 / 9.5, 8 of 300 to 400 10.9 / 8.5, 16 of 400 to 800 17.0 / 13.3; 8 key heads of 128, 32 of
@@ -174,7 +175,8 @@ template <int DT_, int DP_, int RG_> struct Form {
     // 1024 to 4096 positions (8 key heads of 128) take 154 and 200 us for 136, 512 of up to 256 (16 of 64) 65 and 80 for 54.
     static constexpr int NS = 2;
     static constexpr int RING = NS * 2 * TILEB, LDS = RING + NS * 256;             // of a wavefront: tiles, page numbers
-    static constexpr int PER_CU = 163840 / LDS < (RG == 2 ? 8 : 12) ? 163840 / LDS : RG == 2 ? 8 : 12;   // wavefronts that a compute unit holds
+    static constexpr int ROOM = 163840 / LDS, MOST = RG == 2 ? 8 : 12;             // by LDS; by registers
+    static constexpr int PER_CU = ROOM < MOST ? ROOM : MOST;                       // wavefronts that a compute unit holds
     static constexpr int WAVES = PER_CU >= 8 ? 8 : PER_CU >= 4 ? 4 : 2;            // of a workgroup, at most
 };
 
@@ -539,66 +541,89 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
     }
 }
 
-// Joins the pieces of a sequence that was cut: one (sequence, query row, head) a workgroup.  Bound by latency: the statistics of all
-// pieces in one round trip, the weighted sums in another.
+// Joins the pieces of a sequence that was cut: PER wavefronts a (sequence, query row, head), 4 / PER of those a workgroup.  Bound by
+// latency, so the first weighted sums are requested together with the statistics.
+template <int PER>
 __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int tile, float shift)
 {
-    extern __shared__ float weight[];                                // [pieces]
-    __shared__ float red[4];
-    __shared__ f4 sums[256];
-    const int tid = threadIdx.x, b = blockIdx.x / (a.beam * a.heads), x = blockIdx.x - b * (a.beam * a.heads);
+    __shared__ float red[PER == 1 ? 1 : 8];
+    __shared__ f4 sums[PER == 1 ? 1 : 256];
+    constexpr int LANES = 64 * PER, AHEAD = 4;
+    const int tid = threadIdx.x % LANES, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x * (4 / PER) + (PER == 1 ? w : 0);
+    if (row >= (int64_t)a.B * a.beam * a.heads) return;
+    const int b = (int)(row / (a.beam * a.heads)), x = (int)(row - (int64_t)b * (a.beam * a.heads));
     const int2 pc = a.pieces[b];                                     // (not written for a sequence without a tile)
     const int2 range = tile_range(a, length_of(a, b), tile);
     if (range.y == range.x) {
-        if (tid < a.d / 4) store4(a.out, (int64_t)blockIdx.x * a.d + 4 * tid, a.out_dtype, f4{0.f, 0.f, 0.f, 0.f});
-        if (tid == 0 && a.lse) a.lse[blockIdx.x] = -INFINITY;
+        if (tid < a.d / 4) store4(a.out, row * a.d + 4 * tid, a.out_dtype, f4{0.f, 0.f, 0.f, 0.f});
+        if (tid == 0 && a.lse) a.lse[row] = -INFINITY;
         return;
     }
     if (pc.y < 2) return;
     const int j = x / a.heads, head = x - j * a.heads, kvh = head / a.group, r = j * a.group + head % a.group;
     const int units = a.kv_heads * a.row_blocks, unit = r / a.rows * a.kv_heads + kvh, rb = r % a.rows;
-    auto slot = [&](int s) { return ((int64_t)(pc.x + s) * units + unit) * a.rows + rb; };
+    const int64_t first = ((int64_t)pc.x * units + unit) * a.rows + rb, step = (int64_t)units * a.rows;
+    const float2 *const ml = a.part_ml + first;
+    const int d4 = a.d / 4, groups = LANES / d4, grp = tid / d4, col = tid - grp * d4;
+    const float *const po = a.part_o + first * a.d + 4 * col;
+    const int begin = grp < groups ? grp : pc.y;
+    f4 ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        ahead[i] = f4{0.f, 0.f, 0.f, 0.f};
+        if (begin + i * groups < pc.y) ahead[i] = *(const f4 *)(po + (begin + i * groups) * step * a.d);
+    }
     float M = -INFINITY;
-    for (int s = tid; s < pc.y; s += 256) M = fmaxf(M, a.part_ml[slot(s)].x);
+    for (int s = tid; s < pc.y; s += LANES) M = fmaxf(M, ml[s * step].x);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-    if ((tid & 63) == 0) red[tid >> 6] = M;
-    __syncthreads();
-    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    if constexpr (PER > 1) {
+        if (lane == 0) red[w] = M;
+        __syncthreads();
+        M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    }
     const float ref = M == -INFINITY ? 0.f : M;
+    // (a piece without a position: sum 0.  A NaN score leaves its maximum at -inf and its sum at NaN, which stays)
+    auto weight = [&](float m) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - ref); };
     float L = 0.f;
-    for (int s = tid; s < pc.y; s += 256) {
-        const float2 v = a.part_ml[slot(s)];
-        // (a span without a position: sum 0.  A NaN score leaves its maximum at -inf and its sum at NaN, which stays)
-        const float f = v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(v.x - ref);
-        weight[s] = f;
-        L += f * v.y;
+    for (int s = tid; s < pc.y; s += LANES) {
+        const float2 v = ml[s * step];
+        L += weight(v.x) * v.y;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o, 64);
-    __syncthreads();
-    if ((tid & 63) == 0) red[tid >> 6] = L;
-    __syncthreads();
-    L = (red[0] + red[1]) + (red[2] + red[3]);
+    if constexpr (PER > 1) {
+        if (lane == 0) red[4 + w] = L;
+        __syncthreads();
+        L = (red[4] + red[5]) + (red[6] + red[7]);
+    }
     const bool empty = M == -INFINITY && !(L != L);
-    const int64_t row = (int64_t)blockIdx.x;
     if (tid == 0 && a.lse) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - shift) * kLn2;
-    const int d4 = a.d / 4, groups = 256 / d4, grp = tid / d4, col = tid - grp * d4;
     f4 o{0.f, 0.f, 0.f, 0.f};
-    if (grp < groups)
+    auto add = [&](const f4 &v, float f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += f * v[e];
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (begin + i * groups < pc.y) add(ahead[i], weight(ml[(begin + i * groups) * step].x));
 #pragma unroll 8
-        for (int s = grp; s < pc.y; s += groups) {
-            const f4 v = *(const f4 *)(a.part_o + slot(s) * a.d + 4 * col);
-            const float f = weight[s];
+    for (int s = begin + AHEAD * groups; s < pc.y; s += groups) add(*(const f4 *)(po + s * step * a.d), weight(ml[s * step].x));
+    if constexpr (PER > 1) {
+        sums[tid] = o;
+        __syncthreads();
+        if (tid < d4)
+            for (int k = 1; k < groups; ++k) add(sums[k * d4 + tid], 1.f);
+    } else {
+        for (int k = 1; k < groups; ++k) {
+            f4 v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += f * v[e];
+            for (int e = 0; e < 4; ++e) v[e] = __shfl(o[e], min(lane + k * d4, 63), 64);
+            if (lane < d4) add(v, 1.f);
         }
-    sums[tid] = o;
-    __syncthreads();
+    }
     if (tid < d4) {
-        for (int k = 1; k < groups; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += sums[k * d4 + tid][e];
         const float inv = 1.f / L;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = empty ? 0.f : o[e] * inv;
@@ -629,7 +654,9 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     AttendPlan p;
     const int R = beam * (heads / c.kv_heads);
     p.padded = c.d_head <= 64 ? 64 : c.d_head <= 128 ? 128 : 256;
-    // (two groups of rows share a tile's operand reads; in fp32 beyond 128 columns their registers do not suffice)
+    // Two groups of rows share a tile's operand reads; in fp32 beyond 128 columns their registers do not suffice.  (Four, for more than 32
+    // rows, gain nothing sure: 16 sequences of 1000 to 4096, 8 key heads of 128, 64 rows 75 us with two blocks of two / 70 with one of four,
+    // 16 key heads of 64 51 / 55.)
     p.row_groups = R <= 16 || (c.dtype == EL_F32 && p.padded == 256) ? 1 : 2;
     p.row_blocks = (R + 16 * p.row_groups - 1) / (16 * p.row_groups);
     p.rows = R < 16 * p.row_groups ? R : 16 * p.row_groups;
@@ -721,7 +748,11 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     launch_attend(a, p, cache->dtype, s);
     if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
     if (p.spans) {
-        hipLaunchKernelGGL(k_attend_join, dim3((unsigned)(rows * heads)), dim3(256), p.spans * sizeof(float), s, a, p.tile, cache->dtype == EL_F16 ? 12.f : 0.f);
+        // four wavefronts a row where sequences are cut into many pieces
+        const float shift = cache->dtype == EL_F16 ? 12.f : 0.f;
+        const int64_t all = rows * heads;
+        if (p.spans > kManyPieces * B) hipLaunchKernelGGL(k_attend_join<4>, dim3((unsigned)all), dim3(256), 0, s, a, p.tile, shift);
+        else hipLaunchKernelGGL(k_attend_join<1>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, p.tile, shift);
         if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
     }
     return EL_OK;

@@ -145,6 +145,27 @@ def test_many_sequences_of_very_different_lengths():
     c.check("1500 ragged")
 
 
+@pytest.mark.parametrize("dtype,d,heads,kv,x", [("bf16", 8, 2, 1, 1), ("f16", 40, 4, 4, 1), ("bf16", 80, 8, 2, 5), ("f32", 96, 3, 1, 1), ("f16", 248, 2, 2, 1),
+                                                ("f32", 256, 2, 1, 9), ("f32", 20, 2, 1, 17), ("bf16", 128, 20, 1, 2)])
+def test_cut_sequences_of_every_width(dtype, d, heads, kv, x):
+    """Few long sequences, whose many pieces are joined by four wavefronts a row, and many, by one, with spans that go on from one
+    sequence to the next, empty ones among them."""
+    c = Case(52, dtype, 2, x, heads, kv, d, 16, [5000, 2100])
+    c.check(f"cut, few {dtype} d {d}", segment=True, window=4000)
+    g = np.random.default_rng(d)
+    lengths = np.where(g.random(70) < 0.2, 0, g.integers(1, 2200, 70))
+    lengths[-1] = 2150
+    c = Case(53, dtype, 70, x, heads, kv, d, 16, lengths)
+    c.check(f"cut, many {dtype} d {d}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_short_sequences_taken_whole(dtype):
+    g = np.random.default_rng(8)
+    c = Case(54, dtype, 640, 1, 4, 4, 64, 16, g.integers(0, 200, 640))
+    c.check(f"640 whole {dtype}", segment=True)
+
+
 def test_lengths_outside_the_call_are_taken_as_the_nearer_end():
     c = Case(45, "bf16", 4, 1, 4, 4, 64, 16, [300, 7, 0, 160])
     c.lengths = np.array([400, -3, -2147483648, 2147483647], dtype=np.int32)
