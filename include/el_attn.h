@@ -494,7 +494,8 @@ el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_t *src, con
  * A logit of -inf is a token that may not follow: probability 0, never an alternative.  Where fewer than k tokens may
  * follow, the rest have log-probability -inf and index -1.  In a row where none may, the given token's log-probability is
  * -inf and the entropy 0.  A NaN or +inf in a row makes its log-probabilities and entropy NaN; NaN is never an alternative.
- * All sums are fp32 relative to the largest logit.  `workspace` as above, el_attn_score_workspace_bytes.
+ * All sums are fp32 relative to the largest logit.  The same call gives the same bits; rows that start at other places between
+ * 16-byte boundaries are summed in another order.  `workspace` as above, el_attn_score_workspace_bytes.
  * Errors: INVALID_ARG (null operands, sizes < 1, k, row_stride < vocab, alignment; rows beyond
  * 2^23), UNSUPPORTED (dtype, vocab), WORKSPACE, HIP.
  */

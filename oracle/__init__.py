@@ -339,7 +339,7 @@ def score_tokens_reference(logits, tokens, k):
         if tokens is not None:
             t = int(tokens[r])
             logprob[r] = 0.0 if t < 0 else np.nan if t >= vocab else x[t] - lse
-        best = sorted((v for v in range(vocab) if allowed[v]), key=lambda v: (-x[v], v))[:k]
-        for i, v in enumerate(best):
+        which = np.nonzero(allowed)[0]                               # ascending: a stable sort leaves equal ones in this order
+        for i, v in enumerate(which[np.argsort(-x[which], kind="stable")[:k]]):
             top_logprob[r, i], top_index[r, i] = x[v] - lse, v
     return logprob, entropy, top_logprob, top_index, away

@@ -19,6 +19,7 @@ constexpr int kMaxAlternatives = 64;
 constexpr int kLanes = 256;
 constexpr int kCandidates = 1024;        // of a chunk that are ranked by counting; with more (ties) one is taken at a time
 constexpr int kFillWorkgroups = 512;     // chunks get smaller until about so many workgroups share the logits: two a compute unit
+constexpr int kRowLanes = 1024, kRowsWhole = 256;
 constexpr int32_t kMaxVocab = 1 << 19;
 constexpr int kListMax = 65 * kMaxAlternatives;                      // entries of the lists that k_score_join holds in LDS: the largest vocabulary's in fp32
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -87,6 +88,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b)
     return Sums{m, fa * a.S + fb * b.S, fa * (a.W + da * a.S) + fb * (b.W + db * b.S)};
 }
 
+__device__ __forceinline__ float first_lane(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 __device__ __forceinline__ float lse_of(Sums s) { return s.S == 0.f ? 0.f : (s.m + __builtin_amdgcn_logf(s.S)) * kLn2; }
 
 // The given token's logit; where there is none, NaN (beyond the vocabulary) or +inf (no token given).
@@ -167,31 +169,31 @@ __device__ __forceinline__ unsigned kth_of(const unsigned (&mine)[COUNT], int k)
     return bound;
 }
 
-// A chunk of up to NV pieces a lane of one row.  Grid: rows x chunks.
-template <typename T, int NV>
-__global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
+// A chunk of up to NV pieces a lane of one row; LANES 1024: the whole row.  Grid: rows x chunks.
+template <typename T, int NV, int LANES>
+__global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
 {
-    constexpr int N = Piece<T>::N;
-    __shared__ unsigned best[kLanes];
+    constexpr int N = Piece<T>::N, WAVES = LANES / 64;
+    __shared__ unsigned best[256];
     __shared__ __attribute__((aligned(16))) Key cand[kCandidates + 8];
-    __shared__ Sums part[4];
+    __shared__ Sums part[WAVES];
     __shared__ int count;
-    __shared__ Key top[4];
+    __shared__ Key top[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t r = blockIdx.x / a.chunks;
     const int chunk = blockIdx.x - (int)r * a.chunks;
     const Row row = row_at<T>(a, r);
-    const int used = NV < 16 ? NV : (a.pieces + kLanes - 1) / kLanes;          // (uniform) pieces that some lane has
-    const int from = chunk * a.pieces + tid, end = min((chunk + 1) * a.pieces, row.full);           // this lane's pieces: kLanes apart
+    const int used = NV < 16 ? NV : (a.pieces + LANES - 1) / LANES;          // (uniform) pieces that some lane has
+    const int from = chunk * a.pieces + tid, end = min((chunk + 1) * a.pieces, row.full);           // this lane's pieces: LANES apart
     if (tid == 0) count = 0;
     if (a.k)
-        for (int i = tid; i < kCandidates + 8; i += kLanes) cand[i] = 0;
+        for (int i = tid; i < kCandidates + 8; i += LANES) cand[i] = 0;
 
     u4 v[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         v[j] = Piece<T>::none();
-        if (j < used) v[j] = load_piece<T>(row, from + j * kLanes, end);
+        if (j < used) v[j] = load_piece<T>(row, from + j * LANES, end);
     }
     const int edge = chunk == 0 ? edge_of<T>(row, tid, a.vocab) : -1;
     const float x_edge = edge >= 0 ? to_f32(((const T *)row.row)[edge]) : -INFINITY;
@@ -205,7 +207,13 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
         m = fmaxf(m, most[j]);
         asm volatile("" : "+v"(v[j]));                               // (one piece unpacked at a time)
     }
-    best[tid] = m > -INFINITY ? order32(m) : 0u;
+    if constexpr (LANES == 256) {
+        best[tid] = m > -INFINITY ? order32(m) : 0u;
+    } else {                                                         // (of four lanes each: 256 numbers again)
+        float m4 = fmaxf(m, quad_xor1(m));
+        m4 = fmaxf(m4, quad_xor2(m4));
+        if (tid % 4 == 0) best[tid / 4] = m4 > -INFINITY ? order32(m4) : 0u;
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     m *= kLog2e;
@@ -224,7 +232,11 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     if (lane == 0) part[w] = Sums{m, S, W};
     __syncthreads();
     const bool whole = a.chunks == 1;
-    const Sums s = join(join(part[0], part[1]), join(part[2], part[3]));
+    Sums s = part[lane % WAVES];
+#pragma unroll
+    for (int o = WAVES / 2; o > 0; o >>= 1) s = join(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)});
+    // (lanes join the same numbers in another order: lane 0's result for all, to the bit)
+    s = Sums{first_lane(s.m), first_lane(s.S), first_lane(s.W)};
     if (tid == 0) {
         if (whole) write_row(a, r, s, given);
         else a.stats[blockIdx.x] = f4{s.m, s.S, s.W, 0.f};
@@ -249,17 +261,17 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
     for (int j = 0; j < NV; ++j) {
         if (!__ballot(most[j] >= least)) continue;
 #pragma unroll
-        for (int i = 0; i < N; ++i) collect(Piece<T>::at(v[j], i), row.head + (from + j * kLanes) * N + i);
+        for (int i = 0; i < N; ++i) collect(Piece<T>::at(v[j], i), row.head + (from + j * LANES) * N + i);
     }
     __syncthreads();
     const int n = count;
     if (n <= kCandidates) {
-        for (int c = tid; c < n; c += kLanes) {
+        for (int c = tid; c < n; c += LANES) {
             const Key key = cand[c];
             const int rank = rank_in(cand, n, key);
             if (rank < a.k) emit(rank, key);
         }
-        for (int c = n + tid; c < a.k; c += kLanes) emit(c, 0);
+        for (int c = n + tid; c < a.k; c += LANES) emit(c, 0);
         return;
     }
     Key last = ~(Key)0;
@@ -272,9 +284,9 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
         better(x_edge, edge);
 #pragma unroll 1
         for (int j = 0; j < NV; ++j) {                               // (read again: rare, and registers are short)
-            const u4 again = load_piece<T>(row, from + j * kLanes, end);
+            const u4 again = load_piece<T>(row, from + j * LANES, end);
 #pragma unroll
-            for (int e = 0; e < N; ++e) better(Piece<T>::at(again, e), row.head + (from + j * kLanes) * N + e);
+            for (int e = 0; e < N; ++e) better(Piece<T>::at(again, e), row.head + (from + j * LANES) * N + e);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
@@ -284,8 +296,9 @@ __global__ void __launch_bounds__(kLanes) k_score_chunk(const ScoreArgs a)
         __syncthreads();
         if (lane == 0) top[w] = mine;
         __syncthreads();
-        const Key x = top[0] > top[1] ? top[0] : top[1], y = top[2] > top[3] ? top[2] : top[3];
-        last = x > y ? x : y;
+        last = 0;
+#pragma unroll 4
+        for (int j = 0; j < WAVES; ++j) last = top[j] > last ? top[j] : last;
         if (tid == 0) emit(i, last);
     }
 }
@@ -349,13 +362,14 @@ __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
 }
 
 // How a call is cut: pieces a lane, chunks of a row.
-struct ScorePlan { int form, chunks, pieces; size_t stats_bytes, workspace; };
+struct ScorePlan { int form, lanes, chunks, pieces; size_t stats_bytes, workspace; };
 
 ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
 {
     const int n = 16 / element_size;
     const int pieces = vocab < n ? 1 : vocab / n;                    // full ones of a row, at most
     ScorePlan p;
+    p.lanes = kLanes;
     p.form = 16;
     auto chunks = [&](int form) { return (pieces + form * kLanes - 1) / (form * kLanes); };
     // The more a workgroup holds, the fewer lists there are to join: 1024 rows of 128003 in fp32, 20 alternatives, 111 us with 8 pieces a
@@ -363,6 +377,10 @@ ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
     while (p.form > 1 && (int64_t)rows * chunks(p.form) < (p.form > 8 ? 2 * kFillWorkgroups : kFillWorkgroups) && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
     p.chunks = chunks(p.form);
     while (p.form > 1 && chunks(p.form / 2) == p.chunks) p.form /= 2;
+    if (p.chunks > 1 && rows <= kRowsWhole && pieces <= 16 * kRowLanes) {
+        p.lanes = kRowLanes; p.chunks = 1;
+        p.form = pieces <= 4 * kRowLanes ? 4 : pieces <= 8 * kRowLanes ? 8 : 16;
+    }
     p.pieces = (pieces + p.chunks - 1) / p.chunks;                   // chunks of one size
     p.stats_bytes = p.workspace = 0;
     if (p.chunks > 1) {
@@ -376,11 +394,15 @@ template <typename T>
 void launch_score(const ScoreArgs &a, const ScorePlan &p, int rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(rows * p.chunks)), block(kLanes);
-    if (p.form == 16) hipLaunchKernelGGL((k_score_chunk<T, 16>), grid, block, 0, s, a);
-    else if (p.form == 8) hipLaunchKernelGGL((k_score_chunk<T, 8>), grid, block, 0, s, a);
-    else if (p.form == 4) hipLaunchKernelGGL((k_score_chunk<T, 4>), grid, block, 0, s, a);
-    else if (p.form == 2) hipLaunchKernelGGL((k_score_chunk<T, 2>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_score_chunk<T, 1>), grid, block, 0, s, a);
+    if (p.lanes == kRowLanes) {
+        if (p.form == 16) hipLaunchKernelGGL((k_score_chunk<T, 16, kRowLanes>), grid, dim3(kRowLanes), 0, s, a);
+        else if (p.form == 8) hipLaunchKernelGGL((k_score_chunk<T, 8, kRowLanes>), grid, dim3(kRowLanes), 0, s, a);
+        else hipLaunchKernelGGL((k_score_chunk<T, 4, kRowLanes>), grid, dim3(kRowLanes), 0, s, a);
+    } else if (p.form == 16) hipLaunchKernelGGL((k_score_chunk<T, 16, kLanes>), grid, block, 0, s, a);
+    else if (p.form == 8) hipLaunchKernelGGL((k_score_chunk<T, 8, kLanes>), grid, block, 0, s, a);
+    else if (p.form == 4) hipLaunchKernelGGL((k_score_chunk<T, 4, kLanes>), grid, block, 0, s, a);
+    else if (p.form == 2) hipLaunchKernelGGL((k_score_chunk<T, 2, kLanes>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_score_chunk<T, 1, kLanes>), grid, block, 0, s, a);
     if (p.chunks > 1) hipLaunchKernelGGL((k_score_join<T>), dim3(rows), block, ((size_t)p.chunks * a.k + 8) * sizeof(Key), s, a);
 }
 

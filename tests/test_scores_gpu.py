@@ -71,6 +71,12 @@ def test_sizes(dtype, rows, V, k):
     _check(f"{dtype} {rows}x{V} k {k}", _logits(V, rows, V), dtype, k)
 
 
+@pytest.mark.parametrize("dtype,rows,V,k", [("bf16", 300, 33333, 8), ("f16", 600, 16001, 64), ("f32", 257, 20011, 20), ("bf16", 1100, 4097, 3), ("f32", 280, 70001, 5),
+                                            ("bf16", 256, 131072, 2), ("f32", 3, 524288, 64), ("bf16", 2, 524287, 64)])
+def test_many_rows_and_the_largest_vocabulary(dtype, rows, V, k):
+    _check(f"{dtype} {rows}x{V} k {k}", _logits(V + rows, rows, V), dtype, k)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("pad,offset", [(1, 0), (7, 3), (64, 1), (0, 5)])
 def test_rows_that_start_anywhere(dtype, pad, offset):
@@ -87,6 +93,22 @@ def test_ties_and_orders(dtype):
     x = np.stack(rows).astype(np.float32)
     for k in (1, 8, 64):
         _check(f"ties {dtype} k {k}", x, dtype, k)
+    # rows that are cut: ties within a chunk and across chunks
+    for k in (1, 64):
+        _check(f"ties, cut {dtype} k {k}", np.tile(x, (1, 7)), dtype, k)
+
+
+@pytest.mark.parametrize("dtype,rows,V", [("bf16", 4, 50265), ("f32", 300, 30011), ("bf16", 2, 250000)])
+def test_results_repeat_to_the_bit(dtype, rows, V):
+    """Which lane writes an alternative is a matter of chance; what it writes is not."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    x = to_device(wl.round_to_storage(_logits(13, rows, V), dtype), dtype)
+    t = torch.arange(rows, dtype=torch.int32, device="cuda")
+    once = el_attn.score_tokens(x, t, k=20)
+    for _ in range(20):
+        for a, b in zip(once, el_attn.score_tokens(x, t, k=20)):
+            assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
