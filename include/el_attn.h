@@ -432,8 +432,8 @@ typedef struct {
  * Accumulations and softmax statistics are fp32.  The result does not depend on what else runs, and is the same on
  * every call.  `workspace`: el_attn_paged_workspace_bytes of device memory, 16-byte aligned, used by this call only, any
  * contents; NULL where that is 0.
- * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, heads no multiple of kv_heads, strides, a rule with a
- * negative or non-finite number, n beyond the table, B * beam * heads beyond 2^23), UNSUPPORTED (dtypes, d_head), WORKSPACE, HIP.
+ * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, heads no multiple of kv_heads, strides, a rule with a cap or window
+ * below 0, a cap, scale or scale / cap that is not finite, n beyond the table, B * beam * heads beyond 2^23), UNSUPPORTED (dtypes, d_head), WORKSPACE, HIP.
  */
 size_t el_attn_paged_workspace_bytes(const el_attn_pages *cache, int32_t heads, int32_t B, int32_t beam, int32_t n);
 el_status el_attn_paged_attend(const el_attn_pages *cache,

@@ -25,16 +25,20 @@
 namespace el {
 namespace {
 
-constexpr int kCrossing = 1;
-constexpr int64_t kManyPieces = 16;  // of a sequence, from which the join takes four wavefronts a row
 constexpr int kComputeUnits = 256;
+constexpr int kCrossing = 1;         // tiles that a span may be longer if it then starts with a sequence anew (find_span)
+// Pieces of a sequence on average from which the join takes four wavefronts a row instead of one: one sequence of 16384 positions, one key head
+// 20.7 us with four, 25.0 with one; 16 of 1000 to 4096, 32 rows on 8 key heads 50.8 / 47.0.
+constexpr int64_t kManyPieces = 16;
 // Tiles of a wavefront up to which a workgroup of several takes a whole sequence, without a second launch.  us on the device, cut and joined /
 // whole: bf16, 16 heads of 64, 1 sequence of 613 9.9 / 9.5, 8 of 300 to 400 10.9 / 8.5, 16 of 400 to 800 17.0 / 13.3; 8 key heads of 128, 32 of
 // 200 to 500 19.8 / 15.7, 1 of 500 (four tiles each) 11.0 / 12.6; fp32, 4 of 300 to 500 10.7 / 13.2.  Outside a graph the second launch and its
 // scratch memory cost the host 5 us more than what the last two lose.  With eight tiles they lose 3 to 6 us.
 constexpr int kFew = 4;
-constexpr int kShort = 2048;         // positions that one wavefront may be left with where sequences alone fill the device
-constexpr int kCutMax = 1024;        // most sequences that are cut; beyond them the sequences alone fill the device twice
+// Positions that one wavefront may be left with where the sequences alone fill the device, so that nothing is joined: 300 sequences of 100 to 512
+// (16 heads of 64) 87 us whole, 98 cut; 200 of 200 to 1024 120 / 123.
+constexpr int kShort = 2048;
+constexpr int kCutMax = 1024;        // sequences whose lengths every wavefront adds up; of more, each is one wavefront's whatever its length
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArgs {
@@ -95,8 +99,8 @@ __device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int til
     s.T = max(1, (int)(((int64_t)total + a.spans - 1) / a.spans));
     s.aligned = false;
     if (a.B <= 64) {
-        // a span that goes on to another sequence costs about kCrossing tiles more (the way through length, pages and first tile): where
-        // spans no longer than that suffice that start with a sequence anew, they are taken
+        // A span that goes on to another sequence goes the way through length, pages and first tile once more: where spans hardly longer
+        // suffice that start with a sequence anew, they are taken (24 sequences with a window of 1024, d 256, 43 us; 51 with crossings).
         for (int T = s.T; T <= s.T + kCrossing && !s.aligned; ++T) {
             const int spans = sum_lanes((tiles + T - 1) / T);
             if (spans <= a.spans) { s.aligned = true; s.T = T; tiles = (tiles + T - 1) / T * T; total = spans * T; }
@@ -220,6 +224,22 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
     asm volatile("" : "+v"(lane));          // (what follows from it is worked out anew for a piece, instead of being held over all of them)
     const int r16 = lane & 15, g = lane >> 4;
     const int64_t b = st.b;
+    // query rows: row r of the key head is beam r / group, head kvh * group + r % group
+    u4 q[RG][QC];
+    float slope[RG];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        const int r = row0 + 16 * rg + r16;
+        const bool here = 16 * rg + r16 < a.rows && r < a.R;
+        const int head = kvh * a.group + r % a.group;
+        const char *p = a.queries + (b * a.beam + r / a.group) * a.query_stride + (int64_t)head * a.d * ES;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+            q[rg][c] = u4{0, 0, 0, 0};
+            if (here && (4 * c + g) * 16 < a.d * ES) q[rg][c] = *(const u4 *)(p + (4 * c + g) * 16);
+        }
+        slope[rg] = here && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    }
     const int len = length_of(a, st.b), first = a.window ? max(0, len - a.window) : 0;
     const int2 range = tile_range(a, len, TP);
     const int tiles = range.y - range.x;
@@ -286,22 +306,6 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
     if (nt > 0) {
 #pragma unroll
         for (int i = 0; i < NS - 1; ++i) request_pages(i);
-    }
-    // query rows: row r of the key head is beam r / group, head kvh * group + r % group
-    u4 q[RG][QC];
-    float slope[RG];
-#pragma unroll
-    for (int rg = 0; rg < RG; ++rg) {
-        const int r = row0 + 16 * rg + r16;
-        const bool here = 16 * rg + r16 < a.rows && r < a.R;
-        const int head = kvh * a.group + r % a.group;
-        const char *p = a.queries + (b * a.beam + r / a.group) * a.query_stride + (int64_t)head * a.d * ES;
-#pragma unroll
-        for (int c = 0; c < QC; ++c) {
-            q[rg][c] = u4{0, 0, 0, 0};
-            if (here && (4 * c + g) * 16 < a.d * ES) q[rg][c] = *(const u4 *)(p + (4 * c + g) * 16);
-        }
-        slope[rg] = here && a.slopes ? a.slopes[head] * kLog2e : 0.f;
     }
     // (in registers before the first tile is requested: a wait of the compiler's for them would wait for all that is under way)
 #pragma unroll
@@ -723,7 +727,8 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     if (!queries || !rule || !out || !valid_sizes(cache, heads, B, beam, n)) return EL_ERR_INVALID_ARG;
     if (out_dtype != EL_F32 && out_dtype != cache->dtype) return EL_ERR_UNSUPPORTED;
     if (n > (int64_t)table_pages * cache->page_size) return EL_ERR_INVALID_ARG;
-    if (!(fabsf(rule->scale) < INFINITY) || !finite_non_negative(rule->softcap) || rule->window < 0) return EL_ERR_INVALID_ARG;
+    if (!finite_non_negative(rule->softcap) || rule->window < 0) return EL_ERR_INVALID_ARG;
+    if (!(fabsf(rule->softcap > 0.f ? rule->scale / rule->softcap : rule->scale * kLog2e) < INFINITY)) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)dtype_size(cache->dtype), row = (int64_t)heads * cache->d_head, rows = (int64_t)B * beam;
     if (((uintptr_t)lengths | (uintptr_t)lse | (uintptr_t)rule->slopes) & 3 || ((uintptr_t)queries | (uintptr_t)out) & 15) return EL_ERR_INVALID_ARG;
     if (query_stride > ((int64_t)1 << 44) || query_stride * es % 16 != 0 || (rows > 1 && query_stride < row)) return EL_ERR_INVALID_ARG;

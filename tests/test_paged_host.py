@@ -71,7 +71,7 @@ def test_attend_refuses_bad_operands(ea):
     for out_dtype in (ea.EL_F16, 9):
         assert call(c, out_dtype=out_dtype) == U
     inf, nan = float("inf"), float("nan")
-    for rule in ((inf, 0, 0, None), (nan, 0, 0, None), (0.1, -1.0, 0, None), (0.1, inf, 0, None), (0.1, nan, 0, None), (0.1, 0, -1, None),
+    for rule in ((inf, 0, 0, None), (nan, 0, 0, None), (0.1, -1.0, 0, None), (0.1, inf, 0, None), (0.1, nan, 0, None), (0.1, 0, -1, None), (1.0, 1e-44, 0, None), (3e38, 0, 0, None),
                  (0.1, 0, 0, ctypes.c_void_p(0x100002))):
         assert call(c, rule=ea.ElAttnScoreRule(*rule)) == I, rule
     need = ea.el_attn_paged_workspace_bytes(c, 32, 4, 1, 160)
