@@ -325,21 +325,20 @@ def score_tokens_reference(logits, tokens, k):
         x = logits[r].astype(np.float64)
         allowed = x > -np.inf                                        # (False for NaN)
         broken = bool(np.isnan(x).any() or (x == np.inf).any())
+        m = log_S = 0.0
         if broken:
-            lse = entropy[r] = np.nan
+            log_S = entropy[r] = np.nan
         elif allowed.any():
             m = x.max()
-            e = np.exp(x[allowed] - m)
-            lse = m + np.log(e.sum())
-            p = e / e.sum()
-            entropy[r] = lse - (p * x[allowed]).sum()
-            away[r] = (p * (m - x[allowed])).sum()
-        else:
-            lse = 0.0
+            d = x[allowed] - m                                       # (of any size: the sums are relative to the largest)
+            log_S = np.log(np.exp(d).sum())
+            p = np.exp(d - log_S)
+            entropy[r] = log_S - (p * d).sum()
+            away[r] = -(p * d).sum()
         if tokens is not None:
             t = int(tokens[r])
-            logprob[r] = 0.0 if t < 0 else np.nan if t >= vocab else x[t] - lse
+            logprob[r] = 0.0 if t < 0 else np.nan if t >= vocab else (x[t] - m) - log_S
         which = np.nonzero(allowed)[0]                               # ascending: a stable sort leaves equal ones in this order
         for i, v in enumerate(which[np.argsort(-x[which], kind="stable")[:k]]):
-            top_logprob[r, i], top_index[r, i] = x[v] - lse, v
+            top_logprob[r, i], top_index[r, i] = (x[v] - m) - log_S, v
     return logprob, entropy, top_logprob, top_index, away

@@ -1,8 +1,9 @@
 // What a row of logits says about the next token: log-probability of a given one, entropy, the best alternatives.
 //
-//   lse = (m + log2 S) ln 2,  S = sum 2^y,  entropy = (log2 S - W / S) ln 2,  W = sum 2^y y,  y = x log2(e) - m
+//   log p(x) = (x - m) - log S,  S = sum exp(x - m),  entropy = log S - W / S,  W = sum exp(x - m) (x - m)
 //
-// with m the largest logit times log2(e), rounded: whatever it is, it is what y is relative to.
+// with m the largest logit: the differences are exact to a rounding whatever m is, a row of the type's lowest value included.
+//
 // Bound by HBM where rows are many: every logit is read once.  A workgroup holds a chunk of a row in registers, so maximum, sums
 // and alternatives are passes over registers.  Rows start anywhere (an odd vocabulary): chunks are cut at 16-byte boundaries of
 // memory, and the elements at a row's ends that do not fill 16 bytes are a lane's each.
@@ -82,14 +83,14 @@ struct Sums { float m, S, W; };
 __device__ __forceinline__ Sums join(Sums a, Sums b)
 {
     const float m = fmaxf(a.m, b.m);
-    // (nothing above -inf on a side: its sums are 0, or NaN, and stay)
-    const float da = a.m == -INFINITY ? 0.f : a.m - m, db = b.m == -INFINITY ? 0.f : b.m - m;
-    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+    // (nothing above -inf on a side: its sums are 0, or NaN, and stay; a difference beyond the type's range is one whose power is 0)
+    const float da = a.m == -INFINITY ? 0.f : fmaxf(a.m - m, -1e30f), db = b.m == -INFINITY ? 0.f : fmaxf(b.m - m, -1e30f);
+    const float fa = __builtin_amdgcn_exp2f(da * kLog2e), fb = __builtin_amdgcn_exp2f(db * kLog2e);
     return Sums{m, fa * a.S + fb * b.S, fa * (a.W + da * a.S) + fb * (b.W + db * b.S)};
 }
 
 __device__ __forceinline__ float first_lane(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
-__device__ __forceinline__ float lse_of(Sums s) { return s.S == 0.f ? 0.f : (s.m + __builtin_amdgcn_logf(s.S)) * kLn2; }
+__device__ __forceinline__ float log_of(float S) { return __builtin_amdgcn_logf(S) * kLn2; }
 
 // The given token's logit; where there is none, NaN (beyond the vocabulary) or +inf (no token given).
 template <typename T>
@@ -104,13 +105,13 @@ __device__ __forceinline__ float given_logit(const ScoreArgs &a, int64_t r)
 // logprob and entropy of a row, by one lane.
 __device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t r, Sums s, float given)
 {
-    const bool none = s.S == 0.f;                                    // no token may follow
-    if (a.entropy) a.entropy[r] = none ? 0.f : (__builtin_amdgcn_logf(s.S) - s.W / s.S) * kLn2;
-    if (a.logprob) a.logprob[r] = given == INFINITY ? 0.f : given - lse_of(s);
+    const bool none = s.S == 0.f;                                    // no token may follow: `given` is -inf, or NaN
+    if (a.entropy) a.entropy[r] = none ? 0.f : log_of(s.S) - s.W / s.S;
+    if (a.logprob) a.logprob[r] = given == INFINITY ? 0.f : none ? given : (given - s.m) - log_of(s.S);
 }
-__device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r, int i, Key key, float lse)
+__device__ __forceinline__ void write_alternative(const ScoreArgs &a, int64_t r, int i, Key key, float m, float log_S)
 {
-    a.top_logprob[r * a.k + i] = key ? value_of((unsigned)(key >> 32)) - lse : -INFINITY;
+    a.top_logprob[r * a.k + i] = key ? (value_of((unsigned)(key >> 32)) - m) - log_S : -INFINITY;
     a.top_index[r * a.k + i] = key ? (int)(0xffffffffu - (unsigned)key) : -1;
 }
 
@@ -148,9 +149,9 @@ __device__ __forceinline__ float largest(u4 v)
 }
 __device__ __forceinline__ void add_term(float x, float ref, float &S, float &W)
 {
-    const float y = fmaf(x, kLog2e, -ref), e = __builtin_amdgcn_exp2f(y);
+    const float d = x - ref, e = __builtin_amdgcn_exp2f(d * kLog2e);
     S += e;
-    W = fmaf(e, fmaxf(y, -1e4f), W);                                 // (a banned token: 0, not 0 * inf)
+    W = fmaf(e, fmaxf(d, -1e4f), W);                                 // (a banned token: 0, not 0 * inf)
 }
 
 // The k-th largest of the numbers of `COUNT` x 64 lanes, by its upper 16 bits (0: fewer than k are above 0).
@@ -216,7 +217,6 @@ __global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    m *= kLog2e;
     const float ref = m == -INFINITY ? 0.f : m;
     float S = 0.f, W = 0.f;
     add_term(x_edge, ref, S, W);
@@ -242,9 +242,9 @@ __global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
         else a.stats[blockIdx.x] = f4{s.m, s.S, s.W, 0.f};
     }
     if (a.k == 0) return;
-    const float lse = lse_of(s);
+    const float log_S = log_of(s.S);
     auto emit = [&](int i, Key key) __attribute__((always_inline)) {
-        if (whole) write_alternative(a, r, i, key, lse);
+        if (whole) write_alternative(a, r, i, key, s.m, log_S);
         else a.keys[(int64_t)blockIdx.x * a.k + i] = key;
     };
     const unsigned maxima[4] = {best[lane], best[lane + 64], best[lane + 128], best[lane + 192]};
@@ -352,13 +352,13 @@ __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
     }
     __syncthreads();
     const int n = count;
-    const float lse = lse_of(s);
+    const float log_S = log_of(s.S);
     for (int c = tid; c < n; c += kLanes) {
         const Key k = list[c];
         const int rank = rank_in(list, n, k);
-        if (rank < a.k) write_alternative(a, r, rank, k, lse);
+        if (rank < a.k) write_alternative(a, r, rank, k, s.m, log_S);
     }
-    for (int i = n + tid; i < a.k; i += kLanes) write_alternative(a, r, i, 0, lse);
+    for (int i = n + tid; i < a.k; i += kLanes) write_alternative(a, r, i, 0, s.m, log_S);
 }
 
 // How a call is cut: pieces a lane, chunks of a row.

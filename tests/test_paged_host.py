@@ -197,6 +197,8 @@ def test_scores_reference_is_torchs():
     assert np.allclose(top[0], torch.sort(logp[0], descending=True)[0][:7].numpy())
     uniform = oracle.score_tokens_reference(np.full((1, 64), 2.5), None, 3)
     assert np.isclose(uniform[1][0], np.log(64)) and list(uniform[3][0]) == [0, 1, 2]
+    lowest = oracle.score_tokens_reference(np.full((2, 64), [[-3.4e38], [3.4e38]]), [5, 9], 2)      # whatever size the logits have
+    assert np.allclose(lowest[0], -np.log(64)) and np.allclose(lowest[1], np.log(64)) and np.allclose(lowest[2], -np.log(64))
     none = oracle.score_tokens_reference(np.full((1, 8), -np.inf), [3], 2)
     assert none[0][0] == -np.inf and none[1][0] == 0 and list(none[3][0]) == [-1, -1]
     assert np.isnan(oracle.score_tokens_reference(np.array([[1.0, np.nan, 3.0]]), [0], 2)[1][0])
