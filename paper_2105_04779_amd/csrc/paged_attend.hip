@@ -670,7 +670,9 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     const int64_t units = (int64_t)c.kv_heads * p.row_blocks;
     int slots = 0, most = 1, lds = 0;
     with_form(c.dtype, p.padded, p.row_groups, [&](auto f) { p.tile = f.TP; slots = kComputeUnits * f.PER_CU; most = f.WAVES; lds = f.LDS; });
-    const int64_t tiles = ((int64_t)n + p.tile - 1) / p.tile, all = B * tiles, target = units < slots ? slots / units : 1;
+    const int64_t tiles = ((int64_t)n + p.tile - 1) / p.tile, all = B * tiles;
+    // spans: one round of wavefronts; where the units are so many that one round would leave much of the device idle, four
+    const int64_t target = units <= slots / 8 ? slots / units : (4 * (int64_t)slots + units - 1) / units;
     p.waves = 1;
     while (p.waves < most && 2 * p.waves * B * units <= slots && 2 * p.waves <= tiles) p.waves *= 2;
     // whole sequences: where they alone fill the device and none is long, where the lengths would take long to add up, and where a few

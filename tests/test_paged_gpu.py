@@ -166,6 +166,12 @@ def test_many_short_sequences_taken_whole(dtype):
     c.check(f"640 whole {dtype}", segment=True)
 
 
+@pytest.mark.parametrize("dtype,kv", [("bf16", 700), ("f32", 1500)])
+def test_key_heads_that_do_not_divide_the_device_evenly(dtype, kv):
+    c = Case(55, dtype, 2, 1, kv, kv, 16, 16, [700, 333])
+    c.check(f"{kv} key heads {dtype}", segment=True)
+
+
 def test_lengths_outside_the_call_are_taken_as_the_nearer_end():
     c = Case(45, "bf16", 4, 1, 4, 4, 64, 16, [300, 7, 0, 160])
     c.lengths = np.array([400, -3, -2147483648, 2147483647], dtype=np.int32)
