@@ -421,18 +421,19 @@ typedef struct {
  *   lengths  [B] int32 device, each in [0, n] (a value outside is taken as the nearer end), or NULL: n
  *   queries  rows b * beam + j, query_stride ELEMENTS apart, of `heads` heads of d_head each; device, `dtype`.  The `beam`
  *            queries of a sequence read the same positions.  Query head i reads key head i / (heads / kv_heads)
- *   out      [B * beam, heads * d_head] contiguous; `out_dtype`: EL_F32 or `dtype`
+ *   out      [B * beam, heads * d_head] contiguous; `out_dtype`: EL_F32 or `dtype`; not in the memory from the first query to the last
  *   lse      [B * beam, heads] float32 or NULL: log sum_t exp(s_t), natural units
  *   n        the largest length: at most table_pages * page_size
  *
  * With out_dtype EL_F32, (out, lse) is a segment as el_attn_decode_segment returns it, and el_attn_merge_segments joins
  * it with segments over hidden states.  A row with no position (length 0, all pages absent, every score -inf) has output 0
- * and lse -inf.  Storage behind a length or outside a window is never read into a result, whatever it holds.
+ * and lse -inf.  Storage behind a length or outside a window is never read into a result, whatever it holds.  A NaN score
+ * makes its row NaN, an infinite or NaN value of a position that takes part its column (infinite or NaN).
  *
  * Accumulations and softmax statistics are fp32.  The result does not depend on what else runs, and is the same on
  * every call.  `workspace`: el_attn_paged_workspace_bytes of device memory, 16-byte aligned, used by this call only, any
  * contents; NULL where that is 0.
- * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, heads no multiple of kv_heads, strides, a rule with a cap or window
+ * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, heads no multiple of kv_heads, strides, an output among the queries, a rule with a cap or window
  * below 0, a cap, scale or scale / cap that is not finite, n beyond the table, B * beam * heads beyond 2^23), UNSUPPORTED (dtypes, d_head), WORKSPACE, HIP.
  */
 size_t el_attn_paged_workspace_bytes(const el_attn_pages *cache, int32_t heads, int32_t B, int32_t beam, int32_t n);

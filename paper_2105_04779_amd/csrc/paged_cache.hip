@@ -131,7 +131,7 @@ extern "C" el_status el_attn_paged_append(const el_attn_pages *cache,
     const int64_t es = (int64_t)el::dtype_size(cache->dtype), most = (int64_t)1 << 44, row = (int64_t)cache->kv_heads * cache->d_head;
     if (token_stride > most || batch_stride > most || token_stride * es % 16 != 0 || batch_stride * es % 16 != 0) return EL_ERR_INVALID_ARG;
     if ((T > 1 && token_stride < row) || (B > 1 && batch_stride < row)) return EL_ERR_INVALID_ARG;
-    if (row * es / 16 > INT32_MAX) return EL_ERR_INVALID_ARG;
+    if (row * es / 16 > INT32_MAX - 256) return EL_ERR_INVALID_ARG;
     const el::AppendArgs a{el::page_view(*cache, table, table_stride, table_pages), lengths, counts, (const char *)K_new, (const char *)V_new,
                            batch_stride * es, token_stride * es, cache->kv_heads, (int)(cache->d_head * es / 16), T};
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's

@@ -373,7 +373,7 @@ ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
     p.form = 16;
     auto chunks = [&](int form) { return (pieces + form * kLanes - 1) / (form * kLanes); };
     // The more a workgroup holds, the fewer lists there are to join: 1024 rows of 128003 in fp32, 20 alternatives, 111 us with 8 pieces a
-    // lane, 95 with 16, which take two rounds of workgroups; 1024 of 50265 in bf16 29 / 25.
+    // lane, 96 with 16, which take two rounds of workgroups; 1024 of 50265 in bf16 29 / 26.
     while (p.form > 1 && (int64_t)rows * chunks(p.form) < (p.form > 8 ? 2 * kFillWorkgroups : kFillWorkgroups) && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
     p.chunks = chunks(p.form);
     while (p.form > 1 && chunks(p.form / 2) == p.chunks) p.form /= 2;

@@ -82,6 +82,20 @@ def test_attend_refuses_bad_operands(ea):
     assert ea.el_attn_paged_workspace_bytes(_pages(ea, pages=0), 32, 4, 1, 160) == 0
 
 
+def test_attend_refuses_an_output_among_the_queries(ea):
+    call, c = _calls(ea)["attend"], _pages(ea)
+    row, at = 32 * 128 * 2, 0x40000000                               # bytes of a row of bf16 heads; four rows
+    none = dict(table_stride=200, table_pages=200, n=3200, workspace_bytes=0, workspace=None)      # (refused behind the check: nothing is launched)
+    assert ea.el_attn_paged_workspace_bytes(c, 32, 4, 1, 3200) > 0
+    for queries, out in ((at, at), (at, at + 4 * row - 16), (at + 4 * row - 16, at)):
+        assert call(c, queries=ctypes.c_void_p(queries), out=ctypes.c_void_p(out), **none) == ea.EL_ERR_INVALID_ARG
+    for queries, out in ((at, at + 4 * row), (at + 4 * row, at)):
+        assert call(c, queries=ctypes.c_void_p(queries), out=ctypes.c_void_p(out), **none) == ea.EL_ERR_WORKSPACE
+    # rows further apart, and an output of fp32
+    assert call(c, queries=ctypes.c_void_p(at), query_stride=row, out=ctypes.c_void_p(at + 5 * row), **none) == ea.EL_ERR_INVALID_ARG
+    assert call(c, queries=ctypes.c_void_p(at + 5 * row), out=ctypes.c_void_p(at), out_dtype=ea.EL_F32, **none) == ea.EL_ERR_INVALID_ARG
+
+
 def test_append_and_copy_refuse_bad_operands(ea):
     I, c = ea.EL_ERR_INVALID_ARG, _pages(ea)
     call = _calls(ea)["append"]
