@@ -25,7 +25,8 @@
 namespace el {
 namespace {
 
-constexpr int kComputeUnits = 256;
+constexpr int kComputeUnits = 256, kDies = 8;                        // (a level-2 cache each)
+constexpr int kLine = 128;           // bytes of a line of it
 constexpr int kCrossing = 1;         // tiles that a span may be longer if it then starts with a sequence anew (find_span)
 // Pieces of a sequence on average from which the join takes four wavefronts a row instead of one: one sequence of 16384 positions, one key head
 // 20.7 us with four, 25.0 with one; 16 of 1000 to 4096, 32 rows on 8 key heads 50.8 / 47.0.
@@ -50,6 +51,7 @@ struct AttendArgs {
     float scale, softcap;
     int window, n, B, beam, heads, kv_heads, d;
     int group, R, row_blocks, rows;          // heads / kv_heads; query rows of a key head; blocks of them; rows of a block, at most
+    bool near;                               // key heads that are neighbours in memory on one die
     int waves;                               // of a workgroup: a power of 2; more than one only where they share a whole sequence
     int spans;                               // spans that the tiles of all sequences are cut into, at most; 0: a span is a sequence
     void *out;
@@ -203,7 +205,13 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     char *const ring = shared + wave * F::RING;
     int *const Tb = (int *)(shared + a.waves * F::RING + wave * (NS * 256));
-    const int units = a.kv_heads * a.row_blocks, span = blockIdx.x / units, unit = blockIdx.x - span * units;
+    const int units = a.kv_heads * a.row_blocks;
+    int span = blockIdx.x / units, unit = blockIdx.x - span * units;
+    if (a.near && (span / kDies + 1) * kDies * units <= (int)gridDim.x) {            // workgroups go round the dies: a die takes a span's units
+        const int first = span / kDies * kDies, i = blockIdx.x - first * units;
+        span = first + i % kDies;
+        unit = i / kDies;
+    }
     const int kvh = unit % a.kv_heads, row0 = unit / a.kv_heads * a.rows;
     EL_LDS(char) *const lds = (EL_LDS(char) *)ring;
     const unsigned lds_at = (unsigned)(uintptr_t)lds, tb_at = (unsigned)(uintptr_t)(EL_LDS(int) *)Tb;
@@ -639,7 +647,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int til
 }
 
 // What a call is launched with: host arithmetic.
-struct AttendPlan { int padded, row_groups, row_blocks, rows, tile, waves, spans, grid, lds; size_t pieces_bytes, ml_bytes, workspace; };
+struct AttendPlan { int padded, row_groups, row_blocks, rows, tile, waves, spans, grid, lds; bool near; size_t pieces_bytes, ml_bytes, workspace; };
 
 template <class Fn>
 void with_form(int dtype, int padded, int row_groups, Fn fn)
@@ -682,6 +690,12 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     if (!few) p.waves = 1;
     p.spans = whole ? 0 : (int)(target < all ? target : all);
     p.grid = (int)((whole ? B : p.spans) * units);
+    // Heads that share lines are read by one die, or each of the two fetches them: 500 sequences of 500 to 700, 16 heads of 32, 159 us, 233 apart;
+    // 16 of 1000 to 3000, 5 rows on each of 20 heads of 40, 41 / 54; 100 of 100 to 2500, 16 heads of 80, 155 / 182.  So are heads of one line each where
+    // wavefronts take whole sequences: 500 of 512 to 1024, 16 heads of 64, 265 / 299.  In spans, with few heads and at longer rows apart is better by up to 5 %
+    // (150 of up to 2500 167, 174 near; 600 of 500 to 700, 4 heads, 81 / 83; 300 of 100 to 800, 8 heads of 128, 115 / 118).
+    const int64_t head_bytes = c.head_stride * (int64_t)dtype_size(c.dtype);
+    p.near = head_bytes % kLine != 0 || (head_bytes == kLine && whole && p.waves == 1 && units >= kDies);
     p.lds = p.waves * lds;
     p.pieces_bytes = p.ml_bytes = p.workspace = 0;
     if (p.spans) {
@@ -750,7 +764,7 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     a.slopes = rule->slopes; a.scale = rule->scale; a.softcap = rule->softcap; a.window = rule->window;
     a.n = n; a.B = B; a.beam = beam; a.heads = heads; a.kv_heads = cache->kv_heads; a.d = cache->d_head;
     a.group = heads / cache->kv_heads; a.R = beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
-    a.waves = p.waves; a.spans = p.spans;
+    a.near = p.near; a.waves = p.waves; a.spans = p.spans;
     a.out = out; a.out_dtype = out_dtype; a.lse = lse;
     if (p.workspace) {
         a.pieces = (int2 *)workspace;

@@ -172,6 +172,15 @@ def test_key_heads_that_do_not_divide_the_device_evenly(dtype, kv):
     c.check(f"{kv} key heads {dtype}", segment=True)
 
 
+@pytest.mark.parametrize("dtype,B,kv,d,x", [("bf16", 643, 8, 64, 1), ("f16", 8, 9, 64, 3), ("f16", 300, 9, 24, 1), ("bf16", 13, 5, 40, 7), ("f32", 259, 8, 20, 1), ("f32", 300, 8, 32, 1)])
+def test_heads_that_share_lines_of_memory(dtype, B, kv, d, x):
+    """Many heads and sequences in both layouts, numbers of them that divide nothing, a few rows each or enough for several blocks."""
+    g = np.random.default_rng(B)
+    for i, heads_first in enumerate((False, True)):
+        c = Case(56 + i, dtype, B, x, 3 * kv, kv, d, 16, g.integers(0, 180, B), heads_first=heads_first)
+        c.check(f"{B} x {kv} heads of {d} {dtype}", segment=True)
+
+
 def test_lengths_outside_the_call_are_taken_as_the_nearer_end():
     c = Case(45, "bf16", 4, 1, 4, 4, 64, 16, [300, 7, 0, 160])
     c.lengths = np.array([400, -3, -2147483648, 2147483647], dtype=np.int32)
