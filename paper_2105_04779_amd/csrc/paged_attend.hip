@@ -35,11 +35,16 @@ constexpr int64_t kManyPieces = 16;
 // whole: bf16, 16 heads of 64, 1 sequence of 613 9.9 / 9.5, 8 of 300 to 400 10.9 / 8.5, 16 of 400 to 800 17.0 / 13.3; 8 key heads of 128, 32 of
 // 200 to 500 19.8 / 15.7, 1 of 500 (four tiles each) 11.0 / 12.6; fp32, 4 of 300 to 500 10.7 / 13.2.  Outside a graph the second launch and its
 // scratch memory cost the host 5 us more than what the last two lose.  With eight tiles they lose 3 to 6 us.
-constexpr int kFew = 4;
+// Of more sequences than find_span can start spans with, those that go on to the next cost more: 1000 of up to 300, one key head of 64,
+// 30.2 / 14.6 (5 tiles each); 900 of up to 400, one of 128, 46.6 / 31.2 (13); 100 of up to 600 in fp32, two of 64, 21.9 / 16.8 (10); 70 of up to 2000, one
+// of 64, 15.5 / 16.5 (16); 300 of up to 1000, two of 128, 45 / 58 (32).
+constexpr int kFew = 4, kFewOfMany = 16;
 // Positions that one wavefront may be left with where the sequences alone fill the device, so that nothing is joined: 300 sequences of 100 to 512
 // (16 heads of 64) 87 us whole, 98 cut; 200 of 200 to 1024 120 / 123.
 constexpr int kShort = 2048;
-constexpr int kCutMax = 1024;        // sequences whose lengths every wavefront adds up; of more, each is one wavefront's whatever its length
+// Sequences are never cut where there are more than kCutMost, whose lengths every wavefront would have to add up, and of more than kCutMax only
+// longer ones: 8000 of up to 2500, one key head of 64, 447 us whole, 500 cut; 1500 of up to 8192, one of 128, 719 / 554.
+constexpr int kCutMax = 1024, kCutMost = 1 << 14;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArgs {
@@ -86,21 +91,22 @@ __device__ __forceinline__ int running_sum(int v)
 }
 __device__ __forceinline__ int sum_lanes(int v) { return __builtin_amdgcn_readlane(running_sum(v), 63); }
 
-// Every wavefront adds the lengths up by itself.  False: the list is shorter.
+// Every wavefront adds the lengths up by itself: a lane those of a block of sequences, then the lanes theirs, and the block in which the span
+// starts is looked through.  False: the list is shorter.
 __device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int tile, Start &s)
 {
-    const int lane = threadIdx.x;
-    int total = 0, tiles = 0;
-    for (int b = lane; b < a.B; b += 64) {
-        const int2 r = tile_range(a, length_of(a, b), tile);
-        tiles = r.y - r.x;
-        total += tiles;
-    }
-    if (a.B <= 64 && lane >= a.B) tiles = 0;
-    total = sum_lanes(total);
+    const int lane = threadIdx.x, each = (a.B + 63) / 64;            // sequences of a block
+    auto tiles_of = [&](int b, bool there) __attribute__((always_inline)) {          // (loaded in any case, so that many are on their way)
+        const int2 r = tile_range(a, length_of(a, min(b, a.B - 1)), tile);
+        return there ? r.y - r.x : 0;
+    };
+    int tiles = 0;
+#pragma unroll 8
+    for (int j = 0; j < each; ++j) tiles += tiles_of(lane * each + j, lane * each + j < a.B);
+    int total = sum_lanes(tiles);
     s.T = max(1, (int)(((int64_t)total + a.spans - 1) / a.spans));
     s.aligned = false;
-    if (a.B <= 64) {
+    if (each == 1) {
         // A span that goes on to another sequence goes the way through length, pages and first tile once more: where spans hardly longer
         // suffice that start with a sequence anew, they are taken (24 sequences with a window of 1024, d 256, 43 us; 51 with crossings).
         for (int T = s.T; T <= s.T + kCrossing && !s.aligned; ++T) {
@@ -111,21 +117,21 @@ __device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int til
     if ((int64_t)span * s.T >= total) return false;
     s.at = span * s.T;
     s.end = (int)min((int64_t)s.at + s.T, (int64_t)total);
-    int before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        if (a.B > 64) {
-            tiles = 0;
-            if (b0 + lane < a.B) { const int2 r = tile_range(a, length_of(a, b0 + lane), tile); tiles = r.y - r.x; }
-        }
+    s.before = 0;
+    auto find = [&](int tiles) __attribute__((always_inline)) {      // the lane whose tiles hold the start, or -1: it lies behind them
         const int incl = running_sum(tiles);
-        const unsigned long long past = __ballot(before + incl > s.at);
-        if (past) {
-            const int first = __ffsll((long long)past) - 1;
-            s.b = b0 + first;
-            s.before = before + __builtin_amdgcn_readlane(incl, first) - __builtin_amdgcn_readlane(tiles, first);
-            return true;
-        }
-        before += __builtin_amdgcn_readlane(incl, 63);
+        const unsigned long long past = __ballot(s.before + incl > s.at);
+        const int first = past ? __ffsll((long long)past) - 1 : 63;
+        s.before += __builtin_amdgcn_readlane(incl, first) - (past ? __builtin_amdgcn_readlane(tiles, first) : 0);
+        return past ? first : -1;
+    };
+    s.b = find(tiles);
+    if (each == 1) return true;
+    const int b0 = s.b * each;
+    for (int o = 0; o < each; o += 64) {
+        const int i = find(tiles_of(b0 + o + lane, o + lane < each && b0 + o + lane < a.B));
+        s.b = b0 + o + i;
+        if (i >= 0) return true;
     }
     return false;
 }
@@ -685,9 +691,9 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     while (p.waves < most && 2 * p.waves * B * units <= slots && 2 * p.waves <= tiles) p.waves *= 2;
     // whole sequences: where they alone fill the device and none is long, where the lengths would take long to add up, and where a few
     // tiles are all that a wavefront gets
-    const bool few = tiles <= (int64_t)kFew * p.waves;
-    const bool whole = few || B > kCutMax || all > 1 << 30 || (n <= kShort && B * units >= slots);
-    if (!few) p.waves = 1;
+    const bool few = tiles <= (int64_t)(B > 64 ? kFewOfMany : kFew) * p.waves;
+    const bool whole = few || B > kCutMost || all > 1 << 30 || (B > kCutMax ? n <= 2 * kShort : n <= kShort && B * units >= slots);
+    if (!whole) p.waves = 1;
     p.spans = whole ? 0 : (int)(target < all ? target : all);
     p.grid = (int)((whole ? B : p.spans) * units);
     // Heads that share lines are read by one die, or each of the two fetches them: 500 sequences of 500 to 700, 16 heads of 32, 159 us, 233 apart;

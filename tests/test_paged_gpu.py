@@ -157,6 +157,9 @@ def test_cut_sequences_of_every_width(dtype, d, heads, kv, x):
     lengths[-1] = 2150
     c = Case(53, dtype, 70, x, heads, kv, d, 16, lengths)
     c.check(f"cut, many {dtype} d {d}")
+    lengths[[7, 69]] = (4500, 4200)
+    c = Case(59, dtype, 70, x, heads, kv, d, 16, lengths)
+    c.check(f"cut, many, longer {dtype} d {d}", segment=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -170,6 +173,19 @@ def test_many_short_sequences_taken_whole(dtype):
 def test_key_heads_that_do_not_divide_the_device_evenly(dtype, kv):
     c = Case(55, dtype, 2, 1, kv, kv, 16, 16, [700, 333])
     c.check(f"{kv} key heads {dtype}", segment=True)
+
+
+@pytest.mark.parametrize("B,kv,d", [(1100, 2, 32), (4200, 1, 8), (16390, 1, 8)])
+def test_thousands_of_sequences_with_a_few_long_ones(B, kv, d):
+    """Cut by sums over blocks of lengths, of more than 64 each among them, and past the number that is cut."""
+    g = np.random.default_rng(B)
+    lengths = g.integers(0, 4, B)
+    lengths[[0, 63, 64, 700, B - 2]] = (4100, 5, 900, 4250, 1300)
+    lengths[B - 40:B - 2] = 0
+    lengths[B - 1] = 0
+    c = Case(58, "f16", B, 1, kv, kv, d, 64, lengths)
+    c.check(f"{B} sequences", segment=True)
+    c.check(f"{B} sequences, window", window=1500)
 
 
 @pytest.mark.parametrize("dtype,B,kv,d,x", [("bf16", 643, 8, 64, 1), ("f16", 8, 9, 64, 3), ("f16", 300, 9, 24, 1), ("bf16", 13, 5, 40, 7), ("f32", 259, 8, 20, 1), ("f32", 300, 8, 32, 1)])
