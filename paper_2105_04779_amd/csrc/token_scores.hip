@@ -22,7 +22,7 @@ constexpr int kCandidates = 1024;        // of a chunk that are ranked by counti
 constexpr int kFillWorkgroups = 512;     // chunks get smaller until about so many workgroups share the logits: two a compute unit
 constexpr int kRowLanes = 1024, kRowsWhole = 256;
 constexpr int32_t kMaxVocab = 1 << 19;
-constexpr int kListMax = 65 * kMaxAlternatives;                      // entries of the lists that k_score_join holds in LDS: the largest vocabulary's in fp32
+constexpr int kListMax = 2048;           // entries of a row's lists, which k_score_join holds in registers: 32 chunks of the largest vocabulary in fp32
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 typedef unsigned long long Key;
@@ -303,53 +303,51 @@ __global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
     }
 }
 
-// The chunks of a row joined: one row a workgroup.  Every chunk's list is descending, so what lies below the largest of their last
-// entries is none of the k best; the rest, some tens, is collected and ranked by counting.  Bound by latency: everything is requested at
-// once.
+// The chunks of a row joined: one row a workgroup.  The lists are descending; taken across, first entries first, they are numbers of 256 lanes
+// whose k-th largest maximum bounds the k best as in a chunk.  Bound by latency: everything is requested at once.
 template <typename T>
 __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) Key list[];       // [chunks * k + 8] what is left, and zeros
     __shared__ Sums part[4];
-    __shared__ Key last[4];
+    __shared__ unsigned best[kLanes];
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t r = blockIdx.x;
     const int total = a.chunks * a.k;
     const Key *const keys = a.keys + r * total;
-    Key key[4], least = 0;
+    auto key_at = [&](int t) __attribute__((always_inline)) {        // entry t / chunks of list t % chunks
+        const int i = t / a.chunks;
+        return t < total ? keys[(t - i * a.chunks) * a.k + i] : 0;
+    };
+    constexpr int HELD = kListMax / kLanes;
+    Key key[HELD], most = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) key[j] = tid + j * kLanes < total ? keys[tid + j * kLanes] : 0;
+    for (int j = 0; j < HELD; ++j) key[j] = key_at(tid + j * kLanes);
     const float given = tid == 0 ? given_logit<T>(a, r) : 0.f;
     Sums s{-INFINITY, 0.f, 0.f};
     for (int c = tid; c < a.chunks; c += kLanes) {
         const f4 v = a.stats[r * a.chunks + c];
         s = join(s, Sums{v[0], v[1], v[2]});
-        if (a.k) { const Key k = keys[(int64_t)c * a.k + a.k - 1]; least = k > least ? k : least; }
     }
     if (tid == 0) count = 0;
     for (int i = tid; i < total + 8; i += kLanes) list[i] = 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        s = join(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)});
-        const Key other = __shfl_xor(least, o, 64);
-        least = least > other ? least : other;
-    }
-    if (lane == 0) { part[w] = s; last[w] = least; }
+    for (int j = 0; j < HELD; ++j) most = key[j] > most ? key[j] : most;
+    best[tid] = (unsigned)(most >> 32);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s = join(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)});
+    if (lane == 0) part[w] = s;
     __syncthreads();
     s = join(join(part[0], part[1]), join(part[2], part[3]));
     if (tid == 0) write_row(a, r, s, given);
     if (a.k == 0) return;
+    const unsigned maxima[4] = {best[lane], best[lane + 64], best[lane + 128], best[lane + 192]};
+    // (0: no alternative.  64 entries are ranked sooner than bounded: 2000 rows of 50265 in bf16, 8 alternatives, 51.7 us, 53.2 bounded)
+    const Key least = total <= 64 ? (Key)1 : max((Key)kth_of(maxima, a.k) << 32, (Key)1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) least = least > last[i] ? least : last[i];
-    if (least == 0) least = 1;                                       // (0: no alternative)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < HELD; ++j)
         if (key[j] >= least) list[atomicAdd(&count, 1)] = key[j];
-    for (int i = tid + 4 * kLanes; i < total; i += kLanes) {
-        const Key k = keys[i];
-        if (k >= least) list[atomicAdd(&count, 1)] = k;
-    }
     __syncthreads();
     const int n = count;
     const float log_S = log_of(s.S);
@@ -362,6 +360,7 @@ __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
 }
 
 // How a call is cut: pieces a lane, chunks of a row.
+static_assert(kMaxVocab / 4 / (16 * kLanes) * kMaxAlternatives <= kListMax, "the fewest chunks of a row");
 struct ScorePlan { int form, lanes, chunks, pieces; size_t stats_bytes, workspace; };
 
 ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)

@@ -98,6 +98,23 @@ def test_ties_and_orders(dtype):
         _check(f"ties, cut {dtype} k {k}", np.tile(x, (1, 7)), dtype, k)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("k", [1, 8, 20, 64])
+def test_alternatives_of_rows_that_are_cut(dtype, k):
+    """All in one chunk, one in each, in none but a few places, nowhere."""
+    V = 300001
+    g = np.random.default_rng(k)
+    x = np.full((7, V), -np.inf, dtype=np.float32)
+    x[0] = np.linspace(-9, 9, V)
+    x[1] = x[0, ::-1]
+    x[2, g.permutation(V)[:3]] = (1.0, 5.0, -2.0)
+    x[3, ::5003] = g.standard_normal(len(x[3, ::5003]))
+    x[5] = g.standard_normal(V) * 4
+    x[5, 123456:123500] += 40
+    x[6, 170000:170060] = g.standard_normal(60)
+    _check(f"cut {dtype} k {k}", x, dtype, k)
+
+
 @pytest.mark.parametrize("dtype,rows,V", [("bf16", 4, 50265), ("f32", 300, 30011), ("bf16", 2, 250000)])
 def test_results_repeat_to_the_bit(dtype, rows, V):
     """Which lane writes an alternative is a matter of chance; what it writes is not."""
