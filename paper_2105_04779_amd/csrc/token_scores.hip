@@ -373,10 +373,15 @@ ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
     auto chunks = [&](int form) { return (pieces + form * kLanes - 1) / (form * kLanes); };
     // The more a workgroup holds, the fewer lists there are to join: 1024 rows of 128003 in fp32, 20 alternatives, 111 us with 8 pieces a
     // lane, 96 with 16, which take two rounds of workgroups; 1024 of 50265 in bf16 29 / 26.
-    while (p.form > 1 && (int64_t)rows * chunks(p.form) < (p.form > 8 ? 2 * kFillWorkgroups : kFillWorkgroups) && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
+    // A row that one workgroup holds is not cut, unless rows are few and it has more than 8 pieces a lane: 300 rows of 8000 in bf16, 8 alternatives,
+    // 6.6 us, 10.2 cut; of 32001 12.4 / 14.0; 64 rows of 32001 9.5, 8.0 as below.
+    const int alone = rows > kRowsWhole ? 16 : 8;
+    while (p.form > 1 && (chunks(p.form) > 1 || p.form > alone) && (int64_t)rows * chunks(p.form) < (p.form > 8 ? 2 * kFillWorkgroups : kFillWorkgroups) && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
     p.chunks = chunks(p.form);
     while (p.form > 1 && chunks(p.form / 2) == p.chunks) p.form /= 2;
-    if (p.chunks > 1 && rows <= kRowsWhole && pieces <= 16 * kRowLanes) {
+    // Rows that 1024 lanes hold: one launch, a row a workgroup.  256 rows of 50265 in bf16, 8 alternatives, 12.8 us, 15.9 cut; 512 18.5 / 21.7;
+    // 300 of 128003, whose registers leave room for one such workgroup a compute unit, 35 / 27.
+    if (p.chunks > 1 && rows <= (pieces <= 8 * kRowLanes ? 4 * kRowsWhole : kRowsWhole) && pieces <= 16 * kRowLanes) {
         p.lanes = kRowLanes; p.chunks = 1;
         p.form = pieces <= 4 * kRowLanes ? 4 : pieces <= 8 * kRowLanes ? 8 : 16;
     }
