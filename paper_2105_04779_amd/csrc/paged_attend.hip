@@ -39,8 +39,10 @@ constexpr int64_t kManyPieces = 16;
 // 30.2 / 14.6 (5 tiles each); 900 of up to 400, one of 128, 46.6 / 31.2 (13); 100 of up to 600 in fp32, two of 64, 21.9 / 16.8 (10); 70 of up to 2000, one
 // of 64, 15.5 / 16.5 (16); 300 of up to 1000, two of 128, 45 / 58 (32).
 constexpr int kFew = 4, kFewOfMany = 16;
-// Positions that one wavefront may be left with where the sequences alone fill the device, so that nothing is joined: 300 sequences of 100 to 512
-// (16 heads of 64) 87 us whole, 98 cut; 200 of 200 to 1024 120 / 123.
+// Positions that one wavefront may be left with where the sequences alone fill the device, so that nothing is joined: kShort, and as many for each
+// time that they fill it as kRound bytes of keys have.  us, whole / cut: 16 heads of 64, 160 sequences of up to 700 59 / 62, of 1500 122 / 110; 600 of
+// up to 2000 429 / 497; 8 heads of 128, 160 of up to 1000 86 / 74, 600 of 700 164 / 173.
+constexpr int64_t kRound = 128 << 10;
 constexpr int kShort = 2048;
 // Sequences are never cut where there are more than kCutMost, whose lengths every wavefront would have to add up, and of more than kCutMax only
 // longer ones: 8000 of up to 2500, one key head of 64, 447 us whole, 500 cut; 1500 of up to 8192, one of 128, 719 / 554.
@@ -137,7 +139,7 @@ __device__ __forceinline__ bool find_span(const AttendArgs &a, int span, int til
 }
 
 // Keys and values pass the caches by: between two reads of a layer's cache lie those of all others.  us, inputs that are in no cache, kept in
-// them / passed by: 512 continuations of up to 256 positions 66 / 57, 64 sequences of 1024 to 4096 131 / 116, two of up to 131072 179 / 161.
+// them / passed by: 512 continuations of up to 256 positions 63 / 57, 64 sequences of 1024 to 4096 135 / 120, two of up to 131072 178 / 161.
 // (Two blocks of rows that read the same, more than 32 rows a key head, lose 3 %; a cache that the memory-side cache holds from call to call 4 to 9 %.)
 __device__ __forceinline__ void request16(unsigned lds_addr, const char *from)
 {
@@ -691,8 +693,10 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
     while (p.waves < most && 2 * p.waves * B * units <= slots && 2 * p.waves <= tiles) p.waves *= 2;
     // whole sequences: where they alone fill the device and none is long, where the lengths would take long to add up, and where a few
     // tiles are all that a wavefront gets
+    const int64_t key_bytes = p.padded * (int64_t)dtype_size(c.dtype);
     const bool few = tiles <= (int64_t)(B > 64 ? kFewOfMany : kFew) * p.waves;
-    const bool whole = few || B > kCutMost || all > 1 << 30 || (B > kCutMax ? n <= 2 * kShort : n <= kShort && B * units >= slots);
+    const bool fill = B * units >= slots && n <= kShort && n * key_bytes * slots <= kRound * B * units;
+    const bool whole = few || fill || (B > kCutMax && n <= 2 * kShort) || B > kCutMost || all > 1 << 30;
     if (!whole) p.waves = 1;
     p.spans = whole ? 0 : (int)(target < all ? target : all);
     p.grid = (int)((whole ? B : p.spans) * units);
