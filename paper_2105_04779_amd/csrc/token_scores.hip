@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kMaxAlternatives = 64;
 constexpr int kLanes = 256;
-constexpr int kCandidates = 1024;        // of a chunk that are ranked by counting; with more (ties) one is taken at a time
+constexpr int kCandidates = 1024;        // of a chunk that are ranked by counting
 constexpr int kFillWorkgroups = 512;     // chunks get smaller until about so many workgroups share the logits: two a compute unit
 constexpr int kRowLanes = 1024, kRowsWhole = 256;
 constexpr int32_t kMaxVocab = 1 << 19;
@@ -154,13 +154,13 @@ __device__ __forceinline__ void add_term(float x, float ref, float &S, float &W)
     W = fmaf(e, fmaxf(d, -1e4f), W);                                 // (a banned token: 0, not 0 * inf)
 }
 
-// The k-th largest of the numbers of `COUNT` x 64 lanes, by its upper 16 bits (0: fewer than k are above 0).
-template <int COUNT>
+// The k-th largest of the numbers of `COUNT` x 64 lanes, without its bits below LOW (0: fewer than k are above 0).
+template <int LOW, int COUNT>
 __device__ __forceinline__ unsigned kth_of(const unsigned (&mine)[COUNT], int k)
 {
     unsigned bound = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
+    for (int bit = 31; bit >= LOW; --bit) {
         const unsigned t = bound | (1u << bit);
         int n = 0;
 #pragma unroll
@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
     __shared__ Sums part[WAVES];
     __shared__ int count;
     __shared__ Key top[WAVES];
+    __shared__ int equal[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t r = blockIdx.x / a.chunks;
     const int chunk = blockIdx.x - (int)r * a.chunks;
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
         else a.keys[(int64_t)blockIdx.x * a.k + i] = key;
     };
     const unsigned maxima[4] = {best[lane], best[lane + 64], best[lane + 128], best[lane + 192]};
-    const unsigned bound = kth_of(maxima, a.k);
+    const unsigned bound = kth_of<16>(maxima, a.k);
     const float least = bound ? value_of(bound) : -FLT_MAX;
     auto collect = [&](float x, int index) __attribute__((always_inline)) {
         if (x >= least) {
@@ -264,7 +265,62 @@ __global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
         for (int i = 0; i < N; ++i) collect(Piece<T>::at(v[j], i), row.head + (from + j * LANES) * N + i);
     }
     __syncthreads();
-    const int n = count;
+    int n = count;
+    if (n > kCandidates && bound) {
+        // Ties, mostly: what is larger than the exact bound, and of what equals it, looked through in order of index, the first that still
+        // lack.  (Pieces are read again: rare, and registers are short.)  1024 rows of 128003 zeros in fp32, 20 alternatives, 257 us, one at a
+        // time 2260.
+        const float exact = value_of(kth_of<0>(maxima, a.k));
+        __syncthreads();
+        if (tid == 0) count = 0;
+        for (int i = tid; i < kCandidates + 8; i += LANES) cand[i] = 0;
+        __syncthreads();
+        auto above = [&](float x, int index) __attribute__((always_inline)) {
+            if (x > exact) {
+                const int at = atomicAdd(&count, 1);
+                if (at < kCandidates) cand[at] = key_of(x, index);
+            }
+        };
+        above(x_edge, edge);
+#pragma unroll 1
+        for (int j = 0; j < used; ++j) {
+            const u4 again = load_piece<T>(row, from + j * LANES, end);
+#pragma unroll
+            for (int e = 0; e < N; ++e) above(Piece<T>::at(again, e), row.head + (from + j * LANES) * N + e);
+        }
+        __syncthreads();
+        n = count;
+        // the elements before the pieces, the pieces, those behind: a lane's lie behind those of the lanes before it
+#pragma unroll 1
+        for (int j = -1; j <= used && n < a.k; ++j) {
+            unsigned flags = 0;
+            int index = edge;
+            if (j < 0 || j == used) {
+                flags = edge >= 0 && (edge < row.head) == (j < 0) && x_edge == exact;
+            } else {
+                const u4 again = load_piece<T>(row, from + j * LANES, end);
+                index = row.head + (from + j * LANES) * N;
+#pragma unroll
+                for (int e = 0; e < N; ++e) flags |= (unsigned)(Piece<T>::at(again, e) == exact) << e;
+            }
+            int upto = __popc(flags);
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int other = __shfl_up(upto, o, 64);
+                if (lane >= o) upto += other;
+            }
+            if (lane == 63) equal[w] = upto;
+            __syncthreads();
+            int at = n + upto - __popc(flags);
+            for (int i = 0; i < WAVES; ++i) {
+                if (i < w) at += equal[i];
+                n += equal[i];
+            }
+            for (; flags && at < a.k; flags &= flags - 1) cand[at++] = key_of(exact, index + __ffs((int)flags) - 1);
+            __syncthreads();
+        }
+        if (count < a.k) n = min(n, a.k);
+    }
     if (n <= kCandidates) {
         for (int c = tid; c < n; c += LANES) {
             const Key key = cand[c];
@@ -344,7 +400,7 @@ __global__ void __launch_bounds__(kLanes) k_score_join(const ScoreArgs a)
     if (a.k == 0) return;
     const unsigned maxima[4] = {best[lane], best[lane + 64], best[lane + 128], best[lane + 192]};
     // (0: no alternative.  64 entries are ranked sooner than bounded: 2000 rows of 50265 in bf16, 8 alternatives, 51.7 us, 53.2 bounded)
-    const Key least = total <= 64 ? (Key)1 : max((Key)kth_of(maxima, a.k) << 32, (Key)1);
+    const Key least = total <= 64 ? (Key)1 : max((Key)kth_of<16>(maxima, a.k) << 32, (Key)1);
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
         if (key[j] >= least) list[atomicAdd(&count, 1)] = key[j];

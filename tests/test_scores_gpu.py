@@ -98,6 +98,27 @@ def test_ties_and_orders(dtype):
         _check(f"ties, cut {dtype} k {k}", np.tile(x, (1, 7)), dtype, k)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,offset", [(1500, 0), (33337, 3), (120001, 5), (300007, 1)])
+def test_thousands_of_ties_at_the_bound(dtype, V, offset):
+    """More elements tie than are ranked by counting: some larger ones before and behind, ties from a place on, a few lanes' only, at both ends of a
+    row that starts anywhere, all of one sign of zero or both."""
+    g = np.random.default_rng(V)
+    x = np.zeros((10, V), dtype=np.float32)
+    x[1] = np.minimum(g.standard_normal(V), 0)
+    x[2, g.permutation(V)[:5]] = (3.0, 1.0, 2.0, 1.0, 7.0)
+    x[3, :V // 3] = -1
+    x[4] = -2.5
+    x[4, :3], x[4, -4:] = 1.0, 1.0
+    x[5, ::2] = -0.0
+    x[6] = np.where(np.arange(V) % 2048 < 16, 1.0 + (np.arange(V) % 7), -np.inf)     # a few lanes hold all
+    x[7] = np.where(np.arange(V) < V - 1100, -np.inf, 4.0)
+    x[8, V // 2:V // 2 + 1200] = g.integers(1, 4, len(x[8, V // 2:V // 2 + 1200]))
+    x[9, g.permutation(V)[:40]] = 1.0
+    for k in (1, 8, 64):
+        _check(f"ties at the bound {dtype} V {V} k {k}", x, dtype, k, pad=7, offset=offset)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("k", [1, 8, 20, 64])
 def test_alternatives_of_rows_that_are_cut(dtype, k):
