@@ -317,7 +317,8 @@ def test_results_repeat_and_streams_keep_apart():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("B,T,kv,d,page", [(1, 1, 1, 8, 1), (5, 1, 8, 64, 16), (3, 40, 2, 80, 7), (2, 513, 4, 128, 32), (70, 3, 1, 256, 16)])
+@pytest.mark.parametrize("B,T,kv,d,page", [(1, 1, 1, 8, 1), (5, 1, 8, 64, 16), (3, 40, 2, 80, 7), (2, 513, 4, 128, 32), (70, 3, 1, 256, 16),
+                                             (3, 259, 1, 8, 16), (2, 100, 3, 24, 5), (4, 31, 1, 64, 16), (2, 9, 17, 256, 4)])
 def test_append(dtype, B, T, kv, d, page):
     import torch
     g = np.random.default_rng(60 + T)
