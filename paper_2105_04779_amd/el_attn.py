@@ -429,7 +429,7 @@ class PagedCache:
     transposed view of [pages, kv_heads, page_size, d_head] is as good).  The table [B, columns] int32 and the lengths
     int32 [B] are the caller's, shared by all layers: position t of sequence b lies in page table[b, t // page_size];
     an entry outside the pool (-1) holds no positions.  Scratch memory comes from torch per call, so calls on several streams
-    and captured graphs keep apart.
+    and captured graphs keep apart.  No work (no sequence, no token, no pair, no beam) is no error.
     """
 
     def __init__(self, K, V):
@@ -476,6 +476,8 @@ class PagedCache:
             _check_index("counts", counts, device, (B,))
         row = self.kv_heads * self.d_head
         at, stride, columns = self._table(table, B)
+        if B == 0 or T == 0:
+            return
         _call("el_attn_paged_append", device, lib.el_attn_paged_append, self._pages, at, stride, columns, lengths.data_ptr(),
               _ptr(counts), k.data_ptr(), v.data_ptr(), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
 
@@ -493,6 +495,8 @@ class PagedCache:
             if slopes.shape != (heads,) or not slopes.is_contiguous():
                 raise ValueError(f"slopes must be contiguous [{heads}]")
         at, stride, columns = self._table(table, B)
+        if B == 0 or beam == 0:
+            return
         if n is None:
             n = min(columns * self.page_size, _INT32_MAX)
         if abs(n) > _INT32_MAX or abs(window) > _INT32_MAX:
@@ -544,6 +548,8 @@ class PagedCache:
         _check_index("dst", dst, device, shape)
         if counts is not None:
             _check_index("counts", counts, device, shape)
+        if shape[0] == 0:
+            return
         _call("el_attn_paged_copy", device, lib.el_attn_paged_copy, self._pages, src.data_ptr(), dst.data_ptr(), _ptr(counts),
               shape[0])
 
@@ -551,7 +557,7 @@ class PagedCache:
 def score_tokens(logits, tokens=None, *, k=0):
     """What rows of logits [rows, vocab] (rows strided, a row contiguous) say about the next token: (logprob, entropy,
     top_logprob, top_index), float32 [rows], [rows], [rows, k] and int32 [rows, k].  logprob is that of tokens (int32 [rows];
-    None: logprob is None); the k best alternatives come in descending order.  See el_attn_score_tokens."""
+    None: logprob is None); the k best alternatives come in descending order.  No rows: empty results.  See el_attn_score_tokens."""
     import torch
     shape = logits.shape
     if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and logits.stride(1) != 1) or max(shape) > _INT32_MAX:
@@ -568,6 +574,8 @@ def score_tokens(logits, tokens=None, *, k=0):
     entropy = torch.empty(rows, dtype=f32, device=device)
     top_logprob = torch.empty((rows, k), dtype=f32, device=device)
     top_index = torch.empty((rows, k), dtype=torch.int32, device=device)
+    if rows == 0:
+        return logprob, entropy, top_logprob, top_index
     nbytes = lib.el_attn_score_workspace_bytes(rows, vocab, k)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
     _call("el_attn_score_tokens", device, lib.el_attn_score_tokens, code, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab,

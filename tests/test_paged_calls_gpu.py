@@ -1,0 +1,40 @@
+"""Calls of the paged cache and the token scores at the edges of what they take: no work, operands that ask for a derivative,
+values that are not finite."""
+import numpy as np
+import pytest
+
+import oracle
+from test_paged_gpu import Case, _host
+
+pytestmark = pytest.mark.gpu
+
+
+def test_no_work_is_no_error():
+    """A step without forks, without new tokens, of no sequence or no beam, scores of no row: nothing moves, empty results."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    c = Case(90, "bf16", 2, 2, 4, 2, 64, 16, [20, 33])
+    K, V = c.cache.K.clone(), c.cache.V.clone()
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    c.cache.copy_pages(none, none)
+    c.cache.copy_pages(none, none, none)
+    c.cache.append(c.q_d[:, :0, :2], c.q_d[:, :0, :2], c.table_d, c.lengths_d)
+    c.cache.append(c.q_d[:0, :, :2], c.q_d[:0, :, :2], c.table_d[:0], none, none)
+    for q, table, lengths in ((c.q_d[:0], c.table_d[:0], none), (c.q_d[:0], c.table_d[:0], None), (c.q_d[:, :0], c.table_d, c.lengths_d)):
+        rows = q.shape[0] * q.shape[1]
+        out = c.cache.attend(q, table, lengths, out_dtype="f32")
+        assert out.shape == q.shape and out.dtype == torch.float32
+        assert c.cache.attend(q, table, lengths, out=torch.empty_like(q)).shape == q.shape
+        A, lse = c.cache.attend_segment(q, table, lengths, window=3)
+        assert A.shape == (rows, 4 * 64) and lse.shape == (rows, 4)
+    logprob, entropy, top, index = el_attn.score_tokens(torch.zeros((0, 99), device="cuda"), none, k=5)
+    assert logprob.shape == entropy.shape == (0,) and top.shape == index.shape == (0, 5) and index.dtype == torch.int32
+    assert el_attn.score_tokens(torch.zeros((0, 99), device="cuda"))[0] is None
+    torch.cuda.synchronize()
+    assert torch.equal(K.nan_to_num(5.0), c.cache.K.nan_to_num(5.0)) and torch.equal(V.nan_to_num(5.0), c.cache.V.nan_to_num(5.0))
+    # the checks are those of every call
+    for call in (lambda: c.cache.copy_pages(none, none.long()), lambda: c.cache.attend(c.q_d[:0], c.table_d, none), lambda: c.cache.attend(c.q_d[:0].float(), c.table_d[:0], none),
+                 lambda: c.cache.append(c.q_d[:0, :, :2], c.q_d[:0, :, :2], c.table_d[:0], none.long()), lambda: el_attn.score_tokens(torch.zeros((0, 99), device="cuda"), k=65)):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("taken")
