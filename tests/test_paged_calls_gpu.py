@@ -38,3 +38,26 @@ def test_no_work_is_no_error():
         with pytest.raises(ValueError):
             call()
             pytest.fail("taken")
+
+
+def test_a_tangent_is_refused():
+    """Forward-mode differentiation: a result without the tangent would be wrong in silence."""
+    import torch
+    import torch.autograd.forward_ad as fw
+    from paper_2105_04779_amd import el_attn
+    c = Case(91, "f32", 2, 2, 4, 2, 64, 16, [20, 33])
+    slopes, logits, new = torch.ones(4, device="cuda"), torch.randn((3, 50), device="cuda"), c.q_d[:, :, :2]
+    with fw.dual_level():
+        dual = lambda t: fw.make_dual(t, torch.ones_like(t))
+        for call in (lambda: c.cache.attend(dual(c.q_d), c.table_d, c.lengths_d), lambda: c.cache.attend_segment(dual(c.q_d), c.table_d, c.lengths_d),
+                     lambda: c.cache.attend(c.q_d, c.table_d, c.lengths_d, slopes=dual(slopes)),
+                     lambda: c.cache.attend(c.q_d, c.table_d, c.lengths_d, out=dual(torch.empty_like(c.q_d))),
+                     lambda: c.cache.append(dual(new), new, c.table_d, c.lengths_d), lambda: c.cache.append(new, dual(new), c.table_d, c.lengths_d),
+                     lambda: el_attn.PagedCache(dual(c.cache.K), c.cache.V), lambda: el_attn.PagedCache(c.cache.K, dual(c.cache.V)),
+                     lambda: el_attn.score_tokens(dual(logits))):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+                pytest.fail("taken")
+        # operands without one are taken there as elsewhere
+        a = c.cache.attend(c.q_d, c.table_d, c.lengths_d)
+    assert torch.equal(a, c.cache.attend(c.q_d, c.table_d, c.lengths_d))
