@@ -534,10 +534,10 @@ class PagedCache:
         element = self._element if code == self.dtype else _torch_dtype(code)
         if out is None:
             out = self._torch.empty(queries.shape, dtype=element, device=self.device)
-        elif out.shape != queries.shape or out.dtype != element or not out.is_contiguous() or out.device != self.device:
+        elif out.shape != queries.shape or not out.is_contiguous():
             raise ValueError(f"out must be a contiguous {element} tensor of the queries' shape")
         else:
-            _check_tangent("out", out)
+            _check_values("out", out, self.device, element)
         self._attend(queries, table, lengths, n, scale, softcap, window, slopes, out, code, None)
         return out
 

@@ -61,3 +61,14 @@ def test_a_tangent_is_refused():
         # operands without one are taken there as elsewhere
         a = c.cache.attend(c.q_d, c.table_d, c.lengths_d)
     assert torch.equal(a, c.cache.attend(c.q_d, c.table_d, c.lengths_d))
+
+
+def test_an_output_that_asks_for_a_gradient_is_refused():
+    import torch
+    c = Case(92, "f32", 2, 1, 4, 2, 64, 16, [20, 33])
+    out = torch.empty_like(c.q_d).requires_grad_()
+    with pytest.raises(ValueError):
+        c.cache.attend(c.q_d, c.table_d, c.lengths_d, out=out)
+    with torch.no_grad():
+        assert c.cache.attend(c.q_d, c.table_d, c.lengths_d, out=out) is out
+    assert torch.equal(out.detach(), c.cache.attend(c.q_d, c.table_d, c.lengths_d))
