@@ -453,13 +453,22 @@ class PagedCache:
             raise ValueError("K and V are written in place: they must not require a gradient")
         _check_tangent("K", K)
         _check_tangent("V", V)
-        self.K, self.V = K, V
+        self._K, self._V = K, V
         self.device = K.device
         pages, self.page_size, self.kv_heads, self.d_head = K.shape
         self.dtype = _dtype_code(K)
         self._element = K.dtype
         self._pages = ElAttnPages(_ptr(K), _ptr(V), K.stride(0), K.stride(1), K.stride(2),
                                   pages, self.page_size, self.kv_heads, self.d_head, self.dtype)
+
+    @property
+    def K(self):
+        """The pool of keys that the cache was made of; another one needs another cache."""
+        return self._K
+
+    @property
+    def V(self):
+        return self._V
 
     def _table(self, table, B):
         """(address, row stride, columns) of a table for B sequences."""

@@ -6,6 +6,14 @@ import torch.autograd.forward_ad as fw
 from paper_2105_04779_amd import el_attn
 
 
+def test_a_cache_keeps_the_pools_that_it_was_made_of():
+    """The kernels are given the addresses that the constructor saw: another tensor in their place would be ignored."""
+    cache = object.__new__(el_attn.PagedCache)
+    for name in ("K", "V"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, torch.zeros((4, 16, 2, 64)))
+
+
 def test_what_asks_for_a_derivative_is_refused():
     x, cpu = torch.zeros(3), torch.device("cpu")
     el_attn._check_values("x", x, cpu, torch.float32)
