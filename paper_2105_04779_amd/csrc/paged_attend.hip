@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
 #pragma unroll
                 for (int x = 0; x < NA; ++x)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[rg][x][e] = a.softcap * kLog2e * tanhf(p[rg][x][e]);
+                    for (int e = 0; e < 4; ++e) p[rg][x][e] = a.softcap * tanhf(p[rg][x][e]) * kLog2e;         // (a cap times log2 e may be too large)
             }
             if (a.slopes) {
 #pragma unroll

@@ -72,3 +72,21 @@ def test_an_output_that_asks_for_a_gradient_is_refused():
     with torch.no_grad():
         assert c.cache.attend(c.q_d, c.table_d, c.lengths_d, out=out) is out
     assert torch.equal(out.detach(), c.cache.attend(c.q_d, c.table_d, c.lengths_d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_a_cap_of_any_size(dtype):
+    """Beyond the scores' own size a cap changes nothing, up to the largest number there is.  Scores up to 2.5, caps from 1e6: (s / c)^2 / 3 is
+    below 2^-40.  Whole numbers: the products are exact.  scale / c loses digits among the subnormal numbers, 2^-150 of 0.1 / 3.4e38 = 2^-131.3 at most: 2^-18.7 of a score."""
+    import torch
+    c = Case(94, dtype, 3, 1, 4, 4, 64, 16, [33, 64, 40])
+    g = np.random.default_rng(94)
+    c.q_d.copy_(torch.from_numpy(g.integers(-1, 2, c.q.shape) * (np.arange(64) < 25)))
+    c.cache.K.copy_(torch.from_numpy(g.integers(-1, 2, c.K.shape)))
+    none, none_lse = (_host(t) for t in c.cache.attend_segment(c.q_d, c.table_d, c.lengths_d, scale=0.1))
+    spread = np.nanmax(np.abs(c.V))
+    for cap in (1e6, 1e30, 3.0e38, 3.4028234663852886e38):
+        A, lse = (_host(t) for t in c.cache.attend_segment(c.q_d, c.table_d, c.lengths_d, scale=0.1, softcap=cap))
+        D = 2.5 * (2.0 ** -18.7 if cap > 1e30 else 0.0) + 2.5 * 8 * 2.0 ** -24 + 16 * 2.0 ** -24 + 80 * 2.0 ** -24
+        assert np.isfinite(A).all() and np.isfinite(lse).all(), cap
+        assert np.abs(A - none).max() <= 4 * D * spread and np.abs(lse - none_lse).max() <= 2 * D, cap
