@@ -17,6 +17,7 @@
 // once.  A span that goes on to the next sequence closes a piece and starts another.  Every wavefront adds the lengths up by
 // itself, so the cut follows them without the host knowing them.  Where sequences alone fill the device and are short, a
 // wavefront takes one whole, and nothing is joined.
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 #include "mfma.h"
@@ -55,7 +56,10 @@ struct AttendArgs {
     const char *queries;
     int64_t query_stride;                    // bytes
     const float *slopes;
-    float scale, softcap;
+    // Scores stay as they leave the matrix unit; with a cap, a bias or a scale that is not positive (`shaped`) they are multiplied by `product` first
+    // and kept in natural units.  `unit` > 0: powers of two in one of theirs, `natural`: e's.
+    bool shaped;
+    float product, softcap, unit, natural;
     int window, n, B, beam, heads, kv_heads, d;
     int group, R, row_blocks, rows;          // heads / kv_heads; query rows of a key head; blocks of them; rows of a block, at most
     bool near;                               // key heads that are neighbours in memory on one die
@@ -66,7 +70,7 @@ struct AttendArgs {
     float *lse;
     int2 *pieces;                            // [B] first slot and number of slots of a sequence's pieces
     float *part_o;                           // [slot][unit][rows][d] weighted sums relative to part_ml's maximum
-    float2 *part_ml;                         // [slot][unit][rows] (maximum, sum), powers of two
+    float2 *part_ml;                         // [slot][unit][rows] (largest score, sum)
 };
 
 // Tiles [x, y) of a sequence of `len` positions.
@@ -230,7 +234,6 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
     }
     const char *const Kh = a.c.K + kvh * a.c.head;
     const int64_t k_to_v = a.c.V - a.c.K;
-    const float to_exp2 = a.softcap > 0.f ? a.scale / a.softcap : a.scale * kLog2e;  // what a product is multiplied by: the cap's argument
 
     Start st{span, 0, 0, 0, 1, false};
     if (a.spans && !find_span(a, span, TP, st)) return;
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
             q[rg][c] = u4{0, 0, 0, 0};
             if (here && (4 * c + g) * 16 < a.d * ES) q[rg][c] = *(const u4 *)(p + (4 * c + g) * 16);
         }
-        slope[rg] = here && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+        slope[rg] = here && a.slopes ? a.slopes[head] : 0.f;
     }
     const int len = length_of(a, st.b), first = a.window ? max(0, len - a.window) : 0;
     const int2 range = tile_range(a, len, TP);
@@ -382,26 +385,35 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
                     }
                 }
         }
-        // ---- softmax: lane (g, r16) holds positions 16 x + 4 g + e of row r16; scores in powers of two ----
+        // ---- softmax: lane (g, r16) holds positions 16 x + 4 g + e of row r16 ----
+        // (the largest score is taken from the others before they become powers of two: what scores have in common takes no digits from their
+        // distances)
         const unsigned bits = mask >> (4 * g);
+        const float unit = a.unit;
         float p[RG][NA][4];
 #pragma unroll
         for (int rg = 0; rg < RG; ++rg) {
 #pragma unroll
             for (int x = 0; x < NA; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[rg][x][e] = s[rg][x][e] * to_exp2;
-            if (a.softcap > 0.f) {
+                for (int e = 0; e < 4; ++e) p[rg][x][e] = s[rg][x][e];
+            if (a.shaped) {
 #pragma unroll
                 for (int x = 0; x < NA; ++x)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[rg][x][e] = a.softcap * tanhf(p[rg][x][e]) * kLog2e;         // (a cap times log2 e may be too large)
-            }
-            if (a.slopes) {
+                    for (int e = 0; e < 4; ++e) p[rg][x][e] *= a.product;
+                if (a.softcap > 0.f) {
 #pragma unroll
-                for (int x = 0; x < NA; ++x)
+                    for (int x = 0; x < NA; ++x)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[rg][x][e] -= slope[rg] * (float)(dist0 - 16 * x - 4 * g - e);
+                        for (int e = 0; e < 4; ++e) p[rg][x][e] = a.softcap * tanhf(p[rg][x][e]);
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int x = 0; x < NA; ++x)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[rg][x][e] = fmaf(-slope[rg], (float)(dist0 - 16 * x - 4 * g - e), p[rg][x][e]);
+                }
             }
             if (mask != (TP == 32 ? 0xffffffffu : 0xffffu)) {
 #pragma unroll
@@ -417,7 +429,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
                 for (int e = 0; e < 4; ++e) mx = fmaxf(mx, p[rg][x][e]);
             mx = fmaxf(m[rg], max_over_groups(mx));
             if (__ballot(mx > m[rg])) {
-                const float f = m[rg] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rg] - mx);
+                const float f = m[rg] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[rg] - mx) * unit);
                 l[rg] *= f;
 #pragma unroll
                 for (int t = 0; t < DT16; ++t)
@@ -425,12 +437,12 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
                     for (int e = 0; e < 4; ++e) acc[rg][t][e] *= f;
                 m[rg] = mx;
             }
-            const float ref = (m[rg] == -INFINITY ? 0.f : m[rg]) - SHIFT;
+            const float ref = m[rg] == -INFINITY ? 0.f : m[rg];
 #pragma unroll
             for (int x = 0; x < NA; ++x)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[rg][x][e] = __builtin_amdgcn_exp2f(p[rg][x][e] - ref);
+                    p[rg][x][e] = __builtin_amdgcn_exp2f((p[rg][x][e] - ref) * unit + SHIFT);
                     l[rg] += p[rg][x][e];
                 }
         }
@@ -513,7 +525,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
             // (a wavefront without a position: sum 0.  A NaN score leaves its maximum at -inf and its sum at NaN, which stays)
             auto factor = [&](int k) __attribute__((always_inline)) {
                 const float mk = ml0[k * (NS * 32) + 16 * rg + r16].x;
-                return mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - M);
+                return mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mk - M) * a.unit);
             };
 #pragma unroll
             for (int t = 0; t < DT16; ++t) acc[rg][t] = f4{0.f, 0.f, 0.f, 0.f};
@@ -542,7 +554,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
         const int64_t out_row = (b * a.beam + r / a.group) * a.heads + kvh * a.group + r % a.group;
         if (g == 0 && w == 0) {
             if (!whole) a.part_ml[slot + rb] = float2{M, L};
-            else if (a.lse) a.lse[out_row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - SHIFT) * kLn2;
+            else if (a.lse) a.lse[out_row] = empty ? -INFINITY : fmaf(M, a.natural, (__builtin_amdgcn_logf(L) - SHIFT) * kLn2);
         }
         const float inv = whole ? 1.f / L : 1.f;
 #pragma unroll
@@ -608,7 +620,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int til
     }
     const float ref = M == -INFINITY ? 0.f : M;
     // (a piece without a position: sum 0.  A NaN score leaves its maximum at -inf and its sum at NaN, which stays)
-    auto weight = [&](float m) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - ref); };
+    auto weight = [&](float m) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - ref) * a.unit); };
     float L = 0.f;
     for (int s = tid; s < pc.y; s += LANES) {
         const float2 v = ml[s * step];
@@ -622,7 +634,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int til
         L = (red[4] + red[5]) + (red[6] + red[7]);
     }
     const bool empty = M == -INFINITY && !(L != L);
-    if (tid == 0 && a.lse) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L) - shift) * kLn2;
+    if (tid == 0 && a.lse) a.lse[row] = empty ? -INFINITY : fmaf(M, a.natural, (__builtin_amdgcn_logf(L) - shift) * kLn2);
     f4 o{0.f, 0.f, 0.f, 0.f};
     auto add = [&](const f4 &v, float f) __attribute__((always_inline)) {
 #pragma unroll
@@ -771,7 +783,11 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     a.c = page_view(*cache, table, table_stride, table_pages);
     a.lengths = lengths;
     a.queries = (const char *)queries; a.query_stride = query_stride * es;
-    a.slopes = rule->slopes; a.scale = rule->scale; a.softcap = rule->softcap; a.window = rule->window;
+    a.slopes = rule->slopes; a.softcap = rule->softcap; a.window = rule->window;
+    a.shaped = rule->softcap > 0.f || rule->slopes || !(rule->scale >= FLT_MIN);
+    a.product = rule->softcap > 0.f ? rule->scale / rule->softcap : rule->scale;
+    a.unit = a.shaped ? kLog2e : rule->scale * kLog2e;
+    a.natural = a.shaped ? 1.f : rule->scale;
     a.n = n; a.B = B; a.beam = beam; a.heads = heads; a.kv_heads = cache->kv_heads; a.d = cache->d_head;
     a.group = heads / cache->kv_heads; a.R = beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
     a.near = p.near; a.waves = p.waves; a.spans = p.spans;

@@ -1,0 +1,62 @@
+"""How precise attention over pages is where every product is exact (small whole numbers), so that only what follows them errs.
+
+u = 2^-24 (half a step of fp32, relative).  Scores lie at most A below the largest.  Their distance to it is formed in one rounding (u A),
+with a factor that is rounded twice (1.3 u A); an exponential is good to 2 u; a tile with a larger maximum, or the join of two wavefronts, scales
+what is there once more (u A + 2 u, at most twice for two tiles).  Together D = 4.3 u A + 6 u, whatever the size of the scores.  The output is off by
+2 D, by the sums (n / 16 + 64 roundings each), by the parts that a probability is split into (2^-24 of it; in fp16 also 2^-40 of the largest: half
+the smallest step of fp16, 2^-25, at a scale of 2^15) and by half a step.
+"""
+import numpy as np
+import pytest
+
+import oracle
+from helpers import record, to_device
+from test_paged_gpu import HALF_STEP, SMALLEST, Case, _host
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _whole_numbers(dtype, lengths, heads=4, d=64, seed=95):
+    """A case with queries and keys of whole numbers up to 3."""
+    c = Case(seed, dtype, len(lengths), 1, heads, heads, d, 16, lengths)
+    g = np.random.default_rng(seed)
+    c.q = g.integers(-3, 4, c.q.shape).astype(np.float32)
+    c.K = np.where(np.isnan(c.K), c.K, g.integers(-3, 4, c.K.shape)).astype(np.float32)
+    return c
+
+
+def _put(c):
+    c.q_d = to_device(c.q, c.dtype)
+    c.cache.K.copy_(to_device(c.K, c.dtype))
+    c.cache.V.copy_(to_device(c.V, c.dtype))
+
+
+def _compare(tag, c, A, scale, largest_only=0.0, **rule):
+    """Against fp64, every output and log-sum-exp within its bound; scale in fp32."""
+    out, lse = c.cache.attend_segment(c.q_d, c.table_d, c.lengths_d, scale=scale, **rule)
+    ref, ref_lse, info = oracle.paged_attend_reference(c.K, c.V, c.table, c.lengths, c.q, scale=float(np.float32(scale)), **rule)
+    out, lse = _host(out).reshape(ref.shape), _host(lse).reshape(ref_lse.shape)
+    D, sums = 4.3 * U * A + 6 * U, (info["n"] / 16 + 64) * U
+    bound = (2 * D + 2 * sums + 2.0 ** -24)[..., None] * info["spread"] + largest_only
+    bound = bound + HALF_STEP["f32"] * (np.abs(ref) + bound) + 1e-37
+    worst = float((np.abs(out - ref) / bound).max())
+    err = float((np.abs(lse - ref_lse) / (D + sums + 2 * U * np.abs(ref_lse) + 1e-37)).max())
+    record(f"{tag}: {worst:.3f} of the bound, lse {err:.3f} of its")
+    assert worst <= 1 and err <= 1, f"{tag}: {worst:.3f} of the bound, lse {err:.3f} of its"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("scale", [0.125, 0.1])
+@pytest.mark.parametrize("side", [1, -1])
+def test_scores_far_from_zero_keep_their_distances(dtype, scale, side):
+    """Thousands that all scores have in common (keys with a large component along the query) take no digits from their differences."""
+    c = _whole_numbers(dtype, [33, 64, 40, 57, 48, 64])
+    c.q[:] = 16.0
+    c.K[:] = np.where(np.isnan(c.K), c.K, 32.0 * side)
+    g = np.random.default_rng(96)
+    c.K[..., 0] = np.where(np.isnan(c.K[..., 0]), np.nan, 32.0 * side + g.integers(-1, 2, c.K.shape[:3]))       # scores apart by 16 scale
+    c.K[..., 1] = np.where(np.isnan(c.K[..., 1]), np.nan, 32.0 * side + g.integers(0, 2, c.K.shape[:3]))
+    _put(c)
+    _compare(f"far scores {dtype} scale {scale} side {side}", c, 3 * 16 * scale, scale)
