@@ -201,17 +201,17 @@ template <int DT_, int DP_, int RG_> struct Form {
     static constexpr int WAVES = PER_CU >= 8 ? 8 : PER_CU >= 4 ? 4 : 2;            // of a workgroup, at most
 };
 
-template <class F>
+// NP: parts of a probability (launch_attend).
+template <class F, int NP>
 __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(const AttendArgs a)
 {
     constexpr bool F32 = F::F32, BF16 = F::BF16;
     constexpr int DT = F::DT, DP = F::DP, RG = F::RG, ES = F::ES, TP = F::TP, ROWB = F::ROWB, NS = F::NS, TILEB = F::TILEB;
     constexpr int CPR = ROWB / 16, NI = TILEB / 1024, RPI = 64 / CPR, PENDING = (NS - 1) * (2 * NI + 1), DT16 = DP / 16;
     constexpr int QC = F32 ? DP / 16 : DP / 32;                      // pieces of 16 bytes of a query row that a lane holds
-    // P in 16 bits: parts that add up to it.  fp16: two (22 bits), times 2^12, which keeps the low part of small ones out of the
-    // subnormal numbers; bf16: three (24 bits).  The products that they cost are hidden behind HBM.
-    constexpr int NP = F32 ? 1 : BF16 ? 3 : 2;
-    constexpr float SHIFT = DT == EL_F16 ? 12.f : 0.f;
+    // P in 16 bits: parts that add up to it.  fp16: times 2^15, which keeps the low parts of small ones out of the subnormal numbers (what is lost
+    // there is 2^-40 of the largest at most).
+    constexpr float PARTS = DT == EL_F16 ? 32768.f : 1.f;
     extern __shared__ __attribute__((aligned(1024))) char shared[];  // [wavefront] ring of tiles; then [wavefront] page numbers of NS tiles
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
             for (int x = 0; x < NA; ++x)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[rg][x][e] = __builtin_amdgcn_exp2f((p[rg][x][e] - ref) * unit + SHIFT);
+                    p[rg][x][e] = __builtin_amdgcn_exp2f((p[rg][x][e] - ref) * unit);
                     l[rg] += p[rg][x][e];
                 }
         }
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
             for (int rg = 0; rg < RG; ++rg)
 #pragma unroll
                 for (int y = 0; y < 2 * NA; ++y) {
-                    float u = p[rg][y >> 1][2 * (y & 1)], v = p[rg][y >> 1][2 * (y & 1) + 1];
+                    float u = p[rg][y >> 1][2 * (y & 1)] * PARTS, v = p[rg][y >> 1][2 * (y & 1) + 1] * PARTS;
 #pragma unroll
                     for (int k = 0; k < NP; ++k) {
                         if constexpr (BF16) {
@@ -554,9 +554,9 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
         const int64_t out_row = (b * a.beam + r / a.group) * a.heads + kvh * a.group + r % a.group;
         if (g == 0 && w == 0) {
             if (!whole) a.part_ml[slot + rb] = float2{M, L};
-            else if (a.lse) a.lse[out_row] = empty ? -INFINITY : fmaf(M, a.natural, (__builtin_amdgcn_logf(L) - SHIFT) * kLn2);
+            else if (a.lse) a.lse[out_row] = empty ? -INFINITY : fmaf(M, a.natural, __builtin_amdgcn_logf(L) * kLn2);
         }
-        const float inv = whole ? 1.f / L : 1.f;
+        const float inv = (whole ? 1.f / L : 1.f) * (1.f / PARTS);
 #pragma unroll
         for (int t = 0; t < DT16; ++t) {
             const int col = 16 * t + 4 * g;
@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
 // Joins the pieces of a sequence that was cut: PER wavefronts a (sequence, query row, head), 4 / PER of those a workgroup.  Bound by
 // latency, so the first weighted sums are requested together with the statistics.
 template <int PER>
-__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int tile, float shift)
+__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int tile)
 {
     __shared__ float red[PER == 1 ? 1 : 8];
     __shared__ f4 sums[PER == 1 ? 1 : 256];
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int til
         L = (red[4] + red[5]) + (red[6] + red[7]);
     }
     const bool empty = M == -INFINITY && !(L != L);
-    if (tid == 0 && a.lse) a.lse[row] = empty ? -INFINITY : fmaf(M, a.natural, (__builtin_amdgcn_logf(L) - shift) * kLn2);
+    if (tid == 0 && a.lse) a.lse[row] = empty ? -INFINITY : fmaf(M, a.natural, __builtin_amdgcn_logf(L) * kLn2);
     f4 o{0.f, 0.f, 0.f, 0.f};
     auto add = [&](const f4 &v, float f) __attribute__((always_inline)) {
 #pragma unroll
@@ -732,7 +732,14 @@ AttendPlan plan_attend(const el_attn_pages &c, int heads, int B, int beam, int n
 void launch_attend(const AttendArgs &a, const AttendPlan &p, int dtype, hipStream_t s)
 {
     const dim3 grid((unsigned)p.grid);
-    with_form(dtype, p.padded, p.row_groups, [&](auto f) { hipLaunchKernelGGL(k_attend<decltype(f)>, grid, dim3(64 * p.waves), p.lds, s, a); });
+    with_form(dtype, p.padded, p.row_groups, [&](auto f) {
+        using F = decltype(f);
+        // Parts of a probability in 16 bits: three hold its 24 bits, the products that they cost are mostly hidden behind HBM.  Two fp16 ones hold
+        // 22, which a result in fp16 does not see: 16 sequences of 1000 to 4096, 32 rows on each of 4 key heads of 256, 61 us with two, 63 with three.
+        if constexpr (F::F32) hipLaunchKernelGGL((k_attend<F, 1>), grid, dim3(64 * p.waves), p.lds, s, a);
+        else if (F::BF16 || a.out_dtype == EL_F32) hipLaunchKernelGGL((k_attend<F, 3>), grid, dim3(64 * p.waves), p.lds, s, a);
+        else if constexpr (!F::BF16) hipLaunchKernelGGL((k_attend<F, 2>), grid, dim3(64 * p.waves), p.lds, s, a);
+    });
 }
 
 bool finite_non_negative(float x) { return x >= 0.f && x < INFINITY; }
@@ -803,10 +810,9 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
     if (p.spans) {
         // four wavefronts a row where sequences are cut into many pieces
-        const float shift = cache->dtype == EL_F16 ? 12.f : 0.f;
         const int64_t all = rows * heads;
-        if (p.spans > kManyPieces * B) hipLaunchKernelGGL(k_attend_join<4>, dim3((unsigned)all), dim3(256), 0, s, a, p.tile, shift);
-        else hipLaunchKernelGGL(k_attend_join<1>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, p.tile, shift);
+        if (p.spans > kManyPieces * B) hipLaunchKernelGGL(k_attend_join<4>, dim3((unsigned)all), dim3(256), 0, s, a, p.tile);
+        else hipLaunchKernelGGL(k_attend_join<1>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, p.tile);
         if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;
     }
     return EL_OK;

@@ -60,3 +60,36 @@ def test_scores_far_from_zero_keep_their_distances(dtype, scale, side):
     c.K[..., 1] = np.where(np.isnan(c.K[..., 1]), np.nan, 32.0 * side + g.integers(0, 2, c.K.shape[:3]))
     _put(c)
     _compare(f"far scores {dtype} scale {scale} side {side}", c, 3 * 16 * scale, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("scale", [0.1, 0.013])
+def test_log_sum_exp_of_one_position_is_its_score(dtype, scale):
+    """2 u of the score, and what the exponential and the logarithm of nearly 1 are off by: 2 u each, and 2 u for their product with ln 2."""
+    c = _whole_numbers(dtype, [1] * 60, heads=8)
+    _put(c)
+    _, lse = c.cache.attend_segment(c.q_d, c.table_d, c.lengths_d, scale=scale)
+    _, ref, _ = oracle.paged_attend_reference(c.K, c.V, c.table, c.lengths, c.q, scale=float(np.float32(scale)))
+    err = float((np.abs(_host(lse).reshape(ref.shape) - ref) / (2 * U * np.abs(ref) + 6 * U)).max())
+    record(f"lse of one position {dtype} scale {scale}: {err:.3f} of the bound")
+    assert err <= 1
+
+
+def test_small_probabilities_in_fp16():
+    """One position holds nearly all, with a value of 0; what the others, 2^-26 to 2^-31 of it each, add up to is the output."""
+    c = _whole_numbers("f16", [33, 64, 40, 57, 48, 64] * 10)
+    c.V = np.abs(c.V)
+    n = np.asarray(c.lengths)
+    c.q[:] = 1.0
+    c.K[:] = np.where(np.isnan(c.K), c.K, 0.0)
+    g = np.random.default_rng(97)
+    low = g.integers(180, 215, (60, 4))                              # a tenth of each: 18 to 21.4 in natural units
+    for b in range(60):
+        for t in range(n[b]):
+            page, at = int(c.table[b, t // 16]), t % 16
+            c.K[page, at, :, 0] = 0 if t == n[b] // 2 else -low[b]
+            if t == n[b] // 2:
+                c.V[page, at] = 0
+    _put(c)
+    every = np.stack([c.V[c.table[b, :-(-n[b] // 16)]].reshape(-1, 4, 64)[:n[b]].sum(0) for b in range(60)])[:, None]
+    _compare("small probabilities f16", c, 21.5, 0.1, largest_only=2.0 ** -40 * every)
