@@ -427,8 +427,10 @@ typedef struct {
  *
  * With out_dtype EL_F32, (out, lse) is a segment as el_attn_decode_segment returns it, and el_attn_merge_segments joins
  * it with segments over hidden states.  A row with no position (length 0, all pages absent, every score -inf) has output 0
- * and lse -inf.  Storage behind a length or outside a window is never read into a result, whatever it holds.  A NaN score
- * makes its row NaN, an infinite or NaN value of a position that takes part its column (infinite or NaN).
+ * and lse -inf.  Storage behind a length or outside a window is never read into a result, whatever it holds.  A NaN score, or one
+ * of +inf, makes its row NaN.  An infinite or NaN value of a position that is there makes its column infinite or NaN, in every row of the
+ * sequence that has a score above -inf, and whether the position's own probability is 0 (a score of -inf, or far below the largest) or not:
+ * what a mask must hide is hidden by the length, the window or the table, not by a key of -inf.
  *
  * Accumulations and softmax statistics are fp32.  The result does not depend on what else runs, and is the same on
  * every call.  `workspace`: el_attn_paged_workspace_bytes of device memory, 16-byte aligned, used by this call only, any

@@ -4,6 +4,8 @@ import numpy as np
 import pytest
 
 import oracle
+from paper_2105_04779_amd import workloads as wl
+from helpers import to_device
 from test_paged_gpu import Case, _host
 
 pytestmark = pytest.mark.gpu
@@ -72,6 +74,38 @@ def test_an_output_that_asks_for_a_gradient_is_refused():
     with torch.no_grad():
         assert c.cache.attend(c.q_d, c.table_d, c.lengths_d, out=out) is out
     assert torch.equal(out.detach(), c.cache.attend(c.q_d, c.table_d, c.lengths_d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("B,n", [(3, 50), (3, 3000)])
+def test_values_that_are_not_finite_stay_in_their_column(dtype, B, n):
+    """A position that is there passes an infinite or NaN value on to its column, its probability 0 or not (a score of -inf, or one
+    that underflows); other columns and other sequences know nothing of it.  A row whose scores are all -inf is 0.  n: a sequence
+    taken whole, and cut ones."""
+    c = Case(93, dtype, B, 2, 4, 2, 64, 16, [n, n, n - 3])
+    c.q = wl.round_to_storage(np.minimum(np.abs(c.q) + np.float32(0.5), np.float32(4.0)), dtype)
+    c.q_d = to_device(c.q, dtype)
+    K, V = c.cache.K, c.cache.V
+    last = int(c.table[0, (n - 1) // 16])                            # the first sequence's newest position, and its very first
+    K[last, (n - 1) % 16] = -float("inf")
+    c.K[last, (n - 1) % 16] = -np.inf
+    V[last, (n - 1) % 16, :, 5] = float("inf")
+    V[int(c.table[0, 0]), 0, :, 17] = float("nan")
+    K[int(c.table[0, 1]), 2], c.K[int(c.table[0, 1]), 2] = -300.0, -300.0        # scores hundreds below the rest
+    V[int(c.table[0, 1]), 2, :, 40] = -float("inf")
+    for page in c.table[1]:                                          # the second sequence: no score above -inf, no finite value
+        K[int(page)], V[int(page)] = -float("inf"), float("nan")
+        c.K[int(page)] = -np.inf
+        c.V[int(page)] = 0
+    ref, ref_lse, _ = oracle.paged_attend_reference(c.K, c.V, c.table, c.lengths, c.q, scale=0.125)
+    A, lse = c.cache.attend_segment(c.q_d, c.table_d, c.lengths_d)
+    A, lse = _host(A).reshape(ref.shape), _host(lse).reshape(ref_lse.shape)
+    hit = np.zeros(ref.shape, bool)
+    hit[0][..., [5, 17, 40]] = True
+    assert not np.isfinite(A[hit]).any()
+    assert not A[1].any() and np.isneginf(lse[1]).all()
+    assert np.abs(A - ref)[~hit].max() < 1e-4 * np.abs(ref).max()
+    assert np.abs(lse[[0, 2]] - ref_lse[[0, 2]]).max() < 1e-4 * np.abs(ref_lse[[0, 2]]).max()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
