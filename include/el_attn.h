@@ -391,8 +391,13 @@ el_status el_attn_check_inputs(el_dtype dtype, int32_t d_model,
  * outside [0, pages) names no page: its positions are neither read nor written and take no part in a softmax.
  *
  * Limits (UNSUPPORTED beyond): d_head <= 256, d_head a multiple of 16 bytes of elements.  Alignment (INVALID_ARG): K, V and
- * every stride in bytes a multiple of 16; int32 and fp32 operands to 4 bytes.  Strides must not let two elements overlap.
+ * every stride in bytes a multiple of 16; int32 and fp32 operands to 4 bytes.  Strides must not let two elements overlap, and are at most 2^44
+ * elements, 2^40 of a table; a pool spans at most 2^48 bytes.
+ * What a call writes (outputs, workspace, the pool's own positions in append and copy) is no part of anything else that it reads or writes.
  * An argument error is found before any HIP call.
+ *
+ * The attention has one new token per query row: all `beam` queries of a sequence see the same positions.  There is no causal form for
+ * several new tokens of one sequence (a prompt that append has written is attended to by the tokens after it).
  */
 typedef struct {
     void *K, *V;              /* device, `dtype`                                                    */
@@ -426,7 +431,8 @@ typedef struct {
  *   n        the largest length: at most table_pages * page_size
  *
  * With out_dtype EL_F32, (out, lse) is a segment as el_attn_decode_segment returns it, and el_attn_merge_segments joins
- * it with segments over hidden states.  A row with no position (length 0, all pages absent, every score -inf) has output 0
+ * it with segments over hidden states.  Those know neither cap, window nor slopes, and their scale is d_head^(-1/2): the joint softmax of the two is one
+ * of a single rule only where this one is plain too.  A row with no position (length 0, all pages absent, every score -inf) has output 0
  * and lse -inf.  Storage behind a length or outside a window is never read into a result, whatever it holds.  A NaN score, or one
  * of +inf, makes its row NaN.  An infinite or NaN value of a position that is there makes its column infinite or NaN, in every row of the
  * sequence that has a score above -inf, and whether the position's own probability is 0 (a score of -inf, or far below the largest) or not:
@@ -455,8 +461,8 @@ el_status el_attn_paged_attend(const el_attn_pages *cache,
  *   counts        [B] int32 device, each in [0, T] (a value outside is taken as the nearer end), or NULL: T
  *
  * A token whose position is negative, or lies behind the table or in a page outside the pool, is dropped.  Where two
- * sequences write the same position of the same page, either may win.
- * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * tokens have the same position of the same page, each 16 bytes there are of one or the other.
+ * Errors: INVALID_ARG (also B beyond 65535, T beyond 2^23, a token of 32 GB or more), UNSUPPORTED, HIP.
  */
 el_status el_attn_paged_append(const el_attn_pages *cache,
                                const int32_t *table, int64_t table_stride, int32_t table_pages,
@@ -473,7 +479,7 @@ el_status el_attn_paged_append(const el_attn_pages *cache,
  *
  * A page may be the source of several pairs.  The caller sees to it that no page is the destination of two pairs, or the
  * destination of one and the source of another.  Positions at or behind a count stay as they were.
- * Errors: INVALID_ARG, UNSUPPORTED (also a page of 32 GB or more), HIP.
+ * Errors: INVALID_ARG (also pairs beyond 2^23), UNSUPPORTED (also a page of 32 GB or more), HIP.
  */
 el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_t *src, const int32_t *dst, const int32_t *counts,
                              int32_t pairs, void *stream);

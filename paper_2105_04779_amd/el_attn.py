@@ -431,7 +431,7 @@ _INT32_MAX = 2 ** 31 - 1
 
 class PagedCache:
     """Projected keys and values of one attention layer, in pages (see el_attn_pages): new tokens in, attention of one token
-    per query row out, pages copied for beams that fork.
+    per query row out (no causal form for several new tokens of a sequence), pages copied for beams that fork.
 
     K, V: device tensors [pages, page_size, kv_heads, d_head], the last dimension contiguous, with the same strides (a
     transposed view of [pages, kv_heads, page_size, d_head] is as good).  The table [B, columns] int32 and the lengths
@@ -481,7 +481,7 @@ class PagedCache:
 
     def append(self, k, v, table, lengths, counts=None):
         """New tokens k, v [B, T, kv_heads, d_head] (heads of a token contiguous, other strides free, the same for both) to
-        the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already."""
+        the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already.  B up to 65535."""
         shape, strides, device = k.shape, k.stride(), self.device
         if len(shape) != 4 or shape != v.shape or shape[2] != self.kv_heads or shape[3] != self.d_head:
             raise ValueError(f"k and v must be [B, T, {self.kv_heads}, {self.d_head}]")
@@ -552,7 +552,8 @@ class PagedCache:
 
     def attend_segment(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None):
         """The same as a segment (seg_A [B*beam, heads*d_head], seg_lse [B*beam, heads], float32) for
-        ElAttention.merge_segments."""
+        ElAttention.merge_segments.  decode_segment has no cap, window or slopes, and the scale d_k ** -0.5: joined with one of its segments, neither may
+        this one."""
         torch = self._torch
         self._check_queries(queries)
         B, beam, heads, d = queries.shape
