@@ -171,8 +171,10 @@ __device__ __forceinline__ unsigned kth_of(const unsigned (&mine)[COUNT], int k)
 }
 
 // A chunk of up to NV pieces a lane of one row; LANES 1024: the whole row.  Grid: rows x chunks.
+// With 1024 lanes a compute unit holds two rows where NV is at most 8 (64 registers; left alone the compiler takes 70), so that one is loaded while the
+// other is computed: 512 rows of 65000 in bf16, 8 alternatives, 19.9 us, 24.6 with one; 1024 of 50265 32.2 / 44.2; 300 of 30000 in fp32 14.2 / 17.1.
 template <typename T, int NV, int LANES>
-__global__ void __launch_bounds__(LANES) k_score_chunk(const ScoreArgs a)
+__global__ void __launch_bounds__(LANES, LANES == kRowLanes && NV <= 8 ? 8 : 1) k_score_chunk(const ScoreArgs a)
 {
     constexpr int N = Piece<T>::N, WAVES = LANES / 64;
     __shared__ unsigned best[256];
@@ -428,15 +430,16 @@ ScorePlan plan_score(int element_size, int32_t rows, int32_t vocab, int32_t k)
     p.form = 16;
     auto chunks = [&](int form) { return (pieces + form * kLanes - 1) / (form * kLanes); };
     // The more a workgroup holds, the fewer lists there are to join: 1024 rows of 128003 in fp32, 20 alternatives, 111 us with 8 pieces a
-    // lane, 96 with 16, which take two rounds of workgroups; 1024 of 50265 in bf16 29 / 26.
+    // lane, 96 with 16, which take two rounds of workgroups.
     // A row that one workgroup holds is not cut, unless rows are few and it has more than 8 pieces a lane: 300 rows of 8000 in bf16, 8 alternatives,
     // 6.6 us, 10.2 cut; of 32001 12.4 / 14.0; 64 rows of 32001 9.5, 8.0 as below.
     const int alone = rows > kRowsWhole ? 16 : 8;
     while (p.form > 1 && (chunks(p.form) > 1 || p.form > alone) && (int64_t)rows * chunks(p.form) < (p.form > 8 ? 2 * kFillWorkgroups : kFillWorkgroups) && chunks(p.form / 2) * k <= kListMax) p.form /= 2;
     p.chunks = chunks(p.form);
     while (p.form > 1 && chunks(p.form / 2) == p.chunks) p.form /= 2;
-    // Rows that 1024 lanes hold: one launch, a row a workgroup.  256 rows of 50265 in bf16, 8 alternatives, 12.8 us, 15.9 cut; 512 18.5 / 21.7;
-    // 300 of 128003, whose registers leave room for one such workgroup a compute unit, 35 / 27.
+    // Rows that 1024 lanes hold: one launch, a row a workgroup.  256 rows of 50265 in bf16, 8 alternatives, 13.1 us, 16.1 cut; 512 18.9 / 21.7;
+    // 1024 32.2 / 32.4, of 33000 29.5 / 27.3, of 20000 in fp32 23.0 / 24.9; 300 of 128003, whose registers leave room for one such workgroup a compute
+    // unit, 35 / 27.
     if (p.chunks > 1 && rows <= (pieces <= 8 * kRowLanes ? 4 * kRowsWhole : kRowsWhole) && pieces <= 16 * kRowLanes) {
         p.lanes = kRowLanes; p.chunks = 1;
         p.form = pieces <= 4 * kRowLanes ? 4 : pieces <= 8 * kRowLanes ? 8 : 16;
