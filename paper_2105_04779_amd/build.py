@@ -21,7 +21,8 @@ HIPCC_FLAGS = [
 ]
 
 
-# kernels that are built around what their wavefronts hold in registers
+# kernels that are built around what their wavefronts hold in registers.  (Vector registers: k_attend's instances keep 60 to 120 scalar ones in lanes of
+# vector registers, two or three of which are read back in the loop over tiles.)
 NO_SPILL_KERNELS = ("k_core_stream", "k_core_short", "k_qelq", "k_vproj", "k_oproj", "k_small_step", "k_gemm_f32",
                     "k_attend", "k_score_chunk")
 

@@ -41,8 +41,8 @@ constexpr int64_t kManyPieces = 16;
 // of 64, 15.5 / 16.5 (16); 300 of up to 1000, two of 128, 45 / 58 (32).
 constexpr int kFew = 4, kFewOfMany = 16;
 // Positions that one wavefront may be left with where the sequences alone fill the device, so that nothing is joined: kShort, and as many for each
-// time that they fill it as kRound bytes of keys have.  us, whole / cut: 16 heads of 64, 160 sequences of up to 700 59 / 62, of 1500 122 / 110; 600 of
-// up to 2000 429 / 497; 8 heads of 128, 160 of up to 1000 86 / 74, 600 of 700 164 / 173.
+// time that they fill it as kRound bytes of keys have.  us, whole / cut: 16 heads of 64, 160 sequences of up to 700 59 / 62, of up to 1500 122 / 110;
+// 600 of up to 2000 429 / 497; 8 heads of 128, 160 of up to 1000 86 / 74, 600 of up to 700 164 / 173.
 constexpr int64_t kRound = 128 << 10;
 constexpr int kShort = 2048;
 // Sequences are never cut where there are more than kCutMost, whose lengths every wavefront would have to add up, and of more than kCutMax only
