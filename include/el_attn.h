@@ -392,7 +392,7 @@ el_status el_attn_check_inputs(el_dtype dtype, int32_t d_model,
  *
  * Limits (UNSUPPORTED beyond): d_head <= 256, d_head a multiple of 16 bytes of elements.  Alignment (INVALID_ARG): K, V and
  * every stride in bytes a multiple of 16; int32 and fp32 operands to 4 bytes.  Strides must not let two elements overlap, and are at most 2^44
- * elements, 2^40 of a table; a pool spans at most 2^48 bytes.
+ * elements, 2^40 of a table; a pool, and the rows of any operand, span at most 2^48 bytes.
  * What a call writes (outputs, workspace, the pool's own positions in append and copy) is no part of anything else that it reads or writes.
  * An argument error is found before any HIP call.
  *

@@ -73,6 +73,8 @@ __device__ __forceinline__ void dma_row_2k_nt(unsigned lds_addr, unsigned voff, 
 
 static inline size_t dtype_size(int dt) { return dt == EL_F32 ? 4 : 2; }
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+// Whether the last of `count` places, `stride` bytes apart, lies further than an address reaches: 2^48.
+static inline bool out_of_reach(int64_t count, int64_t stride) { return count > 1 && stride > ((int64_t)1 << 48) / (count - 1); }
 
 // EL-Q for the MFMA core is stored in the order its score wavefronts load it: 1 KB fragments of 16 rows x 32
 // columns (row-major inside: element (r16, c32) at r16 * 32 + c32), ordered [batch element][row / 16][column / 32]

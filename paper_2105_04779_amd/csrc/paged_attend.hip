@@ -778,7 +778,7 @@ extern "C" el_status el_attn_paged_attend(const el_attn_pages *cache,
     if (!(fabsf(rule->softcap > 0.f ? rule->scale / rule->softcap : rule->scale * kLog2e) < INFINITY)) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)dtype_size(cache->dtype), row = (int64_t)heads * cache->d_head, rows = (int64_t)B * beam;
     if (((uintptr_t)lengths | (uintptr_t)lse | (uintptr_t)rule->slopes) & 3 || ((uintptr_t)queries | (uintptr_t)out) & 15) return EL_ERR_INVALID_ARG;
-    if (query_stride > ((int64_t)1 << 44) || query_stride * es % 16 != 0 || (rows > 1 && query_stride < row)) return EL_ERR_INVALID_ARG;
+    if (query_stride > ((int64_t)1 << 44) || query_stride * es % 16 != 0 || (rows > 1 && query_stride < row) || out_of_reach(rows, query_stride * es)) return EL_ERR_INVALID_ARG;
     // (several wavefronts read a query row, and one that is done writes its part of the output)
     const uintptr_t q0 = (uintptr_t)queries, q1 = q0 + (uintptr_t)((rows > 1 ? (rows - 1) * query_stride : 0) + row) * es;
     const uintptr_t o0 = (uintptr_t)out, o1 = o0 + (uintptr_t)(rows * row) * dtype_size(out_dtype);

@@ -32,7 +32,7 @@ el_status check_pages(const el_attn_pages *c)
 el_status check_table(const int32_t *table, int64_t table_stride, int32_t table_pages, int32_t B)
 {
     if (!table || table_pages < 1 || B < 1 || table_stride < table_pages || table_stride > ((int64_t)1 << 40)) return EL_ERR_INVALID_ARG;
-    if ((uintptr_t)table & 3) return EL_ERR_INVALID_ARG;
+    if ((uintptr_t)table & 3 || out_of_reach(B, table_stride * 4)) return EL_ERR_INVALID_ARG;
     return EL_OK;
 }
 
@@ -135,7 +135,7 @@ extern "C" el_status el_attn_paged_append(const el_attn_pages *cache,
     const int64_t es = (int64_t)el::dtype_size(cache->dtype), most = (int64_t)1 << 44, row = (int64_t)cache->kv_heads * cache->d_head;
     if (token_stride > most || batch_stride > most || token_stride * es % 16 != 0 || batch_stride * es % 16 != 0) return EL_ERR_INVALID_ARG;
     if ((T > 1 && token_stride < row) || (B > 1 && batch_stride < row)) return EL_ERR_INVALID_ARG;
-    if (row * es / 16 > INT32_MAX - 256) return EL_ERR_INVALID_ARG;
+    if (row * es / 16 > INT32_MAX - 256 || el::out_of_reach(T, token_stride * es) || el::out_of_reach(B, batch_stride * es)) return EL_ERR_INVALID_ARG;
     int lanes = 1;
     while (lanes < 128 && lanes < row * es / 16) lanes *= 2;
     const el::AppendArgs a{el::page_view(*cache, table, table_stride, table_pages), lengths, counts, (const char *)K_new, (const char *)V_new,

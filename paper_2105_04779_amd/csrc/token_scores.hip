@@ -501,7 +501,7 @@ extern "C" el_status el_attn_score_tokens(el_dtype dtype, const void *logits, in
     if ((logprob && !tokens) || (k > 0 && (!top_logprob || !top_index))) return EL_ERR_INVALID_ARG;
     if ((rows > 1 && row_stride < vocab) || row_stride > ((int64_t)1 << 44)) return EL_ERR_INVALID_ARG;
     const int64_t es = (int64_t)dtype_size(dtype);
-    if ((uintptr_t)logits % (size_t)es != 0) return EL_ERR_INVALID_ARG;
+    if ((uintptr_t)logits % (size_t)es != 0 || out_of_reach(rows, row_stride * es)) return EL_ERR_INVALID_ARG;
     if (((uintptr_t)tokens | (uintptr_t)logprob | (uintptr_t)entropy | (uintptr_t)top_logprob | (uintptr_t)top_index) & 3) return EL_ERR_INVALID_ARG;
     const ScorePlan p = plan_score((int)es, rows, vocab, k);
     if ((int64_t)rows * p.chunks > kMaxChunks) return EL_ERR_INVALID_ARG;
