@@ -370,8 +370,14 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
             u4 k[QC];
 #pragma unroll
             for (int c = 0; c < QC; ++c) k[c] = *(const EL_LDS(u4) *)(Kt + (16 * x + r16) * ROWB + (((4 * c + g) ^ swizzle<ROWB>(r16)) << 4));
+            // fp32: four sums instead of one of d / 4 instructions, each of which rounds.  The error of a result against fp64 falls from up to 2.3 times
+            // to 1.1 times that of plain fp32 operations.  us, one sum / four: 250 sequences of 100 to 1000, 8 heads of 128 199 / 200, 4 of 256 423 / 413.
+            constexpr int SUMS = F32 ? 4 : 1;
+            f4 part[RG][SUMS];
 #pragma unroll
-            for (int rg = 0; rg < RG; ++rg) s[rg][x] = f4{0.f, 0.f, 0.f, 0.f};
+            for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+                for (int e = 0; e < SUMS; ++e) part[rg][e] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < QC; ++c)
 #pragma unroll
@@ -379,11 +385,20 @@ __global__ void __launch_bounds__(64 * F::WAVES, (F::PER_CU + 3) / 4) k_attend(c
                     if constexpr (F32) {
                         const f4 kf = __builtin_bit_cast(f4, k[c]), qf = __builtin_bit_cast(f4, q[rg][c]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[rg][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], s[rg][x], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) part[rg][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], part[rg][e], 0, 0, 0);
                     } else {
-                        s[rg][x] = Mma<BF16>::s16(k[c], q[rg][c], s[rg][x]);
+                        part[rg][0] = Mma<BF16>::s16(k[c], q[rg][c], part[rg][0]);
                     }
                 }
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg) {
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[rg][x][e] = (part[rg][0][e] + part[rg][1][e]) + (part[rg][2][e] + part[rg][3][e]);
+                } else {
+                    s[rg][x] = part[rg][0];
+                }
+            }
         }
         // ---- softmax: lane (g, r16) holds positions 16 x + 4 g + e of row r16 ----
         // (the largest score is taken from the others before they become powers of two: what scores have in common takes no digits from their

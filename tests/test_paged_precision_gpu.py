@@ -93,3 +93,21 @@ def test_small_probabilities_in_fp16():
     _put(c)
     every = np.stack([c.V[c.table[b, :-(-n[b] // 16)]].reshape(-1, 4, 64)[:n[b]].sum(0) for b in range(60)])[:, None]
     _compare("small probabilities f16", c, 21.5, 0.1, largest_only=2.0 ** -40 * every)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_products_of_fp32_are_summed_in_four_parts(d):
+    """One product of 2^24 and d - 1 of a quarter.  An instruction adds four products to one of four sums; at 2^24, where fp32 has steps of 2, it may lose
+    all of the 1 that it adds.  One of the sums holds the large product: d / 16 instructions.  Joining the sums rounds three times by 1 at most, the
+    log-sum-exp of the one position by 2 (2 u of 2^24).  (One sum of all would lose d / 4 - 1.)"""
+    c = Case(99, "f32", 5, 1, 4, 4, d, 16, [1, 1, 1, 1, 1])
+    c.q[:] = 0.5
+    c.K[:] = np.where(np.isnan(c.K), c.K, 0.5)
+    for b in range(5):                                               # the large one in another place for each
+        c.q[b, ..., 3 * b], c.K[c.table[b, 0], 0, :, 3 * b] = 4096.0, 4096.0
+    _put(c)
+    out, lse = c.cache.attend_segment(c.q_d, c.table_d, c.lengths_d, scale=1.0)
+    err = np.abs(_host(lse).astype(np.float64) - (2.0 ** 24 + (d - 1) / 4)).max()
+    record(f"products of fp32 d {d}: {err:.1f} of {d / 16 + 5:.1f}")
+    assert err <= d / 16 + 5
+    assert np.array_equal(_host(out).reshape(5, 4, d), np.stack([c.V[c.table[b, 0], 0] for b in range(5)]))
