@@ -515,6 +515,140 @@ el_status el_attn_score_tokens(el_dtype dtype, const void *logits, int64_t row_s
                                int32_t k, float *top_logprob, int32_t *top_index,
                                void *workspace, size_t workspace_bytes, void *stream);
 
+/* ==== The paged cache in 8 bits ====================================================================================
+ *
+ * The same pool of pages with keys and values as 8-bit codes, and a scale in fp32 for every `block` positions of a page and head: a value is
+ * code times scale.  Half the memory of 16-bit storage, and half the bytes that an attention reads.
+ *
+ *   EL_E4M3   floating-point codes (4 bits of exponent, 3 of mantissa, the largest 448, no infinities): relative rounding of 2^-4 whatever the size
+ *   EL_INT8   whole numbers from -127 to 127: absolute rounding of half a scale
+ *
+ * Strides in elements, which are bytes here: the same rules as el_attn_pages (multiples of 16, no overlaps, up to 2^44).  Scales [pages, kv_heads,
+ * page_size / block], contiguous, 4-byte aligned; positive where a position of the block is in use.  Queries, new tokens and outputs are EL_F32, EL_F16 or EL_BF16,
+ * which each call is told.
+ * Limits (UNSUPPORTED beyond): d_head a multiple of 16, at most 256; page_size at most 65536.  block divides page_size (INVALID_ARG otherwise).
+ */
+typedef enum { EL_E4M3 = 1, EL_INT8 = 2 } el_format8;
+
+typedef struct {
+    void *K, *V;              /* device, codes                                                      */
+    float *K_scale, *V_scale; /* device                                                             */
+    int64_t page_stride;
+    int64_t position_stride;
+    int64_t head_stride;
+    int32_t pages, page_size; /* >= 1                                                               */
+    int32_t kv_heads, d_head;
+    int32_t block;            /* positions that share a scale                                       */
+    int32_t format;           /* el_format8                                                         */
+} el_attn_pages8;
+
+/*
+ * Attention of one new token per query row over the sequence's pages: el_attn_paged_attend with K and V the values that codes and scales stand for, and
+ * everything said there (lengths, rule, out, lse, empty rows, NaN, workspace, errors) the same.  `dtype`: of the queries; `out_dtype`: EL_F32 or `dtype`.
+ * Queries are taken with all their bits; probabilities as bf16 numbers that add up to 16 bits, 24 for a result in fp32.
+ */
+size_t el_attn_quantized_workspace_bytes(const el_attn_pages8 *cache, int32_t dtype, int32_t out_dtype, int32_t heads, int32_t B, int32_t beam, int32_t n);
+el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32_t dtype,
+                                const int32_t *table, int64_t table_stride, int32_t table_pages, const int32_t *lengths,
+                                const void *queries, int64_t query_stride, int32_t heads, const el_attn_score_rule *rule,
+                                void *out, int32_t out_dtype, float *lse, int32_t B, int32_t beam, int32_t n,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * New tokens into the pages, as el_attn_paged_append; `dtype`: theirs.  For every block of positions and head that receives one, K and V each apart,
+ * with fl a rounding to fp32 and `most` the largest code:
+ *
+ *   needed = max(fl(largest |x| of the new tokens, finite ones only, times fl(1 / most)), 2^-126)
+ *   scale  = needed, where the sequence has no earlier position in the block (what the block held before is forgotten);
+ *            otherwise the block's own, unless that is below needed: then needed, and the earlier positions' codes are rounded again,
+ *            code = nearest(fl(fl(code * old scale) * fl(1 / scale)))
+ *   code   = nearest(fl(x * fl(1 / scale))) of every new token, ties to the even code, beyond the largest the largest (an infinity too); a NaN is
+ *            NaN in EL_E4M3, 0 in EL_INT8
+ *
+ * A scale never shrinks while its block fills, so a token's codes do not depend on how many calls brought the block, except for what is rounded again.
+ * Earlier positions are those below lengths[b] - counts[b].  Two sequences of one call must not write into the same block: its scale and the codes of both
+ * would be lost (copy a shared page first).
+ * Errors: as el_attn_paged_append, UNSUPPORTED also for sizes whose grid passes 2^31 workgroups.
+ */
+el_status el_attn_quantized_append(const el_attn_pages8 *cache, int32_t dtype,
+                                const int32_t *table, int64_t table_stride, int32_t table_pages,
+                                const int32_t *lengths, const int32_t *counts,
+                                const void *K_new, const void *V_new, int64_t batch_stride, int64_t token_stride,
+                                int32_t B, int32_t T, void *stream);
+
+/* Copies of pages, as el_attn_paged_copy: codes of positions [0, counts[i]), and the scales of the blocks that these begin or fill. */
+el_status el_attn_quantized_copy(const el_attn_pages8 *cache, const int32_t *src, const int32_t *dst, const int32_t *counts,
+                              int32_t pairs, void *stream);
+
+/* ==== The table of the next step ===================================================================================
+ *
+ * From what every sequence holds and how many positions it needs: the next table, on the device.  Nothing is kept between calls: a page is in use if an
+ * entry of the new sequences names it (below their lengths) or `reserved` does; every other one is free.  So a sequence that ends gives its pages
+ * back by not being named as a parent, and a beam that forks shares its parent's pages until one of the two writes.
+ *
+ *   table     [B_old, columns] int32, rows table_stride apart; lengths [B_old] int32 (outside [0, columns * page_size]: the nearer end)
+ *   parents   [B] int32: new sequence b goes on from old sequence parents[b]; outside [0, B_old): a new one of length 0.  NULL: itself (B <= B_old)
+ *   counts    [B] int32: positions that b needs beyond its length, each in [0, T] (outside: the nearer end), or NULL: T
+ *   reserved  [pages] uint8, nonzero: in use by others; or NULL
+ *
+ *   new_table   [B, columns] contiguous: the parent's entries, with the changes below; -1 behind the last page and for entries outside the pool
+ *   new_lengths [B]: with the positions granted
+ *   granted     [B]: positions granted: all that were asked for, or 0
+ *   slots       [B, T] int64 or NULL: page * page_size + place of each position granted, -1 for the others
+ *   copies      [3, B]: source page, destination page and positions of the copy that b needs before it writes; (-1, -1, 0) for none.
+ *               As they are, the operands of el_attn_paged_copy and el_attn_quantized_copy
+ *   free_pages  [1]: pages left
+ *
+ * A sequence that writes into a partly filled page (its length no multiple of page_size) keeps it if no other sequence holds more positions of it, none of a lower
+ * number that writes too holds as many, and it is not reserved; otherwise it gets a page of its own, and a copy.  An absent page that it writes into is
+ * replaced without one.  Free pages are handed out from the lowest number up, sequences in order; the first that the free pages do not suffice for, and every later one
+ * that needs a page, get nothing; so does one whose positions the columns do not hold, without changing what the others get.
+ * `workspace`: el_attn_plan_workspace_bytes, 16-byte aligned, any contents, used by this call only.
+ * What is written must not overlap what is read.  Errors: INVALID_ARG (null or misaligned operands, sizes < 1, B or B_old beyond 2^20, B beyond B_old without
+ * parents, pages beyond 2^24, T beyond 2^23, columns beyond 2^24, B * columns beyond 2^31, columns * page_size beyond 2^31 - 1), WORKSPACE, HIP.
+ */
+size_t el_attn_plan_workspace_bytes(int32_t B, int32_t pages);
+el_status el_attn_plan_pages(const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
+                             const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size, int32_t B, int32_t T,
+                             int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots, int32_t *copies, int32_t *free_pages,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* ==== Sampling =====================================================================================================
+ *
+ * The next token of every row of logits x, drawn by a given random number from what filters leave:
+ *
+ *   weight  w_v = exp((x_v - max x) / temperature)
+ *   order   larger logits first, of equal ones the lowest index
+ *   top_k   the first k in this order
+ *   top_p   of these the shortest beginning whose weights reach top_p times their sum
+ *   min_p   of these those with w_v >= min_p (relative to the largest); the first in order always stays
+ *   token   the first index v, in the order of the vocabulary, at which the sum of the weights left passes uniform times their total
+ *   logprob log(w_token / total)
+ *
+ *   logits   as for el_attn_score_tokens: any row alignment, vocab up to 2^19
+ *   uniform  [rows] float32, in [0, 1); below: the first token left; 1 or more, or NaN: the last
+ *   tokens   [rows] int32;  logprob [rows] float32 or NULL
+ *
+ * A filter's setting is a number, or a device array with one for every row.  Off: top_k <= 0, top_p >= 1, min_p <= 0, NaN.  A temperature of 0 (or below, or NaN)
+ * takes the first in order, with logprob 0.  A logit of -inf is never taken.  A row without any that may be: token -1, logprob -inf.  NaN or +inf in a row: -1 and NaN.
+ * Weights are 64-bit whole numbers, multiples of 2^-43 of the largest weight (a token below half of that has weight 0), so sums are exact and do not depend on an order.
+ * `workspace`: el_attn_sample_workspace_bytes, NULL where that is 0.
+ * Errors: INVALID_ARG (null or misaligned operands, sizes < 1, rows beyond 2^23, row_stride, a temperature that is negative, infinite or NaN), UNSUPPORTED, WORKSPACE, HIP.
+ */
+typedef struct {
+    float temperature;        /* used where the array beside it is NULL                             */
+    int32_t top_k;
+    float top_p, min_p;
+    const float *row_temperature;
+    const int32_t *row_top_k;
+    const float *row_top_p, *row_min_p;
+} el_attn_sample_rule;
+
+size_t el_attn_sample_workspace_bytes(el_dtype dtype, int32_t rows, int32_t vocab);
+el_status el_attn_sample_tokens(el_dtype dtype, const void *logits, int64_t row_stride, int32_t rows, int32_t vocab, const float *uniform,
+                                const el_attn_sample_rule *rule, int32_t *tokens, float *logprob,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
 /* Release the context and its packed weights (not the workspace, which the caller owns). */
 el_status el_attn_destroy(el_attn_ctx *ctx);
 

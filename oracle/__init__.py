@@ -15,6 +15,9 @@ module compiles it with gcc on first use and marshals numpy arrays to it.
 ``check_inputs_reference``  what a decode step assumes about its inputs, counted by definition.
 ``paged_attend_reference``, ``paged_append_reference``, ``paged_copy_reference``  attention of one new token over pages
                    of projected keys and values, and what moves them, position by position.
+``quantized_append_reference``, ``quantized_copy_reference``, ``quantized_values``, ``nearest_codes``  the paged cache in 8 bits.
+``plan_pages_reference``  the table of the next step, one sequence after the other.
+``sample_tokens_reference``  the token that a random number draws from what the filters leave, and how close that was.
 ``score_tokens_reference``  log-probability, entropy and best alternatives of rows of logits, by definition.
 ``gather_batch_reference``  the state gather between decode steps (section 3.1.1's
                    state, re-ordered / compacted by the search), by its definition.
@@ -342,3 +345,187 @@ def score_tokens_reference(logits, tokens, k):
         for i, v in enumerate(which[np.argsort(-x[which], kind="stable")[:k]]):
             top_logprob[r, i], top_index[r, i] = (x[v] - m) - log_S, v
     return logprob, entropy, top_logprob, top_index, away
+
+
+# ---- the paged cache in 8 bits -------------------------------------------------------------------------------------------
+LARGEST_CODE = {"e4m3": 448.0, "int8": 127.0}
+
+
+def e4m3_values():
+    """The 256 values of an e4m3 code, from its bits: sign, 4 bits of exponent (bias 7), 3 of mantissa; no infinities, all ones is NaN."""
+    values = np.zeros(256)
+    for code in range(256):
+        exponent, mantissa = code >> 3 & 15, code & 7
+        size = (8 + mantissa) * 2.0 ** (exponent - 10) if exponent else mantissa * 2.0 ** -9
+        values[code] = np.nan if exponent == 15 and mantissa == 7 else size
+        if code & 128:
+            values[code] = -values[code]
+    return values
+
+
+def quantized_values(codes, fmt):
+    """Codes (uint8 bits of e4m3, or int8) as numbers."""
+    return codes.astype(np.float64) if fmt == "int8" else e4m3_values()[codes]
+
+
+def nearest_codes(y, fmt):
+    """The code nearest to each y, of two the even one; beyond the largest, the largest; NaN: NaN, or 0 among whole numbers."""
+    y = np.asarray(y, dtype=np.float64)
+    if fmt == "int8":
+        return np.where(np.isnan(y), 0, np.rint(np.clip(y, -127, 127))).astype(np.int8)
+    size, x = e4m3_values()[:127], np.minimum(np.abs(np.nan_to_num(y, nan=0.0, posinf=448.0, neginf=-448.0)), 448.0)
+    above = np.clip(np.searchsorted(size, x), 1, 126)                          # size[above - 1] < x <= size[above], x = 0 apart
+    below = above - 1
+    down, up = x - size[below], size[above] - x
+    code = np.where(down < up, below, np.where(up < down, above, np.where(below % 2 == 0, below, above)))
+    return np.where(np.isnan(y), 127, code | np.where(np.signbit(y), 128, 0)).astype(np.uint8)
+
+
+def quantized_append_reference(codes, scale, table, lengths, counts, new, block, fmt):
+    """(codes, scale) with token i < counts[b] of new [B, T, kv_heads, d] (float32 values) at position lengths[b] - counts[b] + i, block by block, in the
+    fp32 arithmetic of the definition.  codes [pages, page_size, kv_heads, d], scale [pages, kv_heads, page_size // block] float32."""
+    codes, scale = codes.copy(), scale.copy()
+    pages, page_size, kv_heads, _ = codes.shape
+    f = np.float32
+    inverse_largest = f(1.0 / LARGEST_CODE[fmt])
+    B, T = new.shape[:2]
+    with np.errstate(all="ignore"):
+        for b in range(B):
+            count = T if counts is None else int(min(max(counts[b], 0), T))
+            start = int(lengths[b]) - count
+            groups = {}
+            for i in range(count):
+                t = start + i
+                if 0 <= t < table.shape[1] * page_size and 0 <= table[b, t // page_size] < pages:
+                    groups.setdefault(t // block, []).append((i, t))
+            for k, tokens in groups.items():
+                base = k * block
+                page, first = int(table[b, base // page_size]), base % page_size
+                had = min(max(start - base, 0), block)
+                for h in range(kv_heads):
+                    x = np.stack([new[b, i, h] for i, _ in tokens]).astype(f)
+                    size = np.abs(x[np.isfinite(x)])
+                    needed = max(f(size.max(initial=f(0))) * inverse_largest, f(2.0 ** -126))
+                    old = scale[page, h, first // block]
+                    now = old if had and not needed > old else needed
+                    inverse = f(1) / f(now)
+                    if had and needed > old:
+                        value = quantized_values(codes[page, first:first + had, h], fmt).astype(f)
+                        codes[page, first:first + had, h] = nearest_codes((value * old) * inverse, fmt)
+                    for (_, t), row in zip(tokens, x):
+                        codes[page, t % page_size, h] = nearest_codes(row * inverse, fmt)
+                    scale[page, h, first // block] = now
+    return codes, scale
+
+
+def quantized_copy_reference(codes, scale, src, dst, counts, block):
+    """(codes, scale) with positions [0, counts[i]) of page dst[i], and the scales of the blocks that they begin or fill, taken from page src[i]."""
+    codes2, scale2 = codes.copy(), scale.copy()
+    pages, page_size = codes.shape[:2]
+    for i in range(len(src)):
+        if 0 <= src[i] < pages and 0 <= dst[i] < pages:
+            c = page_size if counts is None else int(min(max(counts[i], 0), page_size))
+            codes2[dst[i], :c] = codes[src[i], :c]
+            scale2[dst[i], :, :-(-c // block)] = scale[src[i], :, :-(-c // block)]
+    return codes2, scale2
+
+
+# ---- the table of the next step ------------------------------------------------------------------------------------------
+def plan_pages_reference(table, lengths, counts, parents, reserved, pages, page_size, T):
+    """dict of table, lengths, granted, slots, copies, free, as whole numbers, one sequence after the other."""
+    B_old, columns = table.shape
+    parents = list(range(B_old)) if parents is None else [int(p) for p in parents]
+    B = len(parents)
+    had, rows, asked = [], [], []
+    for b, p in enumerate(parents):
+        there = 0 <= p < B_old
+        n = min(max(int(lengths[p]), 0), columns * page_size) if there else 0
+        held = -(-n // page_size)
+        row = [int(table[p, j]) if j < held and 0 <= table[p, j] < pages else -1 for j in range(columns)] if there else [-1] * columns
+        c = T if counts is None else min(max(int(counts[b]), 0), T)
+        had.append(n)
+        rows.append(row)
+        asked.append(c if n + c <= columns * page_size else 0)
+    users = {}                                                                 # page: (positions used, writes, sequence) of each that names it
+    for b in range(B):
+        held = -(-had[b] // page_size)
+        for j in range(held):
+            if rows[b][j] >= 0:
+                writes = asked[b] > 0 and had[b] % page_size != 0 and j == held - 1
+                users.setdefault(rows[b][j], []).append((min(page_size, had[b] - j * page_size), writes, b))
+    free = [p for p in range(pages) if p not in users and not (reserved is not None and reserved[p])]
+    available, wanted = len(free), 0
+    out = {"table": np.full((B, columns), -1), "lengths": np.zeros(B, int), "granted": np.zeros(B, int), "slots": np.full((B, T), -1),
+           "copies": np.stack([np.full(B, -1), np.full(B, -1), np.zeros(B, int)])}
+    taken = 0
+    for b in range(B):
+        held, then = -(-had[b] // page_size), -(-(had[b] + asked[b]) // page_size)
+        replaced = False
+        if asked[b] > 0 and had[b] % page_size != 0:
+            page = rows[b][held - 1]
+            if page < 0 or (reserved is not None and reserved[page]):
+                replaced = True
+            else:
+                most = max(e for e, _, _ in users[page])
+                keeper = min([s for e, w, s in users[page] if e == most and w], default=None)
+                replaced = keeper != b
+        need = then - held + replaced if asked[b] > 0 else 0
+        wanted += need
+        if need and wanted > available:
+            asked[b] = 0
+        row = list(rows[b])
+        if asked[b] > 0 and need:
+            mine = free[wanted - need:wanted]
+            taken = wanted
+            if replaced:
+                page, own = row[held - 1], mine.pop(0)
+                if page >= 0:
+                    out["copies"][:, b] = page, own, had[b] % page_size
+                row[held - 1] = own
+            row[held:then] = mine
+        out["table"][b] = row
+        out["granted"][b], out["lengths"][b] = asked[b], had[b] + asked[b]
+        for i in range(asked[b]):
+            t = had[b] + i
+            out["slots"][b, i] = row[t // page_size] * page_size + t % page_size
+    out["free"] = available - taken
+    return out
+
+
+# ---- sampling ------------------------------------------------------------------------------------------------------------
+def sample_tokens_reference(logits, uniform, temperature, top_k, top_p, min_p):
+    """(tokens, logprob, margin) of float64 rows with a setting of each row; margin: how far the decisions (which token, where the filters cut) are from going
+    the other way, relative to the sums that decide them."""
+    rows, vocab = logits.shape
+    tokens, logprob, margin = np.full(rows, -1), np.zeros(rows), np.full(rows, np.inf)
+    for r in range(rows):
+        x = logits[r].astype(np.float64)
+        t, k, p, q, u = float(temperature[r]), int(top_k[r]), float(top_p[r]), float(min_p[r]), float(uniform[r])
+        if np.isnan(x).any() or (x == np.inf).any():
+            logprob[r] = np.nan
+            continue
+        order = np.argsort(-x, kind="stable")
+        order = order[x[order] > -np.inf]
+        if len(order) == 0:
+            logprob[r] = -np.inf
+            continue
+        if not t > 0:
+            tokens[r] = order[0]
+            continue
+        w = np.exp((x[order] - x[order[0]]) / t)
+        n = min(k, len(order)) if k > 0 else len(order)
+        before = np.concatenate([[0.0], np.cumsum(w[:n])])
+        if p < 1:
+            margin[r] = min(margin[r], np.abs(before[1:n] - p * before[n]).min(initial=np.inf) / before[n])
+            n = max(1, int((before[:n] < p * before[n]).sum()))
+        if q > 0:
+            margin[r] = min(margin[r], np.abs(w[1:n] / q - 1).min(initial=np.inf))
+            n = max(1, int((w[:n] >= q).sum()))
+        left = np.sort(order[:n])
+        weights = np.exp((x[left] - x[order[0]]) / t)
+        upto = np.cumsum(weights)
+        past = np.nonzero(upto > u * upto[-1])[0]
+        at = int(past[0]) if len(past) else n - 1
+        margin[r] = min(margin[r], np.abs(upto[:-1] / upto[-1] - u).min(initial=np.inf))
+        tokens[r], logprob[r] = left[at], np.log(weights[at] / upto[-1])
+    return tokens, logprob, margin

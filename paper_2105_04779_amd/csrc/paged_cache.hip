@@ -4,29 +4,35 @@
 
 namespace el {
 
-el_status check_pages(const el_attn_pages *c)
+el_status check_layout(const void *K, const void *V, int64_t page_stride, int64_t position_stride, int64_t head_stride,
+                       int32_t pages, int32_t page_size, int32_t kv_heads, int32_t d_head, int64_t es)
 {
-    if (!c || !c->K || !c->V) return EL_ERR_INVALID_ARG;
-    if (c->dtype != EL_F32 && c->dtype != EL_F16 && c->dtype != EL_BF16) return EL_ERR_UNSUPPORTED;
-    if (c->pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->d_head < 1) return EL_ERR_INVALID_ARG;
-    const int64_t es = (int64_t)dtype_size(c->dtype);
-    if (c->d_head > kMaxHeadDim || c->d_head * es % 16 != 0) return EL_ERR_UNSUPPORTED;
+    if (pages < 1 || page_size < 1 || kv_heads < 1 || d_head < 1) return EL_ERR_INVALID_ARG;
+    if (d_head > kMaxHeadDim || d_head * es % 16 != 0) return EL_ERR_UNSUPPORTED;
     // strides: multiples of 16 bytes, and no two elements in one place: each axis steps over all that the smaller steps cover
-    struct Axis { int64_t size, stride; } ax[3] = {{c->pages, c->page_stride}, {c->page_size, c->position_stride}, {c->kv_heads, c->head_stride}};
+    struct Axis { int64_t size, stride; } ax[3] = {{pages, page_stride}, {page_size, position_stride}, {kv_heads, head_stride}};
     for (const Axis &a : ax)
         if (a.stride < 0 || a.stride > ((int64_t)1 << 44) || a.stride * es % 16 != 0) return EL_ERR_INVALID_ARG;
     for (int i = 0; i < 2; ++i)
         for (int j = 0; j < 2 - i; ++j)
             if (ax[j].stride > ax[j + 1].stride) { const Axis t = ax[j]; ax[j] = ax[j + 1]; ax[j + 1] = t; }
-    __int128 extent = c->d_head;
+    __int128 extent = d_head;
     for (const Axis &a : ax) {
         if (a.size == 1) continue;
         if (a.stride < extent) return EL_ERR_INVALID_ARG;
         extent = (__int128)a.stride * (a.size - 1) + extent;
     }
     if (extent * es > ((__int128)1 << 48)) return EL_ERR_INVALID_ARG;
-    if (((uintptr_t)c->K | (uintptr_t)c->V) & 15) return EL_ERR_INVALID_ARG;
+    if (((uintptr_t)K | (uintptr_t)V) & 15) return EL_ERR_INVALID_ARG;
     return EL_OK;
+}
+
+el_status check_pages(const el_attn_pages *c)
+{
+    if (!c || !c->K || !c->V) return EL_ERR_INVALID_ARG;
+    if (c->dtype != EL_F32 && c->dtype != EL_F16 && c->dtype != EL_BF16) return EL_ERR_UNSUPPORTED;
+    return check_layout(c->K, c->V, c->page_stride, c->position_stride, c->head_stride, c->pages, c->page_size, c->kv_heads, c->d_head,
+                        (int64_t)dtype_size(c->dtype));
 }
 
 el_status check_table(const int32_t *table, int64_t table_stride, int32_t table_pages, int32_t B)
@@ -34,6 +40,24 @@ el_status check_table(const int32_t *table, int64_t table_stride, int32_t table_
     if (!table || table_pages < 1 || B < 1 || table_stride < table_pages || table_stride > ((int64_t)1 << 40)) return EL_ERR_INVALID_ARG;
     if ((uintptr_t)table & 3 || out_of_reach(B, table_stride * 4)) return EL_ERR_INVALID_ARG;
     return EL_OK;
+}
+
+el_status check_new_tokens(const int32_t *lengths, const int32_t *counts, const void *K_new, const void *V_new, int64_t batch_stride, int64_t token_stride,
+                           int64_t row, int64_t es, int32_t B, int32_t T)
+{
+    if (!lengths || !K_new || !V_new || T < 1 || T > 1 << 23 || B > 65535) return EL_ERR_INVALID_ARG;        // (grid)
+    if (((uintptr_t)lengths | (uintptr_t)counts) & 3 || ((uintptr_t)K_new | (uintptr_t)V_new) & 15) return EL_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 44;
+    if (token_stride > most || batch_stride > most || token_stride * es % 16 != 0 || batch_stride * es % 16 != 0) return EL_ERR_INVALID_ARG;
+    if ((T > 1 && token_stride < row) || (B > 1 && batch_stride < row)) return EL_ERR_INVALID_ARG;
+    if (row * es / 16 > INT32_MAX - 256 || out_of_reach(T, token_stride * es) || out_of_reach(B, batch_stride * es)) return EL_ERR_INVALID_ARG;
+    return EL_OK;
+}
+
+el_status check_pairs(const int32_t *src, const int32_t *dst, const int32_t *counts, int32_t pairs)
+{
+    if (!src || !dst || pairs < 1 || pairs > 1 << 23) return EL_ERR_INVALID_ARG;
+    return ((uintptr_t)src | (uintptr_t)dst | (uintptr_t)counts) & 3 ? EL_ERR_INVALID_ARG : EL_OK;
 }
 
 PageView page_view(const el_attn_pages &c, const int32_t *table, int64_t table_stride, int table_pages)
@@ -84,11 +108,14 @@ struct CopyArgs {
     const int32_t *src, *dst, *counts;
     unsigned kv_heads, chunks;
     int heads_first;                         // a head's positions lie closer together than a position's heads
+    float *K_scale, *V_scale;                // SCALES: [pages, kv_heads, per], `block` positions each
+    unsigned block, per;
 };
 
 // Grid: (pairs, slices of a page).  Bound by HBM: four pieces of K and of V on their way per lane, stored past the caches: 2048 pages of 64
 // positions, 16 heads of 64 in bf16, half full on average, 114 us for 545 MB = 4.8 TB/s of reads and writes; 512 of 16 positions 7.6 us (8.8 with
 // stores that stay in the caches).
+template <bool SCALES>
 __global__ void __launch_bounds__(256) k_copy(const CopyArgs a)
 {
     const int src = a.src[blockIdx.x], dst = a.dst[blockIdx.x];
@@ -117,9 +144,37 @@ __global__ void __launch_bounds__(256) k_copy(const CopyArgs a)
         for (int j = 0; j < AHEAD; ++j)
             if (at[j] >= 0) { __builtin_nontemporal_store(kk[j], (u4v *)(Kd + at[j])); __builtin_nontemporal_store(vv[j], (u4v *)(Vd + at[j])); }
     }
+    if constexpr (SCALES) {
+        // those of the blocks that the positions begin or fill, by the pair's last slice, which has the fewest pieces
+        if (blockIdx.y != gridDim.y - 1) return;
+        const unsigned used = (count + a.block - 1) / a.block;
+        const int64_t page = (int64_t)a.kv_heads * a.per;
+        for (unsigned k = threadIdx.x; k < used * a.kv_heads; k += 256) {
+            const unsigned h = k / used, at = h * a.per + (k - h * used);
+            a.K_scale[dst * page + at] = a.K_scale[src * page + at];
+            a.V_scale[dst * page + at] = a.V_scale[src * page + at];
+        }
+    }
 }
 
 } // namespace
+
+el_status launch_copy(const PageView &c, const int32_t *src, const int32_t *dst, const int32_t *counts, int32_t pairs, int kv_heads, int head_bytes,
+                      float *K_scale, float *V_scale, int block, void *stream)
+{
+    const int64_t chunks = head_bytes / 16, pieces = (int64_t)c.page_size * kv_heads * chunks;
+    if (pieces > INT32_MAX) return EL_ERR_UNSUPPORTED;
+    const CopyArgs a{c, src, dst, counts, (unsigned)kv_heads, (unsigned)chunks, c.position < c.head, K_scale, V_scale, (unsigned)block,
+                     (unsigned)(block ? c.page_size / block : 0)};
+    // slices of 1024 pieces, most of them a workgroup's only one (2048 of those pages: 125 us with 2048 workgroups, 114 with 16384)
+    const int64_t most = (pieces + 1023) / 1024, want = (32768 + pairs - 1) / pairs;
+    const dim3 grid(pairs, (unsigned)(most < want ? most : want));
+    (void)hipGetLastError();
+    if (block) hipLaunchKernelGGL(k_copy<true>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(k_copy<false>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
+}
+
 } // namespace el
 
 extern "C" el_status el_attn_paged_append(const el_attn_pages *cache,
@@ -130,12 +185,8 @@ extern "C" el_status el_attn_paged_append(const el_attn_pages *cache,
 {
     if (const el_status st = el::check_pages(cache); st != EL_OK) return st;
     if (const el_status st = el::check_table(table, table_stride, table_pages, B); st != EL_OK) return st;
-    if (!lengths || !K_new || !V_new || T < 1 || T > 1 << 23 || B > 65535) return EL_ERR_INVALID_ARG;        // (grid)
-    if (((uintptr_t)lengths | (uintptr_t)counts) & 3 || ((uintptr_t)K_new | (uintptr_t)V_new) & 15) return EL_ERR_INVALID_ARG;
-    const int64_t es = (int64_t)el::dtype_size(cache->dtype), most = (int64_t)1 << 44, row = (int64_t)cache->kv_heads * cache->d_head;
-    if (token_stride > most || batch_stride > most || token_stride * es % 16 != 0 || batch_stride * es % 16 != 0) return EL_ERR_INVALID_ARG;
-    if ((T > 1 && token_stride < row) || (B > 1 && batch_stride < row)) return EL_ERR_INVALID_ARG;
-    if (row * es / 16 > INT32_MAX - 256 || el::out_of_reach(T, token_stride * es) || el::out_of_reach(B, batch_stride * es)) return EL_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)el::dtype_size(cache->dtype), row = (int64_t)cache->kv_heads * cache->d_head;
+    if (const el_status st = el::check_new_tokens(lengths, counts, K_new, V_new, batch_stride, token_stride, row, es, B, T); st != EL_OK) return st;
     int lanes = 1;
     while (lanes < 128 && lanes < row * es / 16) lanes *= 2;
     const el::AppendArgs a{el::page_view(*cache, table, table_stride, table_pages), lengths, counts, (const char *)K_new, (const char *)V_new,
@@ -151,17 +202,7 @@ extern "C" el_status el_attn_paged_copy(const el_attn_pages *cache, const int32_
                                         int32_t pairs, void *stream)
 {
     if (const el_status st = el::check_pages(cache); st != EL_OK) return st;
-    if (!src || !dst || pairs < 1 || pairs > 1 << 23) return EL_ERR_INVALID_ARG;
-    if (((uintptr_t)src | (uintptr_t)dst | (uintptr_t)counts) & 3) return EL_ERR_INVALID_ARG;
-    const int64_t es = (int64_t)el::dtype_size(cache->dtype);
-    const int64_t chunks = cache->d_head * es / 16, pieces = (int64_t)cache->page_size * cache->kv_heads * chunks;
-    if (pieces > INT32_MAX) return EL_ERR_UNSUPPORTED;
-    const el::CopyArgs a{el::page_view(*cache, nullptr, 0, 0), src, dst, counts, (unsigned)cache->kv_heads, (unsigned)chunks,
-                         cache->position_stride < cache->head_stride};
-    // slices of 1024 pieces, most of them a workgroup's only one (2048 of those pages: 125 us with 2048 workgroups, 114 with 16384)
-    const int64_t most = (pieces + 1023) / 1024, want = (32768 + pairs - 1) / pairs;
-    const dim3 grid(pairs, (unsigned)(most < want ? most : want));
-    (void)hipGetLastError();
-    hipLaunchKernelGGL(el::k_copy, grid, dim3(256), 0, (hipStream_t)stream, a);
-    return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
+    if (const el_status st = el::check_pairs(src, dst, counts, pairs); st != EL_OK) return st;
+    return el::launch_copy(el::page_view(*cache, nullptr, 0, 0), src, dst, counts, pairs, cache->kv_heads, (int)(cache->d_head * el::dtype_size(cache->dtype)),
+                           nullptr, nullptr, 0, stream);
 }

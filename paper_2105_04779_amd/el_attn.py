@@ -6,6 +6,7 @@ library has not been built -- there is no CPU fallback.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -14,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libelattn.so")
 
 EL_OK, EL_ERR_INVALID_ARG, EL_ERR_UNSUPPORTED, EL_ERR_ALLOC, EL_ERR_HIP, EL_ERR_WORKSPACE = range(6)
 EL_F32, EL_F16, EL_BF16 = 0, 1, 2
+EL_E4M3, EL_INT8 = 1, 2
 EL_FLAG_FORCE_GENERIC = 1
 
 DTYPE_CODES = {"f32": EL_F32, "f16": EL_F16, "bf16": EL_BF16}
@@ -28,6 +30,8 @@ EXPORTED_SYMBOLS = (
     "el_attn_decode_segment", "el_attn_merge_segments", "el_attn_max_segments",
     "el_attn_paged_workspace_bytes", "el_attn_paged_attend", "el_attn_paged_append", "el_attn_paged_copy",
     "el_attn_max_alternatives", "el_attn_score_workspace_bytes", "el_attn_score_tokens",
+    "el_attn_quantized_workspace_bytes", "el_attn_quantized_attend", "el_attn_quantized_append", "el_attn_quantized_copy",
+    "el_attn_plan_workspace_bytes", "el_attn_plan_pages", "el_attn_sample_workspace_bytes", "el_attn_sample_tokens",
     "el_attn_destroy", "el_attn_status_string", "el_attn_version",
 )
 
@@ -54,6 +58,20 @@ class ElAttnPages(ctypes.Structure):
 class ElAttnScoreRule(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
                 ("slopes", ctypes.c_void_p)]
+
+
+class ElAttnPages8(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64), ("position_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("d_head", ctypes.c_int32),
+        ("block", ctypes.c_int32), ("format", ctypes.c_int32),
+    ]
+
+
+class ElAttnSampleRule(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("row_temperature", ctypes.c_void_p), ("row_top_k", ctypes.c_void_p), ("row_top_p", ctypes.c_void_p), ("row_min_p", ctypes.c_void_p)]
 
 
 class ElAttnError(RuntimeError):
@@ -133,6 +151,23 @@ def _load():
     lib.el_attn_score_workspace_bytes.restype = sz
     lib.el_attn_score_tokens.argtypes = [ctypes.c_int, vp, i64, i32, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.el_attn_score_tokens.restype = ctypes.c_int
+    pages8 = ctypes.POINTER(ElAttnPages8)
+    lib.el_attn_quantized_workspace_bytes.argtypes = [pages8, i32, i32, i32, i32, i32, i32]
+    lib.el_attn_quantized_workspace_bytes.restype = sz
+    lib.el_attn_quantized_attend.argtypes = [pages8, i32, vp, i64, i32, vp, vp, i64, i32, rule, vp, i32, vp, i32, i32, i32, vp, sz, vp]
+    lib.el_attn_quantized_attend.restype = ctypes.c_int
+    lib.el_attn_quantized_append.argtypes = [pages8, i32, vp, i64, i32, vp, vp, vp, vp, i64, i64, i32, i32, vp]
+    lib.el_attn_quantized_append.restype = ctypes.c_int
+    lib.el_attn_quantized_copy.argtypes = [pages8, vp, vp, vp, i32, vp]
+    lib.el_attn_quantized_copy.restype = ctypes.c_int
+    lib.el_attn_plan_workspace_bytes.argtypes = [i32, i32]
+    lib.el_attn_plan_workspace_bytes.restype = sz
+    lib.el_attn_plan_pages.argtypes = [vp, i64, i32, vp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.el_attn_plan_pages.restype = ctypes.c_int
+    lib.el_attn_sample_workspace_bytes.argtypes = [ctypes.c_int, i32, i32]
+    lib.el_attn_sample_workspace_bytes.restype = sz
+    lib.el_attn_sample_tokens.argtypes = [ctypes.c_int, vp, i64, i32, i32, vp, ctypes.POINTER(ElAttnSampleRule), vp, vp, vp, sz, vp]
+    lib.el_attn_sample_tokens.restype = ctypes.c_int
     lib.el_attn_destroy.argtypes = [vp]
     lib.el_attn_destroy.restype = ctypes.c_int
     lib.el_attn_status_string.argtypes = [ctypes.c_int]
@@ -285,6 +320,45 @@ def el_attn_score_tokens(dtype, logits, row_stride, rows, vocab, tokens, logprob
                                     top_logprob, top_index, workspace, workspace_bytes, stream)
 
 
+def el_attn_quantized_workspace_bytes(cache: ElAttnPages8, dtype, out_dtype, heads, B, beam, n) -> int:
+    return int(lib.el_attn_quantized_workspace_bytes(cache, dtype, out_dtype, heads, B, beam, n))
+
+
+def el_attn_quantized_attend(cache: ElAttnPages8, dtype, table, table_stride, table_pages, lengths, queries, query_stride, heads,
+                             rule: ElAttnScoreRule, out, out_dtype, lse, B, beam, n, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib.el_attn_quantized_attend(cache, dtype, table, table_stride, table_pages, lengths, queries, query_stride, heads, rule,
+                                        out, out_dtype, lse, B, beam, n, workspace, workspace_bytes, stream)
+
+
+def el_attn_quantized_append(cache: ElAttnPages8, dtype, table, table_stride, table_pages, lengths, counts, K_new, V_new,
+                             batch_stride, token_stride, B, T, stream=None) -> int:
+    return lib.el_attn_quantized_append(cache, dtype, table, table_stride, table_pages, lengths, counts, K_new, V_new,
+                                        batch_stride, token_stride, B, T, stream)
+
+
+def el_attn_quantized_copy(cache: ElAttnPages8, src, dst, counts, pairs, stream=None) -> int:
+    return lib.el_attn_quantized_copy(cache, src, dst, counts, pairs, stream)
+
+
+def el_attn_plan_workspace_bytes(B, pages) -> int:
+    return int(lib.el_attn_plan_workspace_bytes(B, pages))
+
+
+def el_attn_plan_pages(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
+                       new_table, new_lengths, granted, slots, copies, free_pages, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib.el_attn_plan_pages(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
+                                  new_table, new_lengths, granted, slots, copies, free_pages, workspace, workspace_bytes, stream)
+
+
+def el_attn_sample_workspace_bytes(dtype, rows, vocab) -> int:
+    return int(lib.el_attn_sample_workspace_bytes(dtype, rows, vocab))
+
+
+def el_attn_sample_tokens(dtype, logits, row_stride, rows, vocab, uniform, rule: ElAttnSampleRule, tokens, logprob,
+                          workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib.el_attn_sample_tokens(dtype, logits, row_stride, rows, vocab, uniform, rule, tokens, logprob, workspace, workspace_bytes, stream)
+
+
 def el_attn_core_timing_enable(ctx, max_steps) -> int:
     return lib.el_attn_core_timing_enable(ctx, max_steps)
 
@@ -429,37 +503,19 @@ def _call(where, device, fn, *args):
 _INT32_MAX = 2 ** 31 - 1
 
 
-class PagedCache:
-    """Projected keys and values of one attention layer, in pages (see el_attn_pages): new tokens in, attention of one token
-    per query row out (no causal form for several new tokens of a sequence), pages copied for beams that fork.
+def _check_pools(K, V):
+    """Pools of a paged cache, given as K and V: what holds for both storage widths."""
+    if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype or K.stride() != V.stride():
+        raise ValueError("K and V must be [pages, page_size, kv_heads, d_head] of one dtype and the same strides")
+    if not K.is_cuda or K.device != V.device:
+        raise ValueError("K and V must be on one device")
+    if K.stride(3) != 1 or max(K.shape) > _INT32_MAX:
+        raise ValueError("the last dimension of K and V must be contiguous, and every dimension below 2^31")
 
-    K, V: device tensors [pages, page_size, kv_heads, d_head], the last dimension contiguous, with the same strides (a
-    transposed view of [pages, kv_heads, page_size, d_head] is as good).  The table [B, columns] int32 and the lengths
-    int32 [B] are the caller's, shared by all layers: position t of sequence b lies in page table[b, t // page_size];
-    an entry outside the pool (-1) holds no positions.  Scratch memory comes from torch per call, so calls on several streams
-    and captured graphs keep apart.  No work (no sequence, no token, no pair, no beam) is no error.
-    """
 
-    def __init__(self, K, V):
-        import torch
-        self._torch = torch
-        if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype or K.stride() != V.stride():
-            raise ValueError("K and V must be [pages, page_size, kv_heads, d_head] of one dtype and the same strides")
-        if not K.is_cuda or K.device != V.device:
-            raise ValueError("K and V must be on one device")
-        if K.stride(3) != 1 or max(K.shape) > _INT32_MAX:
-            raise ValueError("the last dimension of K and V must be contiguous, and every dimension below 2^31")
-        if K.requires_grad or V.requires_grad:
-            raise ValueError("K and V are written in place: they must not require a gradient")
-        _check_tangent("K", K)
-        _check_tangent("V", V)
-        self._K, self._V = K, V
-        self.device = K.device
-        pages, self.page_size, self.kv_heads, self.d_head = K.shape
-        self.dtype = _dtype_code(K)
-        self._element = K.dtype
-        self._pages = ElAttnPages(_ptr(K), _ptr(V), K.stride(0), K.stride(1), K.stride(2),
-                                  pages, self.page_size, self.kv_heads, self.d_head, self.dtype)
+class _Pages:
+    """What the paged caches share: tables, new tokens, queries, copies.  A cache sets _torch, device, page_size, kv_heads, d_head, _pages, and
+    says how its calls are made."""
 
     @property
     def K(self):
@@ -479,16 +535,14 @@ class PagedCache:
             raise ValueError(f"table must be an int32 tensor on {self.device}")
         return table.data_ptr(), strides[0] if B > 1 else shape[1], shape[1]
 
-    def append(self, k, v, table, lengths, counts=None):
-        """New tokens k, v [B, T, kv_heads, d_head] (heads of a token contiguous, other strides free, the same for both) to
-        the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already.  B up to 65535."""
+    def _append(self, where, fn, head, element, k, v, table, lengths, counts):
         shape, strides, device = k.shape, k.stride(), self.device
         if len(shape) != 4 or shape != v.shape or shape[2] != self.kv_heads or shape[3] != self.d_head:
             raise ValueError(f"k and v must be [B, T, {self.kv_heads}, {self.d_head}]")
         if strides[3] != 1 or (self.kv_heads > 1 and strides[2] != self.d_head) or v.stride() != strides:
             raise ValueError("a token's heads must be contiguous, and k and v have the same strides")
-        _check_values("k", k, device, self._element)
-        _check_values("v", v, device, self._element)
+        _check_values("k", k, device, element)
+        _check_values("v", v, device, element)
         B, T = shape[0], shape[1]
         _check_index("lengths", lengths, device, (B,))
         if counts is not None:
@@ -497,11 +551,11 @@ class PagedCache:
         at, stride, columns = self._table(table, B)
         if B == 0 or T == 0:
             return
-        _call("el_attn_paged_append", device, lib.el_attn_paged_append, self._pages, at, stride, columns, lengths.data_ptr(),
+        _call(where, device, fn, *head, at, stride, columns, lengths.data_ptr(),
               _ptr(counts), k.data_ptr(), v.data_ptr(), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
 
     def _attend(self, queries, table, lengths, n, scale, softcap, window, slopes, out, out_code, lse):
-        """`queries` has been found to be [B, beam, heads, d_head] of this cache's type."""
+        """`queries` has been found to be [B, beam, heads, d_head] of a type that this cache takes."""
         (B, beam, heads, d), strides, device = queries.shape, queries.stride(), self.device
         if strides[3] != 1 or (heads > 1 and strides[2] != d):
             raise ValueError("the heads of a query must be contiguous")
@@ -521,26 +575,29 @@ class PagedCache:
         if abs(n) > _INT32_MAX or abs(window) > _INT32_MAX:
             raise ValueError("n and window must be 32-bit numbers")
         rule = ElAttnScoreRule(d ** -0.5 if scale is None else scale, softcap, window, _ptr(slopes))
-        nbytes = lib.el_attn_paged_workspace_bytes(self._pages, heads, B, beam, n)
+        where, fn, head, nbytes = self._attend_call(queries, out_code, heads, B, beam, n)
         ws = self._torch.empty(nbytes, dtype=self._torch.uint8, device=device) if nbytes else None
-        _call("el_attn_paged_attend", device, lib.el_attn_paged_attend, self._pages, at, stride, columns, _ptr(lengths),
+        _call(where, device, fn, *head, at, stride, columns, _ptr(lengths),
               queries.data_ptr(), strides[1] if beam > 1 else strides[0] if B > 1 else heads * d, heads, rule,
               out.data_ptr(), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
 
     def _check_queries(self, queries):
+        """The queries' type, as a code and as torch's."""
         shape = queries.shape
         if len(shape) != 4 or shape[3] != self.d_head or shape[2] % self.kv_heads != 0:
             raise ValueError(f"queries must be [B, beam, heads, {self.d_head}], heads a multiple of {self.kv_heads}")
-        _check_values("queries", queries, self.device, self._element)
+        code, element = self._query_type(queries)
+        _check_values("queries", queries, self.device, element)
+        return code, element
 
     def attend(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None,
                out_dtype=None, out=None):
         """Attention of queries [B, beam, heads, d_head] over each sequence's lengths[b] positions (None: n; n: the most that
         any sequence has, default what the table holds).  Returns out [B, beam, heads, d_head] in `out_dtype` ("f32" or the
-        cache's own, the default).  See el_attn_score_rule for scale (default d_head ** -0.5), softcap, window and slopes."""
-        self._check_queries(queries)
-        code = self.dtype if out_dtype is None else DTYPE_CODES[out_dtype]
-        element = self._element if code == self.dtype else _torch_dtype(code)
+        queries' own, the default).  See el_attn_score_rule for scale (default d_head ** -0.5), softcap, window and slopes."""
+        own, own_element = self._check_queries(queries)
+        code = own if out_dtype is None else DTYPE_CODES[out_dtype]
+        element = own_element if code == own else _torch_dtype(code)
         if out is None:
             out = self._torch.empty(queries.shape, dtype=element, device=self.device)
         elif out.shape != queries.shape or not out.is_contiguous():
@@ -562,9 +619,7 @@ class PagedCache:
         self._attend(queries, table, lengths, n, scale, softcap, window, slopes, A, EL_F32, lse)
         return A, lse
 
-    def copy_pages(self, src, dst, counts=None):
-        """Positions [0, counts[i]) (default all) of page dst[i] become those of page src[i]; int32 device tensors.  No page
-        may be the destination of two pairs, or the destination of one and the source of another."""
+    def _copy_pages(self, where, fn, src, dst, counts):
         device, shape = self.device, (src.numel(),)
         _check_index("src", src, device, shape)
         _check_index("dst", dst, device, shape)
@@ -572,8 +627,202 @@ class PagedCache:
             _check_index("counts", counts, device, shape)
         if shape[0] == 0:
             return
-        _call("el_attn_paged_copy", device, lib.el_attn_paged_copy, self._pages, src.data_ptr(), dst.data_ptr(), _ptr(counts),
-              shape[0])
+        _call(where, device, fn, self._pages, src.data_ptr(), dst.data_ptr(), _ptr(counts), shape[0])
+
+
+class PagedCache(_Pages):
+    """Projected keys and values of one attention layer, in pages (see el_attn_pages): new tokens in, attention of one token
+    per query row out (no causal form for several new tokens of a sequence), pages copied for beams that fork.
+
+    K, V: device tensors [pages, page_size, kv_heads, d_head], the last dimension contiguous, with the same strides (a
+    transposed view of [pages, kv_heads, page_size, d_head] is as good).  The table [B, columns] int32 and the lengths
+    int32 [B] are the caller's, shared by all layers: position t of sequence b lies in page table[b, t // page_size];
+    an entry outside the pool (-1) holds no positions.  Scratch memory comes from torch per call, so calls on several streams
+    and captured graphs keep apart.  No work (no sequence, no token, no pair, no beam) is no error.
+    """
+
+    def __init__(self, K, V):
+        import torch
+        self._torch = torch
+        _check_pools(K, V)
+        if K.requires_grad or V.requires_grad:
+            raise ValueError("K and V are written in place: they must not require a gradient")
+        _check_tangent("K", K)
+        _check_tangent("V", V)
+        self._K, self._V = K, V
+        self.device = K.device
+        pages, self.page_size, self.kv_heads, self.d_head = K.shape
+        self.dtype = _dtype_code(K)
+        self._element = K.dtype
+        self._pages = ElAttnPages(_ptr(K), _ptr(V), K.stride(0), K.stride(1), K.stride(2),
+                                  pages, self.page_size, self.kv_heads, self.d_head, self.dtype)
+
+    def append(self, k, v, table, lengths, counts=None):
+        """New tokens k, v [B, T, kv_heads, d_head] (heads of a token contiguous, other strides free, the same for both) to
+        the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already.  B up to 65535."""
+        self._append("el_attn_paged_append", lib.el_attn_paged_append, (self._pages,), self._element, k, v, table, lengths, counts)
+
+    def _query_type(self, queries):
+        return self.dtype, self._element
+
+    def _attend_call(self, queries, out_code, heads, B, beam, n):
+        return ("el_attn_paged_attend", lib.el_attn_paged_attend, (self._pages,),
+                lib.el_attn_paged_workspace_bytes(self._pages, heads, B, beam, n))
+
+    def copy_pages(self, src, dst, counts=None):
+        """Positions [0, counts[i]) (default all) of page dst[i] become those of page src[i]; int32 device tensors.  No page
+        may be the destination of two pairs, or the destination of one and the source of another."""
+        self._copy_pages("el_attn_paged_copy", lib.el_attn_paged_copy, src, dst, counts)
+
+
+class PagedCache8(_Pages):
+    """The paged cache in 8 bits (see el_attn_pages8): keys and values as codes, with a scale for each block of positions and head.
+
+    K, V: device tensors [pages, page_size, kv_heads, d_head], torch.float8_e4m3fn or torch.int8, strides as for PagedCache; d_head a
+    multiple of 16.  K_scale, V_scale: float32 [pages, kv_heads, page_size // block], contiguous; a value is code times scale.  What `append`
+    has not written needs neither codes nor scales.  Queries and new tokens are float32, float16 or bfloat16, whichever a call is given.
+    Everything else is as with PagedCache: the table and lengths may be the same.
+    """
+
+    def __init__(self, K, V, K_scale, V_scale):
+        import torch
+        self._torch = torch
+        _check_pools(K, V)
+        self.format = {torch.float8_e4m3fn: EL_E4M3, torch.int8: EL_INT8}.get(K.dtype)
+        if self.format is None:
+            raise ValueError(f"unsupported dtype {K.dtype}: float8_e4m3fn or int8")
+        pages, self.page_size, self.kv_heads, self.d_head = K.shape
+        self.device = K.device
+        shape = K_scale.shape
+        if len(shape) != 3 or tuple(shape[:2]) != (pages, self.kv_heads) or shape[2] < 1 or self.page_size % shape[2] != 0 or V_scale.shape != shape:
+            raise ValueError("K_scale and V_scale must be [pages, kv_heads, blocks of a page], the blocks all of one size")
+        for name, t in (("K", K), ("V", V), ("K_scale", K_scale), ("V_scale", V_scale)):
+            if t.requires_grad:
+                raise ValueError(f"{name} is written in place: it must not require a gradient")
+            _check_tangent(name, t)
+        for name, t in (("K_scale", K_scale), ("V_scale", V_scale)):
+            _check_values(name, t, self.device, torch.float32)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        self._K, self._V, self._K_scale, self._V_scale = K, V, K_scale, V_scale
+        self.block = self.page_size // shape[2]
+        self._pages = ElAttnPages8(_ptr(K), _ptr(V), _ptr(K_scale), _ptr(V_scale), K.stride(0), K.stride(1), K.stride(2),
+                                   pages, self.page_size, self.kv_heads, self.d_head, self.block, self.format)
+
+    @property
+    def K_scale(self):
+        return self._K_scale
+
+    @property
+    def V_scale(self):
+        return self._V_scale
+
+    def append(self, k, v, table, lengths, counts=None):
+        """New tokens as in PagedCache.append, rounded to codes: a block's scale is its largest value over the largest code, and grows (what the block
+        holds is rounded again) where a later token needs it.  No two sequences of a call may write into one block."""
+        self._append("el_attn_quantized_append", lib.el_attn_quantized_append, (self._pages, _dtype_code(k)), k.dtype, k, v, table, lengths, counts)
+
+    def _query_type(self, queries):
+        return _dtype_code(queries), queries.dtype
+
+    def _attend_call(self, queries, out_code, heads, B, beam, n):
+        code = _dtype_code(queries)
+        return ("el_attn_quantized_attend", lib.el_attn_quantized_attend, (self._pages, code),
+                lib.el_attn_quantized_workspace_bytes(self._pages, code, out_code, heads, B, beam, n))
+
+    def copy_pages(self, src, dst, counts=None):
+        """Positions [0, counts[i]) (default all) of page dst[i], and the scales of their blocks, become those of page src[i]; as PagedCache.copy_pages."""
+        self._copy_pages("el_attn_quantized_copy", lib.el_attn_quantized_copy, src, dst, counts)
+
+
+PagePlan = collections.namedtuple("PagePlan", "table lengths granted slots copies free")
+PagePlan.__doc__ = """The table of a step (see plan_pages): table [B, columns], lengths [B] with the new positions, granted [B] of them, slots [B, tokens] (int64;
+page * page_size + place, -1 for none), copies [3, B] (the operands of copy_pages), free [1] pages left; int32 where not said otherwise."""
+
+
+def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, parents=None, reserved=None, slots=True):
+    """The next step's table from what every sequence holds and needs, on the device (see el_attn_plan_pages).
+
+    table int32 [B_old, columns] (rows strided, a row contiguous) and lengths int32 [B_old]: what the sequences hold.  parents int32 [B] (None: each goes on
+    from itself): whom sequence b goes on from; -1 starts a new one.  counts int32 [B] (None: `tokens` each): positions that it needs, up to `tokens`.
+    pages, page_size: of the pool; reserved uint8 or bool [pages]: pages that others use.  A page that the new sequences do not name is free.
+
+        plan = plan_pages(table, lengths, counts, pages=cache.K.shape[0], page_size=cache.page_size, parents=parents)
+        cache.copy_pages(*plan.copies)
+        cache.append(k, v, plan.table, plan.lengths, plan.granted)
+
+    Returns a PagePlan of new tensors (slots=False: None in the place of its slots).  Where the free pages do not suffice, the first sequences
+    are served: granted is 0 for the others. """
+    import torch
+    shape, device, i32 = table.shape, table.device, torch.int32
+    if len(shape) != 2 or not table.is_cuda or table.dtype is not i32 or (shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be an int32 device tensor [B, columns] with contiguous rows")
+    B_old, columns = shape
+    _check_index("lengths", lengths, device, (B_old,))
+    B = B_old if parents is None else parents.numel()
+    if parents is not None:
+        _check_index("parents", parents, device, (B,))
+    if counts is not None:
+        _check_index("counts", counts, device, (B,))
+    if reserved is not None and (reserved.dtype not in (torch.uint8, torch.bool) or reserved.device != device or reserved.shape != (pages,) or not reserved.is_contiguous()):
+        raise ValueError(f"reserved must be a contiguous uint8 or bool tensor [{pages}] on {device}")
+    if max(pages, page_size, tokens, columns, B, B_old) > _INT32_MAX or min(B, B_old, columns) < 1:
+        raise ValueError("sizes must be 32-bit numbers, with at least one sequence and one column")
+    new_table = torch.empty((B, columns), dtype=i32, device=device)
+    small = torch.empty(5 * B + 1, dtype=i32, device=device)         # lengths, granted, copies, free
+    places = torch.empty((B, tokens), dtype=torch.int64, device=device) if slots and tokens > 0 else None
+    nbytes = lib.el_attn_plan_workspace_bytes(B, pages)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    at = small.data_ptr()
+    _call("el_attn_plan_pages", device, lib.el_attn_plan_pages, table.data_ptr(), table.stride(0) if B_old > 1 else columns, columns, lengths.data_ptr(), B_old,
+          _ptr(parents), _ptr(counts), _ptr(reserved), pages, page_size, B, tokens, new_table.data_ptr(), at, at + 4 * B, _ptr(places), at + 8 * B, at + 20 * B,
+          ws.data_ptr(), nbytes)
+    return PagePlan(new_table, small[:B], small[B:2 * B], places, small[2 * B:5 * B].view(3, B), small[5 * B:])
+
+
+def _setting(name, value, rows, device, dtype):
+    """A filter's setting: (number, address of a number for each row or None)."""
+    import torch
+    if not isinstance(value, torch.Tensor):
+        return value, None
+    if value.dtype is not dtype or value.device != device or value.shape != (rows,) or not value.is_contiguous():
+        raise ValueError(f"{name} must be a number or a contiguous {dtype} tensor [{rows}] on {device}")
+    if dtype is torch.float32:
+        _check_values(name, value, device, dtype)
+    return 0, value.data_ptr()
+
+
+def sample_tokens(logits, uniform, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """The next token of every row of logits [rows, vocab] (rows strided, a row contiguous): (tokens int32 [rows], logprob float32 [rows]).
+
+    uniform float32 [rows]: random numbers in [0, 1), one a row; the token is the first of the vocabulary at which the probabilities left by the filters add up to
+    more.  temperature, top_k, top_p, min_p: numbers, or a tensor [rows] (float32; top_k int32) with a setting for each row, in this order; off: 1.0, 0, 1.0, 0.0.  A
+    temperature of 0 takes the largest logit.  logprob is the token's among what is left.  See el_attn_sample_tokens."""
+    import torch
+    shape = logits.shape
+    if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and logits.stride(1) != 1) or max(shape) > _INT32_MAX:
+        raise ValueError("logits must be a device tensor [rows, vocab] with contiguous rows")
+    rows, vocab = shape
+    device, code, f32 = logits.device, _dtype_code(logits), torch.float32
+    _check_values("logits", logits, device, logits.dtype)
+    _check_values("uniform", uniform, device, f32)
+    if uniform.shape != (rows,) or not uniform.is_contiguous():
+        raise ValueError(f"uniform must be contiguous [{rows}]")
+    t, row_t = _setting("temperature", temperature, rows, device, f32)
+    k, row_k = _setting("top_k", top_k, rows, device, torch.int32)
+    p, row_p = _setting("top_p", top_p, rows, device, f32)
+    m, row_m = _setting("min_p", min_p, rows, device, f32)
+    if abs(k) > _INT32_MAX:
+        raise ValueError("top_k must be a 32-bit number")
+    tokens = torch.empty(rows, dtype=torch.int32, device=device)
+    logprob = torch.empty(rows, dtype=f32, device=device)
+    if rows == 0:
+        return tokens, logprob
+    nbytes = lib.el_attn_sample_workspace_bytes(code, rows, vocab)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _call("el_attn_sample_tokens", device, lib.el_attn_sample_tokens, code, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
+          uniform.data_ptr(), ElAttnSampleRule(t, k, p, m, row_t, row_k, row_p, row_m), tokens.data_ptr(), logprob.data_ptr(), _ptr(ws), nbytes)
+    return tokens, logprob
 
 
 def score_tokens(logits, tokens=None, *, k=0):

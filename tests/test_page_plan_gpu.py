@@ -1,0 +1,108 @@
+"""GPU parity of the page plan against the reference: whole numbers, all equal."""
+import numpy as np
+import pytest
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(tag, table, lengths, counts, parents, reserved, pages, page_size, T, slots=True, pad=0):
+    import torch
+    from paper_2105_04779_amd import el_attn
+    to = lambda a, t=np.int32: None if a is None else torch.from_numpy(np.ascontiguousarray(np.asarray(a, t))).cuda()
+    wide = np.full((table.shape[0], table.shape[1] + pad), 3, np.int32)
+    wide[:, :table.shape[1]] = table
+    plan = el_attn.plan_pages(to(wide)[:, :table.shape[1]], to(lengths), to(counts), pages=pages, page_size=page_size, tokens=T, parents=to(parents),
+                              reserved=to(reserved, np.uint8), slots=slots)
+    torch.cuda.synchronize()
+    want = oracle.plan_pages_reference(table, lengths, counts, parents, reserved, pages, page_size, T)
+    for name in ("table", "lengths", "granted", "copies", "free") + (("slots",) if slots else ()):
+        got = getattr(plan, name).cpu().numpy()
+        ref = np.reshape(want[name], got.shape)
+        assert np.array_equal(got, ref), f"{tag}: {name} differs at {np.argwhere(got != ref)[:4].tolist()}"
+    assert slots or plan.slots is None
+    return want
+
+
+def _random(seed, B_old, B, columns, page_size, T, room, fork, absent=0.0, share=0.0, reserve=0.0):
+    g = np.random.default_rng(seed)
+    lengths = g.integers(0, max(1, columns * page_size - T // 2) + 1, B_old)
+    held = -(-lengths // page_size)
+    used = int(held.sum())
+    pages = max(1, used + room)
+    order = g.permutation(pages)
+    table = np.full((B_old, columns), -1)
+    at = 0
+    for b in range(B_old):
+        table[b, :held[b]] = order[at:at + held[b]]
+        at += held[b]
+    for b in range(1, B_old):                                        # pages that several name, full ones and partly filled ones
+        if g.random() < share:
+            j = int(g.integers(0, columns))
+            table[b, :j] = table[b - 1, :j]
+    table[g.random(table.shape) < absent] = g.choice([-1, -9, pages, 10 ** 9])
+    parents = g.integers(-1, B_old + 1, B) if fork else None
+    counts = g.integers(-1, T + 2, B)
+    reserved = (g.random(pages) < reserve).astype(np.uint8) if reserve else None
+    return table, lengths, counts, parents, reserved, pages
+
+
+@pytest.mark.parametrize("page_size", [1, 5, 16])
+@pytest.mark.parametrize("T", [1, 7, 40])
+@pytest.mark.parametrize("seed", range(4))
+def test_random_plans(page_size, T, seed):
+    B_old, B, columns = [(1, 1, 1), (5, 9, 12), (33, 20, 30), (300, 700, 9)][seed]
+    for k, (room, fork, absent, share, reserve) in enumerate([(1000, False, 0, 0, 0), (40, True, 0, 0.5, 0), (3, True, 0.2, 0.5, 0.3), (0, True, 0, 0, 0)]):
+        b = B if fork else B_old
+        args = _random(100 * seed + 10 * T + k + page_size, B_old, b, columns, page_size, T, room, fork, absent, share, reserve)
+        _check(f"page {page_size} T {T} seed {seed} kind {k}", *args[:5], args[5], page_size, T, slots=k != 1, pad=k % 2 * 3)
+
+
+def test_large_pools_and_tables():
+    args = _random(7, 64, 64, 2000, 16, 300, 200000, True, 0.0, 0.3, 0.01)
+    _check("large", *args[:5], args[5], 16, 300)
+    args = _random(8, 3000, 5000, 6, 4, 3, 2000, True, 0.0, 0.3)
+    _check("many", *args[:5], args[5], 4, 3)
+    args = _random(9, 70000, 70000, 2, 8, 1, 500, False)
+    _check("very many", *args[:5], args[5], 8, 1)
+
+
+def test_lengths_at_and_beyond_the_columns():
+    table = np.arange(12).reshape(3, 4)
+    w = _check("full", table, [16, 15, 10 ** 9], [1, 1, 1], None, None, 40, 4, 1)
+    assert w["granted"].tolist() == [0, 1, 0] and w["lengths"].tolist() == [16, 16, 16]
+    _check("negative", table, [-5, 0, 3], [4, 0, 2], None, None, 40, 4, 4)
+    _check("everything reserved", table, [4, 8, 3], None, None, np.ones(40), 40, 4, 4)
+    _check("one page", np.array([[0]]), [3], None, [0, 0, -1], None, 1, 4, 1)
+
+
+def test_the_order_of_those_that_write_one_page():
+    # three hold page 2 with 5, 7 and 7 positions, the last two write: the second keeps it
+    table = np.array([[1, 2, -1], [3, 2, -1], [4, 2, -1]])
+    w = _check("order", table, [13, 15, 15], [1, 1, 1], None, None, 10, 8, 1)
+    assert w["copies"][0].tolist() == [2, -1, 2]
+    w = _check("a reader with more", table, [13, 15, 15], [1, 0, 0], None, None, 10, 8, 1)
+    assert w["copies"][:, 0].tolist() == [2, 0, 5]
+    w = _check("a reader with as many", table, [15, 15, 15], [0, 1, 0], None, None, 10, 8, 1)
+    assert (w["copies"][0] == -1).all()
+
+
+def test_the_same_plan_again_and_on_another_stream():
+    import torch
+    from paper_2105_04779_amd import el_attn
+    table, lengths, counts, parents, _, pages = _random(3, 50, 80, 40, 16, 5, 300, True, 0, 0.4)
+    t, l, c, p = (torch.from_numpy(np.asarray(a, np.int32)).cuda() for a in (table, lengths, counts, parents))
+    kw = dict(pages=pages, page_size=16, tokens=5, parents=p)
+    first = el_attn.plan_pages(t, l, c, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = el_attn.plan_pages(t, l, c, **kw)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    for bad in (dict(pages=0), dict(page_size=0), dict(tokens=0), dict(parents=p.long()), dict(reserved=torch.zeros(3, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises((ValueError, el_attn.ElAttnError)):
+            el_attn.plan_pages(t, l, c, **{**kw, **bad})
+    with pytest.raises(el_attn.ElAttnError):
+        el_attn.plan_pages(t.repeat(1, 1), l, None, pages=pages, page_size=1 << 30)

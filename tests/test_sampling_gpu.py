@@ -1,0 +1,170 @@
+"""GPU parity of the sampling against the fp64 reference.
+
+Tokens are exact.  Weights are whole multiples of 2^-43 of the largest, each off by half of that and by the exponential's 2^-40 of its own size, so a sum of V of them
+is off by less than 2^-38 of itself for the vocabularies here: where the reference's decisions lie further than that from going the other way (`margin`, which is
+checked), the token must be the same.  The log-probability is computed in 64 bits and rounded once: 2^-24 of itself, and 2^-38.
+"""
+import numpy as np
+import pytest
+
+import oracle
+from paper_2105_04779_amd import workloads as wl
+from helpers import record, to_device
+
+pytestmark = pytest.mark.gpu
+
+MARGIN = 2.0 ** -38
+
+
+def _check(tag, x, dtype, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, pad=0, offset=0, tight=()):
+    """`tight`: rows whose decisions are exact ones (equal weights), however close."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    rows, V = x.shape
+    x = wl.round_to_storage(x, dtype)
+    wide = np.full((rows, V + pad), np.float32(9e4 if dtype != "f16" else 6e4), dtype=np.float32)      # what is between rows would win
+    wide[:, :V] = x
+    flat = np.concatenate([np.full(offset, 5, np.float32), wide.reshape(-1)])
+    dev = to_device(wl.round_to_storage(flat, dtype), dtype)[offset:].view(rows, V + pad)[:, :V]
+    f = np.float32
+    full = {"temperature": (temperature, f), "top_k": (top_k, np.int32), "top_p": (top_p, f), "min_p": (min_p, f)}
+    given = {k: torch.from_numpy(np.asarray(v, t)).cuda() if np.ndim(v) else v for k, (v, t) in full.items()}
+    per_row = {k: np.broadcast_to(np.asarray(v, t), (rows,)) for k, (v, t) in full.items()}
+    uniform = np.asarray(uniform, f)
+    tokens, logprob = el_attn.sample_tokens(dev, torch.from_numpy(uniform).cuda(), **given)
+    torch.cuda.synchronize()
+    tokens, logprob = tokens.cpu().numpy(), logprob.cpu().numpy()
+    want, want_logprob, margin = oracle.sample_tokens_reference(x, uniform, **per_row)
+    margin[list(tight)] = np.inf
+    assert margin.min() > MARGIN, f"{tag}: the reference itself is within {margin.min():.1e} of another answer"
+    assert np.array_equal(tokens, want), f"{tag}: rows {np.nonzero(tokens != want)[0][:5]}: {tokens[tokens != want][:5]} for {want[tokens != want][:5]}"
+    same = (np.isnan(logprob) & np.isnan(want_logprob)) | (logprob == want_logprob)
+    with np.errstate(invalid="ignore"):
+        err = np.where(same, 0.0, np.abs(logprob - want_logprob) / (2.0 ** -24 * np.abs(want_logprob) + MARGIN))
+    record(f"{tag}: logprob {err.max():.3f} of the bound, margin {margin.min():.1e}")
+    assert (err <= 1.0).all(), f"{tag}: logprob {np.nanmax(err)} of the bound"
+    return tokens
+
+
+def _rows(seed, rows, V, banned=0.0):
+    g = np.random.default_rng(seed)
+    x = g.standard_normal((rows, V), dtype=np.float32) * np.float32(2)
+    hot = g.integers(0, V, (rows, 12))
+    for r in range(rows):
+        x[r, hot[r]] += g.random(12, dtype=np.float32) * 10
+    x[g.random((rows, V)) < banned] = -np.inf
+    return x, g.random(rows, dtype=np.float32)
+
+
+FILTERS = [dict(), dict(temperature=0.3), dict(temperature=1.9), dict(top_k=1), dict(top_k=7), dict(top_k=300), dict(top_p=0.5), dict(top_p=0.99), dict(min_p=0.1), dict(min_p=1.0),
+           dict(temperature=0.8, top_k=50, top_p=0.95, min_p=0.02), dict(temperature=0.0), dict(top_p=1e-6), dict(top_p=0.0), dict(min_p=2.0), dict(top_k=10 ** 9, top_p=2.0, min_p=-1.0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rule", FILTERS, ids=lambda r: "-".join(f"{k}{v}" for k, v in r.items()) or "none")
+def test_filters(dtype, rule):
+    for V, rows, pad, offset in ((5, 6, 3, 1), (1000, 9, 0, 0), (50265, 4, 7, 3)):
+        x, u = _rows(V + rows, rows, V)
+        _check(f"{rule} V {V} {dtype}", x, dtype, u, pad=pad, offset=offset, **rule)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 63, 64, 65, 1023, 1024, 1025, 4097, 16383, 65537, 131073, 200003])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_vocabularies(V, dtype):
+    x, u = _rows(V, 3, V, 0.05 if V > 3 else 0.0)
+    for rule in (dict(), dict(top_p=0.9), dict(top_k=min(V, 40), temperature=0.7)):
+        _check(f"V {V} {dtype} {rule}", x, dtype, u, offset=V % 3, pad=V % 5, **rule)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_settings_of_each_row(dtype):
+    g = np.random.default_rng(5)
+    rows, V = 64, 9001
+    x, u = _rows(6, rows, V, 0.1)
+    _check(f"mixed {dtype}", x, dtype, u, temperature=g.choice([0.0, 0.5, 1.0, 1.5], rows), top_k=g.choice([0, -3, 1, 20, 5000], rows),
+           top_p=g.choice([0.3, 0.9, 1.0, 1.5], rows), min_p=g.choice([0.0, -1.0, 0.05, 0.5], rows))
+    nan = np.full(rows, np.nan)
+    _check(f"settings of NaN {dtype}", x, dtype, u, temperature=nan)
+    _check(f"filters of NaN {dtype}", x, dtype, u, top_p=nan, min_p=nan)
+    _check(f"an infinite temperature {dtype}", np.where(x > 0, x, -np.inf), dtype, u, temperature=np.full(rows, 1e30), tight=range(rows))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_equal_logits_go_by_index(dtype):
+    V = 3001
+    flat = np.full((6, V), 2.5, np.float32)
+    u = [0.0, 0.25, 0.5, 0.75, 1.0 - 2.0 ** -24, 0.1]
+    # weights are equal, so the token is the whole part of u times how many stay
+    tokens = _check(f"flat {dtype}", flat, dtype, u, tight=range(6))
+    assert tokens.tolist() == [int(np.float64(np.float32(v)) * V) for v in u]
+    tokens = _check(f"flat top-k {dtype}", flat, dtype, u, top_k=10, tight=range(6))
+    assert tokens.tolist() == [0, 2, 5, 7, 9, 1]
+    _check(f"flat top-p {dtype}", flat, dtype, u, top_p=0.25, tight=range(6))
+    _check(f"flat min-p {dtype}", flat, dtype, u, min_p=1.0, tight=range(6))
+    # ties at the bound of top-k, spread over the vocabulary, some below the larger ones
+    g = np.random.default_rng(9)
+    x = g.choice([0.0, 1.0, 2.0, 3.0], (8, V), p=[0.5, 0.3, 0.15, 0.05]).astype(np.float32)
+    for k in (1, 100, 200, 1000):
+        _check(f"ties k {k} {dtype}", x, dtype, g.random(8), top_k=k, tight=range(8))
+    _check(f"ties top-p {dtype}", x, dtype, g.random(8), top_p=0.37)
+    zeros = np.zeros((4, V), np.float32)
+    zeros[:, ::2] = -0.0
+    assert _check(f"zeros of both signs {dtype}", zeros, dtype, [0.0, 0.5, 0.9, 0.99], top_k=4, tight=range(4)).tolist() == [0, 2, 3, 3]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_rows_without_numbers(dtype):
+    V = 777
+    x, u = _rows(11, 8, V)
+    x[0] = -np.inf
+    x[1, 5] = np.nan
+    x[2, 6] = np.inf
+    x[3] = np.nan
+    x[4] = -np.inf
+    x[4, 700] = -3.0
+    x[5] = -60000.0
+    x[6] = np.where(np.arange(V) % 7 == 3, 60000.0, -60000.0)
+    big = {"f32": 3.0e38, "bf16": 3.0e38, "f16": 65504.0}[dtype]
+    x[7] = np.where(np.arange(V) % 7 == 3, big, -big)
+    for rule in (dict(), dict(top_k=9), dict(top_p=0.5), dict(min_p=0.1), dict(temperature=0.0)):
+        _check(f"odd rows {dtype} {rule}", x, dtype, u, tight=range(8), **rule)
+
+
+def test_random_numbers_outside_their_range():
+    x, _ = _rows(12, 5, 300)
+    x[:, :2] = -np.inf
+    x[:, -3:] = -np.inf
+    u = np.array([-0.5, 1.0, 7.0, np.nan, 0.0], np.float32)
+    tokens = _check("outside", x, "f32", u, tight=range(5))
+    assert tokens.tolist() == [2, 296, 296, 296, 2]
+
+
+def test_frequencies():
+    """Evenly spread random numbers draw every token as often as its probability says, to one draw."""
+    x, _ = _rows(13, 1, 40)
+    n = 20000
+    u = ((np.arange(n) + 0.5) / n).astype(np.float32)
+    import torch
+    from paper_2105_04779_amd import el_attn
+    tokens, _ = el_attn.sample_tokens(torch.from_numpy(np.repeat(x, n, 0)).cuda(), torch.from_numpy(u).cuda(), temperature=1.3)
+    p = torch.softmax(torch.from_numpy(x[0]).double() / float(np.float32(1.3)), 0).numpy()
+    # (u in fp32 is off by 2^-25, far below the 1 / n between two)
+    assert np.abs(np.bincount(tokens.cpu().numpy(), minlength=40) - n * p).max() <= 1.0 + 1e-3
+
+
+def test_refusals_and_no_rows():
+    import torch
+    from paper_2105_04779_amd import el_attn
+    x, u = torch.zeros((4, 9), device="cuda"), torch.zeros(4, device="cuda")
+    tokens, logprob = el_attn.sample_tokens(x[:0], u[:0])
+    assert tokens.shape == logprob.shape == (0,)
+    for bad in (dict(temperature=torch.ones(4, device="cuda", dtype=torch.float64)), dict(top_k=torch.ones(4, device="cuda")), dict(top_p=torch.ones(3, device="cuda")),
+                dict(min_p=torch.ones(4)), dict(temperature=-1.0), dict(temperature=float("nan")), dict(top_k=1 << 40)):
+        with pytest.raises((ValueError, el_attn.ElAttnError)):
+            el_attn.sample_tokens(x, u, **bad)
+    with pytest.raises(ValueError):
+        el_attn.sample_tokens(x, u.double())
+    with pytest.raises(ValueError):
+        el_attn.sample_tokens(x, torch.zeros(5, device="cuda"))
+    with pytest.raises(ValueError, match="gradient"):
+        el_attn.sample_tokens(x.clone().requires_grad_(), u)
