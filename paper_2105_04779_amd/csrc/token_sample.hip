@@ -83,28 +83,35 @@ struct Weight {
     __device__ __forceinline__ u64 operator()(float x) const { return raw(x) - kBase; }
 };
 
-template <typename T> struct Sixteen;    // 16 bytes of logits
-template <> struct Sixteen<float> {
-    static constexpr int N = 4;
-    static __device__ __forceinline__ float at(u4 v, int i) { return __uint_as_float(v[i]); }
-    static __device__ __forceinline__ u4 none() { return u4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }      // all -inf
-};
-template <> struct Sixteen<bf16_t> {
-    static constexpr int N = 8;
-    static __device__ __forceinline__ float at(u4 v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
-    static __device__ __forceinline__ u4 none() { return u4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
-};
-template <> struct Sixteen<f16_t> {
-    static constexpr int N = 8;
-    // (a bit cast of a vector's element itself takes element 0 whatever the index: through a copy)
-    static __device__ __forceinline__ float at(u4 v, int i) { const unsigned u = v[i >> 1]; return (float)__builtin_bit_cast(h2, u)[i & 1]; }
-    static __device__ __forceinline__ u4 none() { return u4{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u}; }
+// Eight logits, which lie at a 16-byte boundary.
+template <typename T> struct Eight {
+    static constexpr int W = sizeof(T) / 2;                          // pieces of 16 bytes
+    u4 w[W];
+    __device__ __forceinline__ static Eight of(const T *at, bool there)
+    {
+        // (all -inf where there is none)
+        constexpr unsigned none = std::is_same<T, float>::value ? 0xff800000u : std::is_same<T, bf16_t>::value ? 0xff80ff80u : 0xfc00fc00u;
+        Eight e;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            e.w[i] = u4{none, none, none, none};
+            if (there) e.w[i] = ((const u4 *)at)[i];
+        }
+        return e;
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[i >> 2][i & 3]);
+        const unsigned u = w[0][i >> 1];             // (a bit cast of a vector's element itself takes element 0 whatever the index: through a copy)
+        if constexpr (std::is_same<T, bf16_t>::value) return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+        else return (float)__builtin_bit_cast(h2, u)[i & 1];
+    }
 };
 
-// A row: `full` pieces of 16 bytes behind `head` elements, `per` of them a wavefront's; the first wavefront has the elements before the pieces, the last those
+// A row: `full` pieces of 8 logits behind `head` of them, `per` of them a wavefront's; the first wavefront has the elements before the pieces, the last those
 // behind them, so shares lie one behind the other.
 template <typename T> struct Row {
-    static constexpr int N = Sixteen<T>::N;
+    static constexpr int N = 8;
     const T *row;
     int head, full, per, vocab;
     __device__ __forceinline__ Row(const SampleArgs &a, int64_t r)
@@ -119,29 +126,23 @@ template <typename T> struct Row {
     // g(x, index of the first) for N neighbours of wavefront w's share at a time, -inf where there is none in the row
     template <typename G> __device__ __forceinline__ void pieces(int w, G g) const
     {
-        constexpr int AHEAD = 4, TURN = N == 4 ? 2 : 1;              // under way, and of a turn: 8 logits (more copies of g would fill the instruction cache)
+        constexpr int AHEAD = std::is_same<T, float>::value ? 3 : 4;                 // under way; one copy of g, whose code would else fill the instruction cache
         const int lane = threadIdx.x & 63, end = min((w + 1) * per, full);
-        const u4 *const from = (const u4 *)(row + head);
-        u4 v[AHEAD];
+        const T *const from = row + head;
+        Eight<T> v[AHEAD];
         int p = w * per + lane;
-        auto load = [&](int at) __attribute__((always_inline)) { u4 x = Sixteen<T>::none(); if (at < end) x = from[at]; return x; };
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) v[j] = load(p + 64 * j);
+        for (int j = 0; j < AHEAD; ++j) v[j] = Eight<T>::of(from + (int64_t)(p + 64 * j) * N, p + 64 * j < end);
 #pragma unroll 1
-        for (int q = w * per; q < end; q += 64 * TURN, p += 64 * TURN) {
-            u4 now[TURN];
+        for (int q = w * per; q < end; q += 64, p += 64) {
+            const Eight<T> now = v[0];
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) {
-                if (j < TURN) now[j] = v[j];
-                v[j] = j + TURN < AHEAD ? v[j + TURN] : load(p + 64 * (j + TURN));
-            }
+            for (int j = 0; j + 1 < AHEAD; ++j) v[j] = v[j + 1];
+            v[AHEAD - 1] = Eight<T>::of(from + (int64_t)(p + 64 * AHEAD) * N, p + 64 * AHEAD < end);
+            float x[N];
 #pragma unroll
-            for (int j = 0; j < TURN; ++j) {
-                float x[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = Sixteen<T>::at(now[j], i);
-                g(x, head + (p + 64 * j) * N);
-            }
+            for (int i = 0; i < N; ++i) x[i] = now.at(i);
+            g(x, head + p * N);
         }
         if (w == 0 || w == kWaves - 1) {
             const int v = w == 0 ? lane : head + full * N + lane, stop = w == 0 ? head : vocab;
@@ -408,15 +409,20 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
                 // (the last range, which may hold most of a row, is summed in registers)
                 u64 last = 0;
                 row.pieces(w, [&](const float (&x)[Row<T>::N], int) __attribute__((always_inline)) {
-                    u64 t[Row<T>::N];
+                    constexpr int AT_ONCE = 4;       // (more weights side by side do not fit the registers)
 #pragma unroll
-                    for (int i = 0; i < Row<T>::N; ++i) t[i] = term(x[i]);
+                    for (int i0 = 0; i0 < Row<T>::N; i0 += AT_ONCE) {
+                        u64 t[AT_ONCE];
 #pragma unroll
-                    for (int i = 0; i < Row<T>::N; ++i) {
-                        const int bin = bin_of(x[i]);
-                        const bool in = x[i] >= floor_;
-                        if (in && bin < kBins - 1) atomicAdd(&bins[bin], t[i]);
-                        last += in && bin == kBins - 1 ? t[i] : 0;
+                        for (int i = 0; i < AT_ONCE; ++i) t[i] = term(x[i0 + i]);
+#pragma unroll
+                        for (int i = 0; i < AT_ONCE; ++i) {
+                            const int bin = bin_of(x[i0 + i]);
+                            const bool in = x[i0 + i] >= floor_;
+                            if (in && bin < kBins - 1) atomicAdd(&bins[bin], t[i]);
+                            last += in && bin == kBins - 1 ? t[i] : 0;
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 });
                 last = sum_wave(last);
@@ -578,7 +584,10 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
             for (int i = 1; i < Row<T>::N; ++i) most = fmaxf(most, x[i]);
             if (!__builtin_amdgcn_ballot_w64(most > least)) return;
 #pragma unroll
-            for (int i = 0; i < Row<T>::N; ++i) sum += weight(x[i] > least ? x[i] : -INFINITY);
+            for (int i = 0; i < Row<T>::N; ++i) {
+                sum += weight(x[i] > least ? x[i] : -INFINITY);
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
         });
         sum = sum_wave(sum);
         int ties = 0;
@@ -612,10 +621,13 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
         if (has_head)
             for (int v = 0; v < row.head; ++v) if (f(to_f32(row.row[v]), v)) return;
         for (int p = p0; p < p1; ++p) {
-            const u4 piece = ((const u4 *)(row.row + row.head))[p];
+            const Eight<T> piece = Eight<T>::of(row.row + row.head + (int64_t)p * N, true);
             bool done = false;
 #pragma unroll
-            for (int i = 0; i < N; ++i) done = done || f(Sixteen<T>::at(piece, i), row.head + p * N + i);
+            for (int i = 0; i < N; ++i) {
+                done = done || f(piece.at(i), row.head + p * N + i);
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
             if (done) return;
         }
         if (has_tail)
