@@ -23,6 +23,7 @@ namespace el {
 namespace {
 
 constexpr int TP = 32;                   // positions of a tile
+constexpr int kRor8 = 0x128;             // 16 lanes rotated by 8
 
 struct Attend8Args : AttendArgs {
     ScaleView s;
@@ -115,9 +116,13 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
     }
 
     // ---- the way of the tiles ----
-    // A lane's place in a row of K (chunk c of 16 bytes at 64 c + 16 g) and of V; columns beyond d_head are some of those below it: in K zeros of the
-    // queries meet them, in V their results are nobody's.
-    const int v_col = min(r16 * (DP / 16), a.d - DP / 16), k_row = 8 * (r16 >> 2) + (r16 & 3), v_row = 8 * g;
+    // A lane's chunk c of 16 bytes in a row of K, and its place in a row of V; columns beyond d_head are some of those below it: in K zeros of the
+    // queries meet them, in V their results are nobody's.  Request (x, n) reads whole lines of 8 rows of K; the lanes trade half of them (scores).
+    constexpr bool LINES = DP >= 128;
+    auto k_col = [&](int c) __attribute__((always_inline)) { return LINES ? 128 * (c >> 1) + 32 * g + 16 * (c & 1) : 64 * c + 16 * g; };
+    const int v_col = min(r16 * (DP / 16), a.d - DP / 16), v_row = 8 * g;
+    constexpr int KR = LINES ? 2 : 1;       // requests for the rows of a product
+    auto k_row = [&](int n) __attribute__((always_inline)) { return LINES ? 16 * n + 8 * (r16 >> 2 & 1) + (r16 & 3) : 8 * (r16 >> 2) + (r16 & 3); };
     const char *const Kh = a.c.K + kvh * a.c.head, *const Vh = a.c.V + kvh * a.c.head + v_col;
     const float *const Ks = a.s.K + (int64_t)kvh * a.s.per, *const Vs = a.s.V + (int64_t)kvh * a.s.per;
     const int32_t *const table = a.c.table + b * a.c.table_stride;
@@ -128,26 +133,50 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
     float ks[SC], vs[SC];
     unsigned mask = 0;                       // of the lane's 8 positions, those that are there
     bool some = false, all = false;          // of the tile's (uniform)
-    // FAST: slot and place of the lane's positions in the tile to be requested next, and the page named there.  Rows of K and V are requested apart, each
-    // when the tile before has been through its operands, so their ways are followed apart.
-    struct At { unsigned slot, off; int page; } ka{}, va{};
-    auto set = [&](At &p, int row) __attribute__((always_inline)) {
-        const unsigned t = (unsigned)t0 * TP + row;
-        p.slot = t / page_size;
-        p.off = t - p.slot * page_size;
-        p.page = table[min(p.slot, last_slot)];
+    // FAST: the four groups of 8 positions of the tile to be requested next: slot, place in the page, and the page, which comes through the scalar cache, a tile
+    // ahead: a wait for it is none for codes under way.
+    typedef const int32_t __attribute__((address_space(4))) *Entries;
+    const Entries entries = (Entries)(uintptr_t)table;
+    unsigned slot_at[4], off_at[4];
+    int page_at[4];
+    auto set = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned t = (unsigned)t0 * TP + 8 * i;
+            slot_at[i] = t / page_size;
+            off_at[i] = t - slot_at[i] * page_size;
+            page_at[i] = entries[min(slot_at[i], last_slot)];
+        }
     };
-    auto advance = [&](At &p) __attribute__((always_inline)) {
-        p.slot += a.step_slots;
-        p.off += a.step_rest;
-        if (p.off >= page_size) { p.off -= page_size; ++p.slot; }
-        p.page = table[min(p.slot, last_slot)];
+    auto advance = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            slot_at[i] += a.step_slots;
+            off_at[i] += a.step_rest;
+            if (off_at[i] >= page_size) { off_at[i] -= page_size; ++slot_at[i]; }
+            page_at[i] = entries[min(slot_at[i], last_slot)];
+        }
     };
+    // one of two or four numbers
+    auto pick = [&](bool one, int64_t x, int64_t y) __attribute__((always_inline)) { return one ? x : y; };
+    auto by_group = [&](int group, int64_t x0, int64_t x1, int64_t x2, int64_t x3) __attribute__((always_inline)) {
+        return group & 2 ? group & 1 ? x3 : x2 : group & 1 ? x1 : x0;
+    };
+    int64_t v_off = 0, s_off = 0;            // where the lane's rows of V, and its scales, of the tile requested next begin
+    bool v_ok = false;
     // (a position beyond the length has a wrapped difference, too large for the range)
     auto there = [&](unsigned t) __attribute__((always_inline)) { return t - (unsigned)first < (unsigned)(len - first); };
-    auto load_k = [&](int x, const char *row) __attribute__((always_inline)) {
+    auto load = [](const auto *p) __attribute__((always_inline)) {
+        if constexpr (LINES) return __builtin_nontemporal_load(p);
+        else return *p;
+    };
+    auto load_k = [&](int x, int n, const char *row) __attribute__((always_inline)) {
+        if constexpr (LINES) {
 #pragma unroll
-        for (int c = 0; c < KC; ++c) k[x][c] = __builtin_nontemporal_load((const u4 *)(row + min(64 * c + 16 * g, a.d - 16)));
+            for (int h = 0; h < KC / 2; ++h) k[x][2 * h + n] = load((const u4 *)(row + min(128 * h + 32 * g + 16 * (r16 >> 3), a.d - 16)));
+        } else {
+            k[x][0] = load((const u4 *)(row + min(16 * g, a.d - 16)));
+        }
     };
     // not FAST: a lane finds one of the tile's 32 rows, the others ask it
     int64_t row_off = 0;
@@ -160,20 +189,55 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
     auto request_k = [&](int i) __attribute__((always_inline)) {
         const unsigned start = (unsigned)(t0 + i) * TP;
         if constexpr (FAST) {
-            const char *const p = Kh + ka.page * a.c.page + (int64_t)(ka.off + (r16 & 3)) * a.c.position;
-            const bool ok = in_pool(ka.page);
-            if (start >= (unsigned)first && start + TP <= (unsigned)len && __ballot(ok) == ~0ull) {
-                load_k(0, p);
-                load_k(1, p + 4 * a.c.position);
-            } else {
+            int64_t row[4], scale[4];
+            bool ok = true, ok_at[4];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-#pragma unroll
-                    for (int c = 0; c < KC; ++c) k[x][c] = u4{0, 0, 0, 0};
-                    if (ok && there(start + k_row + 4 * x)) load_k(x, p + 4 * x * a.c.position);
-                }
+            for (int q = 0; q < 4; ++q) {
+                ok_at[q] = in_pool(page_at[q]);
+                ok &= ok_at[q];
+                row[q] = page_at[q] * a.c.page + (int64_t)off_at[q] * a.c.position;
+                scale[q] = page_at[q] * scale_page + a.s.by_block.of(off_at[q]);
             }
-            advance(ka);
+            advance();
+            v_off = by_group(g, row[0], row[1], row[2], row[3]);
+            s_off = by_group(g, scale[0], scale[1], scale[2], scale[3]);
+            all = ok && start >= (unsigned)first && start + TP <= (unsigned)len;
+            int64_t k_off[KR][2];
+            bool k_ok[KR];
+#pragma unroll
+            for (int n = 0; n < KR; ++n) {
+                const bool odd = r16 >> 2 & 1;
+                k_off[n][0] = (LINES ? pick(odd, row[2 * n + 1], row[2 * n]) : by_group(r16 >> 2, row[0], row[1], row[2], row[3])) + (r16 & 3) * a.c.position;
+                k_off[n][1] = k_off[n][0] + 4 * a.c.position;
+            }
+            if (!all) {
+                // a row that is not there is replaced by one that is, so that as many requests are under way for every tile; where there is none, by some place of the pool
+                v_ok = by_group(g, ok_at[0], ok_at[1], ok_at[2], ok_at[3]) != 0;
+                uint64_t lanes[KR][2];
+                int64_t other = 0;
+#pragma unroll
+                for (int n = 0; n < KR; ++n) {
+                    const bool odd = r16 >> 2 & 1;
+                    k_ok[n] = (LINES ? pick(odd, ok_at[2 * n + 1], ok_at[2 * n]) : by_group(r16 >> 2, ok_at[0], ok_at[1], ok_at[2], ok_at[3])) != 0;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        lanes[n][x] = __ballot(k_ok[n] & there(start + k_row(n) + 4 * x));
+                        if (lanes[n][x]) {
+                            const int from = __ffsll((long long)lanes[n][x]) - 1;
+                            other = (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k_off[n][x] >> 32), from) << 32) |
+                                              (unsigned)__builtin_amdgcn_readlane((int)k_off[n][x], from));
+                        }
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < KR; ++n)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) k_off[n][x] = (k_ok[n] & there(start + k_row(n) + 4 * x)) ? k_off[n][x] : other;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int n = 0; n < KR; ++n) load_k(x, n, Kh + k_off[n][x]);
         } else {
             const unsigned t = start + (lane & 31), slot = t / page_size, off = t - slot * page_size;
             const int page = there(t) ? table[slot] : -1;
@@ -191,38 +255,40 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
             }
             if (row_mask) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) load_k(x, Kh + row_of(k_row + 4 * x));
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int n = 0; n < KR; ++n) load_k(x, n, Kh + row_of(k_row(n) + 4 * x));
             }
         }
     };
     auto request_v = [&](int i) __attribute__((always_inline)) {
         const unsigned start = (unsigned)(t0 + i) * TP, tv = start + v_row;
         if constexpr (FAST) {
-            const bool ok = in_pool(va.page);
-            const char *const p = Vh + va.page * a.c.page + (int64_t)va.off * a.c.position;
-            const int64_t s = va.page * scale_page + a.s.by_block.of(va.off);
-            all = start >= (unsigned)first && start + TP <= (unsigned)len && __ballot(ok) == ~0ull;
-            if (all) {
-                mask = 0xff; some = true;
+            mask = 0xff; some = true;
+            int64_t row[8], of = s_off;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = __builtin_nontemporal_load((const VT *)(p + j * a.c.position));
-                ks[0] = Ks[s]; vs[0] = Vs[s];
-            } else {
-                // rows from lo to hi are there; the others are replaced by the nearest of them
-                const int lo = max(0, first - (int)tv), hi = (int)min((int64_t)7, (int64_t)len - 1 - tv);
-                const bool any = ok && lo <= hi;
+            for (int j = 0; j < 8; ++j) row[j] = v_off + j * a.c.position;
+            if (!all) {
+                // rows from lo to hi are there; the others are replaced by the nearest of them, or by another lane's
+                int lo = max(0, first - (int)tv), hi = (int)min((int64_t)7, (int64_t)len - 1 - tv);
+                const bool any = v_ok & (lo <= hi);
+                const uint64_t lanes = __ballot(any);
+                some = lanes != 0;
                 mask = any ? (0xffu << lo) & (0xffu >> (7 - hi)) : 0u;
-                some = __ballot(any) != 0;
-                ks[0] = vs[0] = 0.f;
+                int64_t at = v_off + lo * a.c.position;
+                const int from = some ? __ffsll((long long)lanes) - 1 : 0;
+                const int low = __builtin_amdgcn_readlane((int)at, from), high = __builtin_amdgcn_readlane((int)(at >> 32), from);
+                at = any ? v_off : some ? (int64_t)(((uint64_t)(unsigned)high << 32) | (unsigned)low) : 0;
+                lo = any ? lo : 0;
+                hi = any ? hi : 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = VT{};
-                if (any) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = *(const VT *)(p + min(max(j, lo), hi) * a.c.position);
-                    ks[0] = Ks[s]; vs[0] = Vs[s];
-                }
+                for (int j = 0; j < 8; ++j) row[j] = at + min(max(j, lo), hi) * a.c.position;
+                of = any ? of : 0;
             }
-            advance(va);
+            // (one sequence of requests for both kinds of tiles: the compiler's waits are by count, and by the shortest way)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = load((const VT *)(Vh + row[j]));
+            ks[0] = Ks[of]; vs[0] = Vs[of];
         } else {
             mask = row_mask >> v_row & 0xffu;
             some = row_mask != 0;
@@ -235,13 +301,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
             for (int j = 0; j < 8; ++j) { ks[j] = __shfl(row_ks, v_row + j, 64); vs[j] = __shfl(row_vs, v_row + j, 64); }
         }
     };
-    if (nt > 0) {
-        if constexpr (FAST) { set(ka, 8 * (r16 >> 2)); set(va, v_row); }
-        request_k(0);
-        request_v(0);
-    }
-
-    // ---- query rows: row r of the key head is beam r / group, head kvh * group + r % group; 8 elements from column 64 c + 16 g + 8 h on a piece ----
+    // ---- query rows: row r of the key head is beam r / group, head kvh * group + r % group; 8 elements from column k_col(c) + 8 h on a piece ----
     u4 q[RG][QP][KC][2];
     float slope[RG];
 #pragma unroll
@@ -252,7 +312,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
         const char *const p = a.queries + (b * a.beam + r / a.group) * a.query_stride + (int64_t)head * a.d * es;
 #pragma unroll
         for (int c = 0; c < 2 * KC; ++c) {
-            const int col = 64 * (c >> 1) + 16 * g + 8 * (c & 1);
+            const int col = k_col(c >> 1) + 8 * (c & 1);
             u4 w0 = u4{0, 0, 0, 0}, w1 = w0;
             if (here && col < a.d) {
                 w0 = *(const u4 *)(p + col * es);
@@ -281,6 +341,21 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
         slope[rg] = here && a.slopes ? a.slopes[head] : 0.f;
     }
 
+    if (nt > 0) {
+        if constexpr (FAST) set();
+        request_k(0);
+        request_v(0);
+        // (the queries are waited for here: a wait for them inside the loop would be one for all that is under way)
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+#pragma unroll
+            for (int n = 0; n < QP; ++n)
+#pragma unroll
+                for (int c = 0; c < 2 * KC; ++c) asm volatile("" : "+v"(q[rg][n][c >> 1][c & 1]));
+            asm volatile("" : "+v"(slope[rg]));
+        }
+    }
+
     f4 acc[RG][DT16];
     float m[RG], l[RG];
 #pragma unroll
@@ -290,13 +365,20 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
         for (int t = 0; t < DT16; ++t) acc[rg][t] = f4{0.f, 0.f, 0.f, 0.f};
     }
 
-#pragma unroll 1
-    for (int i = 0; i < nt; ++i) {
-        const int dist = (int)((unsigned)(len - 1) - ((unsigned)(t0 + i) * TP + v_row));         // of the lane's first position
-        // ---- scores ----
-        f4 s[RG][2];
+    f4 s[RG][2];
+    auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+            if constexpr (LINES) {           // row r16's chunks 2 h and 2 h + 1: half of the lanes have the one of it and the other's of row r16 ^ 8
+#pragma unroll
+                for (int h = 0; h < KC / 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k0 = (int)k[x][2 * h][e], k1 = (int)k[x][2 * h + 1][e];
+                        k[x][2 * h][e] = (unsigned)__builtin_amdgcn_update_dpp(k0, k1, kRor8, 0xf, 0xc, false);
+                        k[x][2 * h + 1][e] = (unsigned)__builtin_amdgcn_update_dpp(k1, k0, kRor8, 0xf, 0x3, false);
+                    }
+            }
 #pragma unroll
             for (int rg = 0; rg < RG; ++rg) s[rg][x] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -311,10 +393,10 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
                         for (int p = QP - 1; p >= 0; --p) s[rg][x] = Mma<BF16>::s16(kk, q[rg][p][c][h], s[rg][x]);
                 }
         }
-        const bool none = !some, whole_tile = all;
+    };
+    auto sums = [&](int i, bool whole_tile) __attribute__((always_inline)) {
+        const int dist = (int)((unsigned)(len - 1) - ((unsigned)(t0 + i) * TP + v_row));         // of the lane's first position
         const unsigned mask_now = mask;
-        if constexpr (FAST) { if (i + 1 < nt) request_k(i + 1); }
-        if (!none) {
         // ---- softmax: lane (g, r16) holds positions 8 g + 4 x + e of row r16 ----
         // (the largest score is taken from the others before they become powers of two: what scores have in common takes no digits from their
         // distances)
@@ -323,6 +405,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
         for (int rg = 0; rg < RG; ++rg) {
             float p[8], mx;
             const bool plain = FAST && whole_tile && !a.shaped;
+            const float v1 = mask_now ? vs[0] : 0.f;                 // (what stands for the scale of positions that are not there reaches nothing)
             if (plain) {
                 mx = s[rg][0][0];
 #pragma unroll
@@ -365,7 +448,7 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
             for (int j = 0; j < 8; ++j) {
                 p[j] = __builtin_amdgcn_exp2f(p[j] * a.unit);
                 l[rg] += p[j];
-                p[j] *= vs[FAST ? 0 : j];
+                p[j] *= FAST ? v1 : vs[j];
             }
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -396,11 +479,22 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
             column(std::integral_constant<int, 2>{});
             column(std::integral_constant<int, 3>{});
         }
-        }
-        if (i + 1 < nt) {
+    };
+    // Codes of the next tile's keys are requested when this one's have been multiplied, those of its values when this one's have.  (The last tile apart: on every way
+    // through the loop as many requests follow one another, and the compiler's waits are by count.)
+    if (nt > 0) {
+        int i = 0;
+#pragma unroll 1
+        for (; i + 1 < nt; ++i) {
+            scores();
+            const bool none = !some, whole_tile = all;
+            if constexpr (FAST) request_k(i + 1);
+            if (!none) sums(i, whole_tile);
             if constexpr (!FAST) request_k(i + 1);
             request_v(i + 1);
         }
+        scores();
+        if (some) sums(i, all);
     }
 
     int at = lane, group = a.group;
