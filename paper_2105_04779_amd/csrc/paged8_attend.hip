@@ -36,8 +36,8 @@ template <int FMT_, int DP_, int RG_, int QT_, int NP_, bool FAST_> struct Form8
     static constexpr int FMT = FMT_, DP = DP_, RG = RG_, QT = QT_, NP = NP_, QP = QT == EL_F32 ? 3 : 1;
     static constexpr bool FAST = FAST_;
     static constexpr int LDS = RG * DP * 64 + 256;                   // of a wavefront that shares its sequence: results, (m, l)
-    // wavefronts that a compute unit holds, by registers
-    static constexpr int PER_CU = DP == 256 || (DP == 128 && RG * QP == 6) ? 4 : RG * QP > 2 ? 8 : DP == 128 ? RG == 2 ? 8 : 12 : RG == 2 ? 12 : 16;
+    // wavefronts that a compute unit holds, by registers (twelve of 128 columns would fit: 91 us for 86 with eight, 64 sequences of 1024 to 4096 on 8 key heads)
+    static constexpr int PER_CU = DP == 256 || (DP == 128 && RG * QP == 6) ? 4 : DP == 128 || RG * QP > 2 ? 8 : RG == 2 ? 12 : 16;
     static constexpr int ROOM = 163840 / LDS, WAVES = ROOM >= 8 && PER_CU >= 8 ? 8 : 4;
 };
 
