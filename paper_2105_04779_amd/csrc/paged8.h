@@ -36,6 +36,12 @@ template <> struct Code<EL_E4M3> {
         const int low = __builtin_amdgcn_cvt_pk_fp8_f32(clamped(a), clamped(b), 0, false);
         return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(clamped(c), clamped(d), low, true);
     }
+    // (none of them NaN or beyond the largest by more than a quarter of a step)
+    static __device__ __forceinline__ unsigned of4_inside(float a, float b, float c, float d)
+    {
+        const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, low, true);
+    }
     static __device__ __forceinline__ f4 values(unsigned w)
     {
         const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
@@ -46,6 +52,16 @@ template <> struct Code<EL_INT8> {
     static constexpr float most = 127.f;
     static __device__ __forceinline__ unsigned one(float y) { return y != y ? 0u : (unsigned)(int)rintf(fminf(fmaxf(y, -most), most)) & 0xffu; }
     static __device__ __forceinline__ unsigned of4(float a, float b, float c, float d) { return one(a) | one(b) << 8 | one(c) << 16 | one(d) << 24; }
+    // (as above; the sum with 1.5 2^23 is rounded to an integer, whose last byte is the code)
+    static __device__ __forceinline__ unsigned of4_inside(float a, float b, float c, float d)
+    {
+        auto bits = [](float y) __attribute__((always_inline)) {
+#pragma clang fp contract(off)               // (y is rounded before it is added)
+            return __float_as_uint(y + 0x1.8p23f);
+        };
+        const unsigned low = __builtin_amdgcn_perm(bits(b), bits(a), 0x0c0c0400u), high = __builtin_amdgcn_perm(bits(d), bits(c), 0x04000c0cu);
+        return low | high;
+    }
     static __device__ __forceinline__ f4 values(unsigned w)
     {
         return f4{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
