@@ -1,7 +1,7 @@
 // The table of the next step: who goes on from whom, pages for new positions, copies of shared pages that are written, a slot for every new position.
 //
-// Pages in use are those that the new sequences name, so nothing is kept between calls.  Four launches, each bound by latency at the sizes of a serving
-// batch: marks cleared; rows copied and their pages marked; the unmarked pages of each chunk listed, and every sequence's need added up; entries, slots.
+// Pages in use are those that the new sequences name, so nothing is kept between calls.  Bound by latency at the sizes of a serving batch: one launch of one
+// workgroup where little is to be done (k_plan_small), else four: marks cleared; rows copied and their pages marked; the unmarked pages of each chunk listed, and every sequence's need added up; entries, slots.
 //
 // A mark is the largest of the keys (positions of the page in use, written?, lowest sequence first) of those that name it: a page is its writer's to keep if the
 // mark is the writer's own key.  Maxima and whole-number sums: the result does not depend on the order in which anything runs.
@@ -77,9 +77,10 @@ __global__ void __launch_bounds__(kLanes) k_plan_mark(const PlanArgs a)
 }
 
 // Sum over the lanes of a workgroup up to and without this one's; `total`: of all.
+template <int LANES = kLanes>
 __device__ __forceinline__ int64_t sum_before(int64_t v, int64_t &total)
 {
-    __shared__ int64_t part[kLanes / 64];
+    __shared__ int64_t part[LANES / 64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     int64_t up = v;
 #pragma unroll
@@ -90,7 +91,7 @@ __device__ __forceinline__ int64_t sum_before(int64_t v, int64_t &total)
     int64_t first = 0;
     total = 0;
 #pragma unroll
-    for (int i = 0; i < kLanes / 64; ++i) { if (i < w) first += part[i]; total += part[i]; }
+    for (int i = 0; i < LANES / 64; ++i) { if (i < w) first += part[i]; total += part[i]; }
     return first + up - v;
 }
 
@@ -211,6 +212,92 @@ __global__ void __launch_bounds__(kLanes) k_plan_assign(const PlanArgs a)
     }
 }
 
+// All of it by one workgroup, marks and free pages in LDS: pools of kSmallPages at most, where few entries and slots are to be gone through.  us on the device, four
+// launches / one: 32 sequences of 10 pages 15.2 / 10.0, 128 of 32 15.3 / 12.3, 64 of 128 16.3 / 15.3 (8256 entries and slots), 256 of 32 16.3 / 16.7, 64 of 119 and 128
+// new positions each 16.3 / 22.3.  Outside a graph three launches less save the host as much again.
+constexpr int kSmallPages = 8192, kSmallLanes = 1024;
+constexpr int64_t kSmallWork = 1 << 13;
+__global__ void __launch_bounds__(kSmallLanes) k_plan_small(const PlanArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    Mark *const marks = (Mark *)shared;                              // [pages]
+    int *const list = (int *)(marks + a.pages);                      // [pages] free pages, ascending
+    __shared__ int first_page[kSmallLanes];                          // of a sequence, of the free ones: its first; -1: nothing granted
+    __shared__ bool replaces[kSmallLanes];
+    const int tid = threadIdx.x;
+    for (int i = tid; i < a.pages; i += kSmallLanes) marks[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < a.B * a.columns; i += kSmallLanes) {
+        const int b = i / a.columns, j = i - b * a.columns;
+        const Ask s = ask(a, b);
+        const int e = entry(a, s, j);
+        a.new_table[i] = e;
+        if (e >= 0) atomicMax(&marks[e], key_of(a, s, j, b));
+    }
+    __syncthreads();
+    int64_t available, all;
+    {
+        constexpr int EACH = kSmallPages / kSmallLanes;
+        unsigned free = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int p = tid * EACH + i;
+            if (p < a.pages && marks[p] == 0 && !(a.reserved && a.reserved[p])) free |= 1u << i;
+        }
+        int at = (int)sum_before<kSmallLanes>(__popc(free), available);
+        for (; free; free &= free - 1) list[at++] = tid * EACH + __ffs((int)free) - 1;
+    }
+    // a sequence a lane
+    Ask s{};
+    int need = 0, last = -1;
+    bool replaced = false;
+    if (tid < a.B) {
+        s = ask(a, tid);
+        if (writes_last(a, s)) {
+            last = entry(a, s, s.held - 1);
+            replaced = last < 0 || (a.reserved && a.reserved[last]) || marks[last] != key_of(a, s, s.held - 1, tid);
+        }
+        if (s.count > 0) need = s.held_then - s.held + replaced;
+    }
+    const int64_t before = sum_before<kSmallLanes>(need, all);       // (and the list is there for all)
+    const bool grant = s.count > 0 && (need == 0 || before + need <= available);
+    if (tid < a.B) {
+        const int at = (int)before, granted = grant ? s.count : 0;
+        first_page[tid] = grant ? at : -1;
+        replaces[tid] = replaced;
+        if (grant) {
+            if (replaced) a.new_table[tid * a.columns + s.held - 1] = list[at];
+            for (int j = s.held; j < s.held_then; ++j) a.new_table[tid * a.columns + j] = list[at + replaced + j - s.held];
+        }
+        a.new_lengths[tid] = s.had + granted;
+        a.granted[tid] = granted;
+        const int src = grant && replaced ? last : -1;
+        a.copies[tid] = src;
+        a.copies[a.B + tid] = src >= 0 ? list[at] : -1;
+        a.copies[2 * a.B + tid] = src >= 0 ? s.had % a.page_size : 0;
+    }
+    // all that is granted is a beginning of what is needed
+    int64_t granted_pages;
+    (void)sum_before<kSmallLanes>(before + need <= available ? need : 0, granted_pages);
+    if (tid == 0) a.free_pages[0] = (int)(available - granted_pages);
+    __syncthreads();
+    if (a.slots)
+        for (int i = tid; i < a.B * a.T; i += kSmallLanes) {
+            const int b = i / a.T, t = i - b * a.T, at = first_page[b];
+            int64_t slot = -1;
+            if (at >= 0) {
+                const Ask x = ask(a, b);
+                if (t < x.count) {
+                    const int position = x.had + t, j = position / a.page_size;
+                    const bool anew = replaces[b];
+                    const int page = j < x.held - (anew ? 1 : 0) ? entry(a, x, j) : list[at + j - (x.held - (anew ? 1 : 0))];
+                    slot = (int64_t)page * a.page_size + (position - j * a.page_size);
+                }
+            }
+            a.slots[i] = slot;
+        }
+}
+
 struct PlanSpace { size_t marks, list, count, before, block_need, need, total; int chunks; };
 PlanSpace plan_space(int32_t B, int32_t pages)
 {
@@ -259,6 +346,12 @@ extern "C" el_status el_attn_plan_pages(const int32_t *table, int64_t table_stri
                      (int64_t *)(w + p.before), (int64_t *)(w + p.block_need), (int32_t *)(w + p.need)};
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
+    const int64_t work = (int64_t)B * columns + (int64_t)B * (slots ? T : T / page_size);
+    if (pages <= kSmallPages && B <= kSmallLanes && work <= kSmallWork) {
+        const int lds = pages * (int)(sizeof(Mark) + sizeof(int));
+        hipLaunchKernelGGL(k_plan_small, dim3(1), dim3(kSmallLanes), lds, s, a);
+        return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
+    }
     const int clear = (pages + 1023) / 1024, parts = (columns + 4 * kLanes - 1) / (4 * kLanes), blocks = (B + kLanes - 1) / kLanes;
     hipLaunchKernelGGL(k_plan_clear, dim3(clear < 2048 ? clear : 2048), dim3(256), 0, s, a.marks, pages);
     hipLaunchKernelGGL(k_plan_mark, dim3(parts, B < 32768 ? B : 32768), dim3(kLanes), 0, s, a);

@@ -59,6 +59,15 @@ def test_random_plans(page_size, T, seed):
         _check(f"page {page_size} T {T} seed {seed} kind {k}", *args[:5], args[5], page_size, T, slots=k != 1, pad=k % 2 * 3)
 
 
+@pytest.mark.parametrize("B,columns,T,pages", [(40, 30, 9, 8192), (40, 30, 9, 8193), (1024, 4, 3, 5000), (1025, 4, 3, 5000), (2, 2048, 2048, 8192), (2, 2048, 2049, 8192)])
+def test_where_one_workgroup_ends(B, columns, T, pages):
+    for k, (fork, share) in enumerate([(False, 0.0), (True, 0.4)]):
+        args = list(_random(31 + k, B, B, columns, 2, T, 0, fork, 0.0, share, 0.1))
+        args[0] = np.where(args[0] >= pages, -1, args[0])
+        args[4] = (np.random.default_rng(k).random(pages) < 0.1).astype(np.uint8)
+        _check(f"B {B} T {T} pages {pages} {fork}", *args[:5], pages, 2, T, slots=True, pad=k)
+
+
 def test_large_pools_and_tables():
     args = _random(7, 64, 64, 2000, 16, 300, 200000, True, 0.0, 0.3, 0.01)
     _check("large", *args[:5], args[5], 16, 300)
