@@ -10,6 +10,11 @@
 // Otherwise the bound of top-p or top-k is found by a histogram of weights (or counts) over 512 ranges of logits, one for each wavefront, and the tokens of the
 // range that it falls into are ranked; a range of too many is cut into 512 again.  The sums of the ranges above are then each wavefront's share of what is left, so
 // the token's sixteenth is known without another look at the row, and only that is gone through in order.
+//
+// Bound by the vector ALU, 23 operations a logit for its weight, 16 of them of 64 bits (HBM alone would allow a row in 11 us on each compute unit).  us of a row in
+// bf16, one on each compute unit, 128003 logits: maxima 11 (HBM's rate), all weights 30, or 43 with their histogram (the rest is atomics in LDS, 11 to 18 clocks
+// each), tokens of the range 17, ranked 5, the sixteenth and the token 6.  256 rows with settings of their own 97, 512 rows in fp32, half of them with top-p, 178 (two
+// rounds: LDS holds one row a compute unit); 4 rows of 50265 with top-k 50 and all filters 17, three looks at the row.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
