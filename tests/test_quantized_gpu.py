@@ -361,3 +361,46 @@ def test_no_work_is_no_error_and_derivatives_are_refused():
         c.cache.attend(q, c.table_d, c.lengths_d)
     with pytest.raises(ValueError):
         c.cache.append(c.q_d, c.q_d.half(), c.table_d, c.lengths_d)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_append_to_large_blocks_with_and_without_infinities(fmt, dtype):
+    def tweak(table, new):
+        new[0][0, 190, 0, 100], new[0][1, 3, 1, 7], new[1][0, 150, 1, 111] = np.inf, np.nan, -np.inf    # in what a wavefront holds, and behind it
+        new[1][1, 40:60] = np.nan
+    _append_case(11, fmt, dtype, 2, 200, 2, 112, 128, 128, [200, 331], [200, 177], tweak, pad=16)
+    _append_case(12, fmt, dtype, 2, 200, 2, 112, 256, 64, [203, 331], [199, 200], pad=48)
+    _append_case(13, fmt, dtype, 1, 70, 3, 80, 64, 32, [75], None, tweak=lambda table, new: new[0].__setitem__((0, 33, 2, 79), np.nan))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_pools_whose_offsets_pass_32_bits(fmt):
+    """Pages 1.7 GB apart: the same bits as in a compact pool."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 25 GB of device memory")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    B, kv, d, page, block, pages, apart = 2, 2, 128, 16, 16, 6, 1_700_000_000 // 16 * 16
+    element = torch.int8 if fmt == "int8" else torch.float8_e4m3fn
+    shape, strides = (pages, page, kv, d), (apart, kv * d, d, 1)
+    table = torch.tensor([[5, 0, 3], [2, 4, 1]], dtype=torch.int32, device="cuda")
+    lengths = torch.tensor([45, 34], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn((B, 45, kv, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((B, 1, 8, d), generator=g, device="cuda").to(torch.bfloat16)
+    results = []
+    for far in (False, True):
+        K, V = (torch.as_strided(torch.empty((pages - 1) * apart + page * kv * d, dtype=torch.uint8, device="cuda").view(element), shape, strides) if far
+                else torch.empty(shape, dtype=torch.uint8, device="cuda").view(element) for _ in range(2))
+        scales = [torch.zeros((pages, kv, page // block), device="cuda") for _ in range(2)]
+        cache = el_attn.PagedCache8(K, V, *scales)
+        cache.append(k, v, table, lengths, counts=lengths)
+        before = cache.attend(q, table, lengths)
+        cache.copy_pages(torch.tensor([5], dtype=torch.int32, device="cuda"), torch.tensor([2], dtype=torch.int32, device="cuda"))
+        after = cache.attend(q, table, lengths)
+        torch.cuda.synchronize()
+        results.append((before, after, *scales))
+        del cache, K, V
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert not torch.equal(results[0][0][1], results[0][1][1])
