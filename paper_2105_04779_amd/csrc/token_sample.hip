@@ -13,8 +13,9 @@
 //
 // Bound by the vector ALU, 23 operations a logit for its weight, 16 of them of 64 bits (HBM alone would allow a row in 11 us on each compute unit).  us of a row in
 // bf16, one on each compute unit, 128003 logits: maxima 11 (HBM's rate), all weights 30, or 43 with their histogram (the rest is atomics in LDS, 11 to 18 clocks
-// each), tokens of the range 17, ranked 5, the sixteenth and the token 6.  256 rows with settings of their own 97, 512 rows in fp32, half of them with top-p, 178 (two
-// rounds: LDS holds one row a compute unit); 4 rows of 50265 with top-k 50 and all filters 17, three looks at the row.
+// each), tokens of the range 17, ranked 5, the sixteenth and the token 6.  256 rows with settings of their own 79 (97 when rows with top-p and min-p were
+// always cut by the one before the other), 512 rows in fp32, half of them with top-p, 178 (two rounds: LDS holds one row a compute unit); 4 rows of 50265 with top-k 50
+// and all filters 17, three looks at the row.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
@@ -389,7 +390,9 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
     float least = -INFINITY;
     u64 equal = 0;
     bool sums = false;                                               // wave_sum and wave_ties are those of (least, equal)
-    // Sets them to where a sum in order, of weights or (COUNT) of ones, reaches a bound: `reached(sum)`.  begin(total) is told the sum of all; false ends it.
+    unsigned min_from = 0;                                           // the smallest order that min-p leaves
+    // Sets them to where a sum in order, of weights or (COUNT) of ones, reaches a bound: `reached(sum)`.  begin(total) is told the sum of all; false ends it.  So does
+    // min-p where it ends in a range before: the tokens that the bound falls between are not looked for then.
     auto select = [&](auto is_count, auto begin, auto reached, float steps) {
         constexpr bool COUNT = decltype(is_count)::value;
         // (those equal to `least` take part as well: of them, the lowest there are, no more than `equal` are taken in the end)
@@ -448,6 +451,7 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
             __syncthreads();
             const int cross = s.cross;
             over = s.before;
+            if (!COUNT && first && min_from && bin_of(value_of(min_from)) < cross) return;
             u64 share = 0;
             for (int i = lane; i < cross; i += 64) share += bins[i];
             share = sum_wave(share);
@@ -555,6 +559,7 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
             }
             equal = last == least ? lesser(equal, taken) : taken;
             least = last;
+            sums = !COUNT;
             __syncthreads();
             return;
         }
@@ -568,18 +573,14 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
         }
         __syncthreads();
     }
+    if (low > 0.0) min_from = first_order(max(order32(least), kLowest), order32(m), [&](float x) { return (double)weight(x) >= low; });
     if (by_weight) {
         double bound = 0.0;
         const u64 less = dropped ? dropped * weight(least) : 0;
         select(std::false_type{}, [&](u64 total) { bound = (double)top_p * (double)(total - less); return true; }, [&](u64 sum) { return (double)sum >= bound; },
                (float)fmin(weight.c * (kBins / 24.0), 1e30));          // (what weighs less than 2^-24 is one range)
-        sums = true;
     }
-    if (low > 0.0) {
-        // the smallest order whose weight min-p leaves
-        const unsigned bottom = max(order32(least), kLowest), from = first_order(bottom, order32(m), [&](float x) { return (double)weight(x) >= low; });
-        if (from > bottom) { least = value_of(from - 1); equal = 0; sums = false; }
-    }
+    if (min_from > max(order32(least), kLowest)) { least = value_of(min_from - 1); equal = 0; sums = false; }
     const u64 w_least = equal ? weight(least) : 0;
     if (!sums) {
         u64 sum = 0;

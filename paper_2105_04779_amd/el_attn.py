@@ -777,7 +777,8 @@ def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, paren
     _call("el_attn_plan_pages", device, lib.el_attn_plan_pages, table.data_ptr(), table.stride(0) if B_old > 1 else columns, columns, lengths.data_ptr(), B_old,
           _ptr(parents), _ptr(counts), _ptr(reserved), pages, page_size, B, tokens, new_table.data_ptr(), at, at + 4 * B, _ptr(places), at + 8 * B, at + 20 * B,
           ws.data_ptr(), nbytes)
-    return PagePlan(new_table, small[:B], small[B:2 * B], places, small[2 * B:5 * B].view(3, B), small[5 * B:])
+    new_lengths, granted, copies, free = torch.split_with_sizes(small, (B, B, 3 * B, 1))
+    return PagePlan(new_table, new_lengths, granted, places, copies.view(3, B), free)
 
 
 def _setting(name, value, rows, device, dtype):

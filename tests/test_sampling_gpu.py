@@ -90,6 +90,14 @@ def test_settings_of_each_row(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_min_p_before_and_behind_the_bound_of_top_p(dtype):
+    p, m = (a.reshape(-1) for a in np.meshgrid([0.2, 0.6, 0.9, 0.99, 0.9999], [1e-7, 1e-5, 1e-3, 0.03, 0.3, 0.7, 0.99]))
+    x, u = _rows(17, p.size, 20011, 0.02)
+    for temperature, k in ((1.0, 0), (2.5, 0), (1.3, 900)):
+        _check(f"top-p and min-p, T {temperature} k {k} {dtype}", x, dtype, u, temperature=temperature, top_k=k, top_p=p, min_p=m, pad=1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_equal_logits_go_by_index(dtype):
     V = 3001
     flat = np.full((6, V), 2.5, np.float32)
