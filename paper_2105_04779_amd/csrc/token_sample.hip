@@ -6,16 +6,18 @@
 // keep a beginning of one order (larger logits first, of equal ones the lowest index), so together they are a smallest logit, `least`, and how many of those equal
 // to it stay, `equal`.
 //
-// A row a workgroup, each wavefront a sixteenth of it.  Few tokens (top-k): those not below a bound from the lanes' maxima are collected and ranked by counting.
+// A row a workgroup of 16 wavefronts, each with a sixteenth of it (8 with an eighth where the rows are more than the compute units).  Few tokens (top-k): those not below a bound from the lanes' maxima are collected and ranked by counting.
 // Otherwise the bound of top-p or top-k is found by a histogram of weights (or counts) over 512 ranges of logits, one for each wavefront, and the tokens of the
 // range that it falls into are ranked; a range of too many is cut into 512 again.  The sums of the ranges above are then each wavefront's share of what is left, so
-// the token's sixteenth is known without another look at the row, and only that is gone through in order.
+// the token's share is known without another look at the row, and only that is gone through in order.
 //
 // Bound by the vector ALU, 23 operations a logit for its weight, 16 of them of 64 bits (HBM alone would allow a row in 11 us on each compute unit).  us of a row in
 // bf16, one on each compute unit, 128003 logits: maxima 11 (HBM's rate), all weights 30, or 43 with their histogram (the rest is atomics in LDS, 11 to 18 clocks
-// each), tokens of the range 17, ranked 5, the sixteenth and the token 6.  256 rows with settings of their own 79 (97 when rows with top-p and min-p were
-// always cut by the one before the other), 512 rows in fp32, half of them with top-p, 178 (two rounds: LDS holds one row a compute unit); 4 rows of 50265 with top-k 50
-// and all filters 17, three looks at the row.
+// each), tokens of the range 17, ranked 5, the share and the token 6.  256 rows with settings of their own 79 (97 when rows with top-p and min-p were
+// always cut by the one before the other), 4 rows of 50265 with top-k 50 and all filters 17, three looks at the row.
+// More rows than compute units: workgroups of 512 lanes, two of which share one, so that a row computes while the other waits.  us with 1024 / 512: 512 rows of 128003 in bf16,
+// top-p 0.9 170 / 157, top-k 40 70 / 59, nothing 100 / 101; of 32000, top-p 72 / 53; 2000 of 32000, top-k and top-p of their own 182 / 123.  Rows that take longer are
+// begun first: 512 in fp32, half of them with top-p, 178 in their order (176 with 512 lanes), 160.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
@@ -24,10 +26,10 @@
 namespace el {
 namespace {
 
-constexpr int kLanes = 1024, kWaves = kLanes / 64;
 constexpr int kBins = 512;
-constexpr int kList = 4096, kEach = 512;         // tokens that are collected, all and of one wavefront
-constexpr int kRanked = 1024;            // of them, those that are ranked by counting: one a lane
+constexpr int kEach = 512;               // tokens that a wavefront collects
+constexpr int kComputeUnits = 256;
+constexpr int kOrdered = 4096;           // rows up to which those that take longer are begun first
 constexpr int kFewTokens = 128;          // top-k up to which the bound from the lanes' maxima is used
 constexpr int32_t kMaxVocab = 1 << 19;
 constexpr double kLog2e = 1.4426950408889634074;
@@ -61,7 +63,19 @@ struct SampleArgs {
     int32_t *tokens;
     float *logprob;
     Powers powers;
+    int rows;
+    bool by_cost;                        // rows that take longer first
 };
+
+// Does row r need the sums over ranges?
+__device__ __forceinline__ bool takes_longer(const SampleArgs &a, int r)
+{
+    const el_attn_sample_rule &f = a.rule;
+    const int k = f.row_top_k ? f.row_top_k[r] : f.top_k;
+    const float p = f.row_top_p ? f.row_top_p[r] : f.top_p;
+    const bool counted = k > 0 && k < a.vocab;
+    return counted ? k > kFewTokens : p > 0.f && p < 1.f;
+}
 
 // The weights of a row: exp((x - m) / T) in units of 2^-43, whole numbers, without a branch.
 struct Weight {
@@ -113,6 +127,12 @@ template <typename T> struct Eight {
         else return (float)__builtin_bit_cast(h2, u)[i & 1];
     }
 };
+
+// What a workgroup of LANES lanes does with a row.
+template <int LANES> struct Sampling {
+static constexpr int kLanes = LANES, kWaves = kLanes / 64;
+static constexpr int kList = kWaves > 8 ? 4096 : (kWaves - 1) * kBins;       // tokens that are collected, of all wavefronts
+static constexpr int kRanked = kLanes;           // of them, those that are ranked by counting: one a lane
 
 // A row: `full` pieces of 8 logits behind `head` of them, `per` of them a wavefront's; the first wavefront has the elements before the pieces, the last those
 // behind them, so shares lie one behind the other.
@@ -187,10 +207,10 @@ struct Shared {
     // (the ranked list lies where the last wavefronts' ranges were, which have been added up by then)
     __device__ __forceinline__ u64 *sorted() { return bins[kWaves - 2]; }
 };
-static_assert(2 * kBins >= kRanked && kBins >= kEach && (kWaves - 1) * kBins >= kList, "room of the lists");
+static_assert(2 * kBins >= kRanked && kBins >= kEach && (kWaves - 1) * kBins >= kList && kLanes >= kBins, "room of the lists");
 
 // Sum over the lanes before this one in the workgroup; `total`: of all.
-__device__ __forceinline__ u64 sum_before(Shared &s, u64 v, u64 &total)
+static __device__ __forceinline__ u64 sum_before(Shared &s, u64 v, u64 &total)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     u64 up = v;
@@ -205,7 +225,7 @@ __device__ __forceinline__ u64 sum_before(Shared &s, u64 v, u64 &total)
     for (int i = 0; i < kWaves; ++i) { if (i < w) first += s.part[i]; total += s.part[i]; }
     return first + up - v;
 }
-__device__ __forceinline__ u64 sum_wave(u64 v)
+static __device__ __forceinline__ u64 sum_wave(u64 v)
 {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -213,7 +233,7 @@ __device__ __forceinline__ u64 sum_wave(u64 v)
 }
 
 // The first of the orders from `from` to `to` whose number is `in`, as all behind it are, the last one among them: 64 candidates a round.
-template <typename F> __device__ __forceinline__ unsigned first_order(unsigned from, unsigned to, F in)
+template <typename F> static __device__ __forceinline__ unsigned first_order(unsigned from, unsigned to, F in)
 {
     const unsigned lane = threadIdx.x & 63;
     unsigned size = to - from;                                       // the answer lies in [from, from + size]
@@ -229,7 +249,7 @@ template <typename F> __device__ __forceinline__ unsigned first_order(unsigned f
 }
 
 // The k-th largest of 256 numbers, four a lane, without its bits below 16 (0: fewer than k are above 0).
-__device__ __forceinline__ unsigned kth_of(const unsigned (&mine)[4], int k)
+static __device__ __forceinline__ unsigned kth_of(const unsigned (&mine)[4], int k)
 {
     unsigned bound = 0;
 #pragma unroll
@@ -261,7 +281,7 @@ struct Taken {
     }
 };
 // The wavefronts' lists as one: how many, or more than kList if there is not room for all.  All lanes.
-__device__ __forceinline__ int gather(Shared &s, const Taken &t)
+static __device__ __forceinline__ int gather(Shared &s, const Taken &t)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     __syncthreads();
@@ -277,7 +297,7 @@ __device__ __forceinline__ int gather(Shared &s, const Taken &t)
 }
 
 // The list's n keys (followed by zeros) in descending order.  All lanes; n up to kRanked.
-__device__ __forceinline__ void rank_list(Shared &s, int n)
+static __device__ __forceinline__ void rank_list(Shared &s, int n)
 {
     const int tid = threadIdx.x;
     if (tid < 8) s.list[n + tid] = 0;
@@ -298,11 +318,26 @@ __device__ __forceinline__ void rank_list(Shared &s, int n)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
+static __device__ __forceinline__ void run(const SampleArgs &a)
 {
     __shared__ Shared s;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t r = blockIdx.x;
+    int64_t r = blockIdx.x;
+    if (a.by_cost) {
+        const int each = (a.rows + kLanes - 1) / kLanes, first = min(tid * each, a.rows), last = min(first + each, a.rows);
+        u64 longer = 0, all;
+        for (int i = first; i < last; ++i) longer += takes_longer(a, i);
+        const u64 before = sum_before(s, longer, all), mine = blockIdx.x;
+        const bool want = mine < all;
+        const u64 front = want ? before : all + (u64)first - before, here = want ? longer : (u64)(last - first) - longer;
+        if (mine >= front && mine < front + here) {
+            int i = first;
+            for (u64 n = mine - front;; ++i) if (takes_longer(a, i) == want && n-- == 0) break;
+            s.cross = i;
+        }
+        __syncthreads();
+        r = __builtin_amdgcn_readfirstlane(s.cross);
+    }
     const Row<T> row(a, r);
 
     // ---- the largest logit, and the lanes' maxima, four lanes each ----
@@ -312,8 +347,9 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
     if (tid == 0) { s.bad = 0; s.token = 0x7fffffff; }
     {
         float m4 = fmaxf(m, quad_xor1(m));
-        m4 = fmaxf(m4, quad_xor2(m4));
-        if (tid % 4 == 0) s.best[tid / 4] = m4 > -INFINITY ? order32(m4) : 0u;
+        if constexpr (kLanes == 1024) m4 = fmaxf(m4, quad_xor2(m4));
+        constexpr int SHARE = kLanes / 256;
+        if (tid % SHARE == 0) s.best[tid / SHARE] = m4 > -INFINITY ? order32(m4) : 0u;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
         if (lane == 0) s.part_m[w] = m;
@@ -664,6 +700,18 @@ __global__ void __launch_bounds__(kLanes) k_sample(const SampleArgs a)
         write(chosen, wv, total);
     }
 }
+};
+
+template <int LANES, typename T>
+__global__ void __launch_bounds__(LANES, 4) k_sample(const SampleArgs a) { Sampling<LANES>::template run<T>(a); }
+
+template <int LANES>
+void launch_sample(const SampleArgs &a, int dtype, int rows, hipStream_t s)
+{
+    if (dtype == EL_F32) hipLaunchKernelGGL((k_sample<LANES, float>), dim3(rows), dim3(LANES), 0, s, a);
+    else if (dtype == EL_F16) hipLaunchKernelGGL((k_sample<LANES, f16_t>), dim3(rows), dim3(LANES), 0, s, a);
+    else hipLaunchKernelGGL((k_sample<LANES, bf16_t>), dim3(rows), dim3(LANES), 0, s, a);
+}
 
 } // namespace
 } // namespace el
@@ -684,11 +732,11 @@ extern "C" el_status el_attn_sample_tokens(el_dtype dtype, const void *logits, i
          (uintptr_t)rule->row_top_p | (uintptr_t)rule->row_min_p) & 3) return EL_ERR_INVALID_ARG;
     if (!rule->row_temperature && !(rule->temperature >= 0.f && rule->temperature < INFINITY)) return EL_ERR_INVALID_ARG;
     (void)workspace; (void)workspace_bytes;
-    const SampleArgs a{(const char *)logits, row_stride * es, vocab, uniform, *rule, tokens, logprob, kPowers};
+    const SampleArgs a{(const char *)logits, row_stride * es, vocab, uniform, *rule, tokens, logprob, kPowers, rows,
+                       rows > kComputeUnits && rows <= kOrdered && (rule->row_top_k || rule->row_top_p)};
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
-    if (dtype == EL_F32) hipLaunchKernelGGL((k_sample<float>), dim3(rows), dim3(kLanes), 0, s, a);
-    else if (dtype == EL_F16) hipLaunchKernelGGL((k_sample<f16_t>), dim3(rows), dim3(kLanes), 0, s, a);
-    else hipLaunchKernelGGL((k_sample<bf16_t>), dim3(rows), dim3(kLanes), 0, s, a);
+    if (rows > kComputeUnits) launch_sample<512>(a, dtype, rows, s);
+    else launch_sample<1024>(a, dtype, rows, s);
     return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
 }

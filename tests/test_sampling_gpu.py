@@ -98,6 +98,22 @@ def test_min_p_before_and_behind_the_bound_of_top_p(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [1, 7, 515, 4099, 30011])
+def test_more_rows_than_compute_units(V, dtype):
+    g = np.random.default_rng(V)
+    rows = 263
+    x, u = _rows(V + 1, rows, V, 0.05 if V > 7 else 0.0)
+    x[5, :] = -np.inf
+    x[6, V // 2] = np.nan
+    x[7, :] = 1.5                                                    # one order
+    x[8, :] = np.where(np.arange(V) % 2, 1.5, 1.0)
+    for n, rule in enumerate((dict(), dict(top_k=40, top_p=0.9), dict(top_p=0.95), dict(top_k=300, temperature=1.7), dict(temperature=0.0),
+                              dict(temperature=g.choice([0.0, 0.7, 1.0, 2.0], rows), top_k=g.choice([0, 1, 60, 200, 900], rows),
+                                   top_p=g.choice([0.2, 0.8, 0.97, 1.0], rows), min_p=g.choice([0.0, 1e-4, 0.04, 0.6], rows)))):
+        _check(f"{rows} rows V {V} {dtype} rule {n}", x, dtype, u, pad=n % 3, offset=n % 2, tight=(7, 8), **rule)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_equal_logits_go_by_index(dtype):
     V = 3001
     flat = np.full((6, V), 2.5, np.float32)
