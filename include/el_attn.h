@@ -545,7 +545,7 @@ typedef struct {
 /*
  * Attention of one new token per query row over the sequence's pages: el_attn_paged_attend with K and V the values that codes and scales stand for, and
  * everything said there (lengths, rule, out, lse, empty rows, NaN, workspace, errors) the same.  `dtype`: of the queries; `out_dtype`: EL_F32 or `dtype`.
- * Queries are taken with all their bits; probabilities as bf16 numbers that add up to 16 bits, 24 for a result in fp32.
+ * Queries are taken with all their bits; probabilities times their scales as bf16 numbers that add up to 24 bits.
  */
 size_t el_attn_quantized_workspace_bytes(const el_attn_pages8 *cache, int32_t dtype, int32_t out_dtype, int32_t heads, int32_t B, int32_t beam, int32_t n);
 el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32_t dtype,

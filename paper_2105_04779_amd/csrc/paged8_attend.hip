@@ -37,10 +37,13 @@ struct Attend8Args : AttendArgs {
     int step_slots, step_rest;           // pages and positions that 32 positions are
 };
 
-// Form of a wavefront: format, d_head padded, query rows in groups of 16, the queries' type (EL_F32: three bf16 parts, which hold any type's bits), bf16 parts
-// of a probability.  FAST: pages and blocks are multiples of 8 positions, so a lane's 8 positions have one page and one scale.
-template <int FMT_, int DP_, int RG_, int QT_, int NP_, bool FAST_> struct Form8 {
-    static constexpr int FMT = FMT_, DP = DP_, RG = RG_, QT = QT_, NP = NP_, QP = QT == EL_F32 ? 3 : 1;
+// Form of a wavefront: format, d_head padded, query rows in groups of 16, the queries' type (EL_F32: three bf16 parts, which hold any type's bits).
+// FAST: pages and blocks are multiples of 8 positions, so a lane's 8 positions have one page and one scale.
+// A probability times its scale is three bf16 parts, which hold its 24 bits, whatever the result's type.  Two (16 bits) would round one result in a thousand
+// to bf16 the other way, fourteen to fp16, and save little, us with two / three: 64 sequences of 1024 to 4096 on 8 key heads of 128 80.4 / 79.4, 512 of up to 256, 16 heads of 64,
+// 54.0 / 56.2, 32 of 1024 to 4096, 32 rows on each of 8 key heads of 128, 65.5 / 67.9, 16 of up to 8192 at 256 columns 70.7 / 72.2, one of 613 11.4 / 11.7.
+template <int FMT_, int DP_, int RG_, int QT_, bool FAST_> struct Form8 {
+    static constexpr int FMT = FMT_, DP = DP_, RG = RG_, QT = QT_, NP = 3, QP = QT == EL_F32 ? 3 : 1;
     static constexpr bool FAST = FAST_;
     static constexpr int LDS = RG * DP * 64 + 256;                   // of a wavefront that shares its sequence: results, (m, l)
     // wavefronts that a compute unit holds, by registers (twelve of 128 columns would fit: 91 us for 86 with eight, 64 sequences of 1024 to 4096 on 8 key heads)
@@ -582,16 +585,15 @@ __global__ void __launch_bounds__(64 * F::WAVES, F::PER_CU / 4) k_coded_attend(c
 bool is_fast(const el_attn_pages8 &c) { return c.page_size % 8 == 0 && c.block % 8 == 0; }
 
 template <class Fn>
-void with_form8(const el_attn_pages8 &c, int dtype, int out_dtype, int row_groups, Fn fn)
+void with_form8(const el_attn_pages8 &c, int dtype, int row_groups, Fn fn)
 {
     auto parts = [&](auto fmt, auto width, auto rg) {
         constexpr int FMT = decltype(fmt)::value, DP = decltype(width)::value, RG = decltype(rg)::value;
-        if (!is_fast(c)) { if constexpr (RG == 1) fn(Form8<FMT, DP, 1, EL_F32, 3, false>{}); }
+        if (!is_fast(c)) { if constexpr (RG == 1) fn(Form8<FMT, DP, 1, EL_F32, false>{}); }
         else if constexpr (DP < 256 || RG == 1) {
-            if (dtype == EL_F32) fn(Form8<FMT, DP, RG, EL_F32, 3, true>{});
-            else if (dtype == EL_F16) { if (out_dtype == EL_F32) fn(Form8<FMT, DP, RG, EL_F16, 3, true>{}); else fn(Form8<FMT, DP, RG, EL_F16, 2, true>{}); }
-            else if (out_dtype == EL_F32) fn(Form8<FMT, DP, RG, EL_BF16, 3, true>{});
-            else fn(Form8<FMT, DP, RG, EL_BF16, 2, true>{});
+            if (dtype == EL_F32) fn(Form8<FMT, DP, RG, EL_F32, true>{});
+            else if (dtype == EL_F16) fn(Form8<FMT, DP, RG, EL_F16, true>{});
+            else fn(Form8<FMT, DP, RG, EL_BF16, true>{});
         }
     };
     auto rows = [&](auto fmt, auto width) {
@@ -607,7 +609,7 @@ void with_form8(const el_attn_pages8 &c, int dtype, int out_dtype, int row_group
     else widths(std::integral_constant<int, EL_INT8>{});
 }
 
-AttendPlan plan_attend8(const el_attn_pages8 &c, int dtype, int out_dtype, int heads, int B, int beam, int n)
+AttendPlan plan_attend8(const el_attn_pages8 &c, int dtype, int heads, int B, int beam, int n)
 {
     const int R = beam * (heads / c.kv_heads);
     SpanForm form{};
@@ -615,7 +617,7 @@ AttendPlan plan_attend8(const el_attn_pages8 &c, int dtype, int out_dtype, int h
     // two groups of rows share a tile's codes; 256 columns leave no registers for them, and without FAST there is one form
     form.row_groups = R <= 16 || !is_fast(c) || form.padded == 256 ? 1 : 2;
     form.tile = TP;
-    with_form8(c, dtype, out_dtype, form.row_groups, [&](auto f) { form.per_cu = f.PER_CU; form.most = f.WAVES; form.lds = f.LDS; });
+    with_form8(c, dtype, form.row_groups, [&](auto f) { form.per_cu = f.PER_CU; form.most = f.WAVES; form.lds = f.LDS; });
     AttendPlan p = plan_spans(form, R, c.kv_heads, c.d_head, form.padded, c.head_stride, B, n);
     if (p.waves == 1) p.lds = 0;
     return p;
@@ -632,7 +634,7 @@ bool valid_types(int32_t dtype, int32_t out_dtype)
 extern "C" size_t el_attn_quantized_workspace_bytes(const el_attn_pages8 *cache, int32_t dtype, int32_t out_dtype, int32_t heads, int32_t B, int32_t beam, int32_t n)
 {
     if (el::check_pages8(cache) != EL_OK || !el::valid_types(dtype, out_dtype) || !el::valid_sizes(cache->kv_heads, heads, B, beam, n)) return 0;
-    return el::plan_attend8(*cache, dtype, out_dtype, heads, B, beam, n).workspace;
+    return el::plan_attend8(*cache, dtype, heads, B, beam, n).workspace;
 }
 
 extern "C" el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32_t dtype,
@@ -646,7 +648,7 @@ extern "C" el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32
     if (!valid_types(dtype, out_dtype)) return EL_ERR_UNSUPPORTED;
     const AttendOperands o{table, table_stride, table_pages, lengths, queries, query_stride, heads, dtype, rule, out, out_dtype, lse, B, beam, n};
     if (const el_status st = check_attend(o, cache->kv_heads, cache->d_head, cache->page_size); st != EL_OK) return st;
-    const AttendPlan p = plan_attend8(*cache, dtype, out_dtype, heads, B, beam, n);
+    const AttendPlan p = plan_attend8(*cache, dtype, heads, B, beam, n);
     if (p.workspace) {
         if (!workspace || workspace_bytes < p.workspace) return EL_ERR_WORKSPACE;
         if ((uintptr_t)workspace & 15) return EL_ERR_INVALID_ARG;
@@ -658,7 +660,7 @@ extern "C" el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32
     a.step_rest = TP % cache->page_size;
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
-    with_form8(*cache, dtype, out_dtype, p.row_groups, [&](auto f) {
+    with_form8(*cache, dtype, p.row_groups, [&](auto f) {
         hipLaunchKernelGGL((k_coded_attend<decltype(f)>), dim3((unsigned)p.grid), dim3(64 * p.waves), p.lds, s, a);
     });
     if (hipGetLastError() != hipSuccess) return EL_ERR_HIP;

@@ -404,3 +404,19 @@ def test_pools_whose_offsets_pass_32_bits(fmt):
         del cache, K, V
     assert all(torch.equal(a, b) for a, b in zip(*results))
     assert not torch.equal(results[0][0][1], results[0][1][1])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_results_in_16_bits_are_those_in_32_rounded_once(fmt, dtype):
+    """Whatever the result's type, sums and probabilities are the same numbers: with probabilities in fewer bits one result in a thousand was rounded the other way."""
+    import torch
+    element = {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    for k, (B, x, heads, kv, d, page, lengths) in enumerate([(1, 1, 16, 16, 64, 16, [613]), (40, 1, 32, 8, 128, 16, list(range(1, 1600, 40))), (2, 5, 8, 1, 128, 24, [70, 999]),
+                                                             (3, 1, 4, 2, 256, 8, [1, 500, 3001]), (5, 2, 4, 4, 96, 10, [9, 100, 33, 700, 0]), (1, 1, 8, 2, 128, 64, [30001])]):
+        c = Case(200 + k, fmt, dtype, B, x, heads, kv, d, page, page, lengths)
+        got = c.cache.attend(c.q_d, c.table_d, c.lengths_d)
+        want = c.cache.attend(c.q_d, c.table_d, c.lengths_d, out_dtype="f32")
+        torch.cuda.synchronize()
+        differ = int((got != want.to(element)).sum())
+        assert got.dtype == element and differ == 0, f"case {k}: {differ} of {got.numel()}"
