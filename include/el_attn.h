@@ -566,8 +566,9 @@ el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32_t dtype,
  *            NaN in EL_E4M3, 0 in EL_INT8
  *
  * A scale never shrinks while its block fills, so a token's codes do not depend on how many calls brought the block, except for what is rounded again.
- * Earlier positions are those below lengths[b] - counts[b].  Two sequences of one call must not write into the same block: its scale and the codes of both
- * would be lost (copy a shared page first).
+ * Earlier positions are those below lengths[b] - counts[b].  No other sequence, of this call or not, may hold or write positions of a block that is written: a larger
+ * scale changes the earlier codes for all who read them, and of two that write, codes and scale would be lost.  Copy a shared page first
+ * (el_attn_plan_pages_exclusive says which).
  * Errors: as el_attn_paged_append, UNSUPPORTED also for sizes whose grid passes 2^31 workgroups.
  */
 el_status el_attn_quantized_append(const el_attn_pages8 *cache, int32_t dtype,
@@ -584,7 +585,8 @@ el_status el_attn_quantized_copy(const el_attn_pages8 *cache, const int32_t *src
  *
  * From what every sequence holds and how many positions it needs: the next table, on the device.  Nothing is kept between calls: a page is in use if an
  * entry of the new sequences names it (below their lengths) or `reserved` does; every other one is free.  So a sequence that ends gives its pages
- * back by not being named as a parent, and a beam that forks shares its parent's pages until one of the two writes.
+ * back by not being named as a parent, and a beam that forks shares its parent's pages, the last one until one of the two writes into positions that
+ * the other has.
  *
  *   table     [B_old, columns] int32, rows table_stride apart; lengths [B_old] int32 (outside [0, columns * page_size]: the nearer end)
  *   parents   [B] int32: new sequence b goes on from old sequence parents[b]; outside [0, B_old): a new one of length 0.  NULL: itself (B <= B_old)
@@ -603,12 +605,20 @@ el_status el_attn_quantized_copy(const el_attn_pages8 *cache, const int32_t *src
  * number that writes too holds as many, and it is not reserved; otherwise it gets a page of its own, and a copy.  An absent page that it writes into is
  * replaced without one.  Free pages are handed out from the lowest number up, sequences in order; the first that the free pages do not suffice for, and every later one
  * that needs a page, get nothing; so does one whose positions the columns do not hold, without changing what the others get.
+ * For a cache in 8 bits (el_attn_quantized_append) take el_attn_plan_pages_exclusive, all the same but for this rule: a write there changes the scale of a block, and
+ * with it the codes of positions that a sequence may share which writes nothing, or is granted nothing.  A partly filled page that is written is kept only if no other
+ * entry of the new sequences names it and it is not reserved; every other writer gets a page of its own, and a copy, or where no page is left nothing.
+ *
  * `workspace`: el_attn_plan_workspace_bytes, 16-byte aligned, any contents, used by this call only.
  * What is written must not overlap what is read.  Errors: INVALID_ARG (null or misaligned operands, sizes < 1, B or B_old beyond 2^20, B beyond B_old without
  * parents, pages beyond 2^24, T beyond 2^23, columns beyond 2^24, B * columns beyond 2^31, columns * page_size beyond 2^31 - 1), WORKSPACE, HIP.
  */
 size_t el_attn_plan_workspace_bytes(int32_t B, int32_t pages);
 el_status el_attn_plan_pages(const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
+                             const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size, int32_t B, int32_t T,
+                             int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots, int32_t *copies, int32_t *free_pages,
+                             void *workspace, size_t workspace_bytes, void *stream);
+el_status el_attn_plan_pages_exclusive(const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
                              const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size, int32_t B, int32_t T,
                              int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots, int32_t *copies, int32_t *free_pages,
                              void *workspace, size_t workspace_bytes, void *stream);

@@ -431,8 +431,9 @@ def quantized_copy_reference(codes, scale, src, dst, counts, block):
 
 
 # ---- the table of the next step ------------------------------------------------------------------------------------------
-def plan_pages_reference(table, lengths, counts, parents, reserved, pages, page_size, T):
-    """dict of table, lengths, granted, slots, copies, free, as whole numbers, one sequence after the other."""
+def plan_pages_reference(table, lengths, counts, parents, reserved, pages, page_size, T, exclusive=False):
+    """dict of table, lengths, granted, slots, copies, free, as whole numbers, one sequence after the other.  exclusive: a page that is written is kept only if one
+    entry names it."""
     B_old, columns = table.shape
     parents = list(range(B_old)) if parents is None else [int(p) for p in parents]
     B = len(parents)
@@ -465,6 +466,8 @@ def plan_pages_reference(table, lengths, counts, parents, reserved, pages, page_
             page = rows[b][held - 1]
             if page < 0 or (reserved is not None and reserved[page]):
                 replaced = True
+            elif exclusive:
+                replaced = len(users[page]) > 1
             else:
                 most = max(e for e, _, _ in users[page])
                 keeper = min([s for e, w, s in users[page] if e == most and w], default=None)

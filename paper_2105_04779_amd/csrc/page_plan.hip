@@ -5,7 +5,8 @@
 // every sequence's need added up; entries, slots.  512 requests of up to 8192 positions on 1.5 times the pages they need: 2.6 + 8.0 + 6.0 + 6.3 us.
 //
 // A mark is the largest of the keys (positions of the page in use, written?, lowest sequence first) of those that name it: a page is its writer's to keep if the
-// mark is the writer's own key.  Maxima and whole-number sums: the result does not depend on the order in which anything runs.
+// mark is the writer's own key.  Where a write changes more than the positions written (a cache in 8 bits), it is the number of entries that name the page, and a page is
+// its writer's to keep if that is 1.  Maxima and whole-number sums: the result does not depend on the order in which anything runs.
 #include "el_internal.h"
 
 namespace el {
@@ -23,6 +24,7 @@ struct PlanArgs {
     const int32_t *lengths, *parents, *counts;
     const uint8_t *reserved;
     int columns, B_old, pages, page_size, B, T, chunks;
+    bool exclusive;                      // a page that is written is named once
     int32_t *new_table, *new_lengths, *granted, *copies, *free_pages;
     int64_t *slots;
     Mark *marks;                         // [pages]
@@ -58,6 +60,13 @@ __device__ __forceinline__ Mark key_of(const PlanArgs &a, const Ask &s, int j, i
     const int extent = min(a.page_size, s.had - j * a.page_size);
     return (Mark)extent << 32 | (j == s.held - 1 && writes_last(a, s) ? (1u << 31) + (unsigned)(kMaxSequences - b) : 0u);
 }
+__device__ __forceinline__ void mark(const PlanArgs &a, Mark *at, const Ask &s, int j, int b)
+{
+    if (a.exclusive) atomicAdd(at, (Mark)1);
+    else atomicMax(at, key_of(a, s, j, b));
+}
+// Is a page with this mark, the last of s, the writer's to keep?
+__device__ __forceinline__ bool keeps(const PlanArgs &a, Mark m, const Ask &s, int b) { return m == (a.exclusive ? (Mark)1 : key_of(a, s, s.held - 1, b)); }
 
 __global__ void __launch_bounds__(256) k_plan_clear(Mark *marks, int pages)
 {
@@ -72,7 +81,7 @@ __global__ void __launch_bounds__(kLanes) k_plan_mark(const PlanArgs a)
         for (int j = blockIdx.x * kLanes + threadIdx.x; j < a.columns; j += gridDim.x * kLanes) {
             const int e = entry(a, s, j);
             a.new_table[(int64_t)b * a.columns + j] = e;
-            if (e >= 0) atomicMax(&a.marks[e], key_of(a, s, j, b));
+            if (e >= 0) mark(a, &a.marks[e], s, j, b);
         }
     }
 }
@@ -120,7 +129,7 @@ __global__ void __launch_bounds__(kLanes) k_plan_count(const PlanArgs a)
         const Ask s = ask(a, b);
         if (writes_last(a, s)) {
             const int e = entry(a, s, s.held - 1);
-            replaced = e < 0 || (a.reserved && a.reserved[e]) || a.marks[e] != key_of(a, s, s.held - 1, b);
+            replaced = e < 0 || (a.reserved && a.reserved[e]) || !keeps(a, a.marks[e], s, b);
         }
         if (s.count > 0) need = s.held_then - s.held + replaced;
     }
@@ -233,7 +242,7 @@ __global__ void __launch_bounds__(kSmallLanes) k_plan_small(const PlanArgs a)
         const Ask s = ask(a, b);
         const int e = entry(a, s, j);
         a.new_table[i] = e;
-        if (e >= 0) atomicMax(&marks[e], key_of(a, s, j, b));
+        if (e >= 0) mark(a, &marks[e], s, j, b);
     }
     __syncthreads();
     int64_t available, all;
@@ -256,7 +265,7 @@ __global__ void __launch_bounds__(kSmallLanes) k_plan_small(const PlanArgs a)
         s = ask(a, tid);
         if (writes_last(a, s)) {
             last = entry(a, s, s.held - 1);
-            replaced = last < 0 || (a.reserved && a.reserved[last]) || marks[last] != key_of(a, s, s.held - 1, tid);
+            replaced = last < 0 || (a.reserved && a.reserved[last]) || !keeps(a, marks[last], s, tid);
         }
         if (s.count > 0) need = s.held_then - s.held + replaced;
     }
@@ -316,21 +325,12 @@ PlanSpace plan_space(int32_t B, int32_t pages)
     return p;
 }
 
-} // namespace
-} // namespace el
-
-extern "C" size_t el_attn_plan_workspace_bytes(int32_t B, int32_t pages)
+// The checks and launches of both calls.
+el_status plan(bool exclusive, const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
+               const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size,
+               int32_t B, int32_t T, int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots,
+               int32_t *copies, int32_t *free_pages, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (B < 1 || B > el::kMaxSequences || pages < 1 || pages > el::kMaxPages) return 0;
-    return el::plan_space(B, pages).total;
-}
-
-extern "C" el_status el_attn_plan_pages(const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
-                                        const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size,
-                                        int32_t B, int32_t T, int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots,
-                                        int32_t *copies, int32_t *free_pages, void *workspace, size_t workspace_bytes, void *stream)
-{
-    using namespace el;
     if (!table || !lengths || !new_table || !new_lengths || !granted || !copies || !free_pages) return EL_ERR_INVALID_ARG;
     if (columns < 1 || columns > 1 << 24 || B_old < 1 || B_old > kMaxSequences || B < 1 || B > kMaxSequences || T < 1 || T > 1 << 23 ||
         pages < 1 || pages > kMaxPages || page_size < 1 || (int64_t)columns * page_size > INT32_MAX || (int64_t)B * columns > ((int64_t)1 << 31)) return EL_ERR_INVALID_ARG;
@@ -342,7 +342,7 @@ extern "C" el_status el_attn_plan_pages(const int32_t *table, int64_t table_stri
     if (!workspace || workspace_bytes < p.total) return EL_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15) return EL_ERR_INVALID_ARG;
     char *const w = (char *)workspace;
-    const PlanArgs a{table, table_stride, lengths, parents, counts, reserved, columns, B_old, pages, page_size, B, T, p.chunks,
+    const PlanArgs a{table, table_stride, lengths, parents, counts, reserved, columns, B_old, pages, page_size, B, T, p.chunks, exclusive,
                      new_table, new_lengths, granted, copies, free_pages, slots, (Mark *)(w + p.marks), (int32_t *)(w + p.list), (int32_t *)(w + p.count),
                      (int64_t *)(w + p.before), (int64_t *)(w + p.block_need), (int32_t *)(w + p.need)};
     const hipStream_t s = (hipStream_t)stream;
@@ -359,4 +359,31 @@ extern "C" el_status el_attn_plan_pages(const int32_t *table, int64_t table_stri
     hipLaunchKernelGGL(k_plan_count, dim3(p.chunks + blocks), dim3(kLanes), 0, s, a);
     hipLaunchKernelGGL(k_plan_assign, dim3(B + 1), dim3(kLanes), 0, s, a);
     return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
+}
+
+} // namespace
+} // namespace el
+
+extern "C" size_t el_attn_plan_workspace_bytes(int32_t B, int32_t pages)
+{
+    if (B < 1 || B > el::kMaxSequences || pages < 1 || pages > el::kMaxPages) return 0;
+    return el::plan_space(B, pages).total;
+}
+
+extern "C" el_status el_attn_plan_pages(const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
+                                        const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size,
+                                        int32_t B, int32_t T, int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots,
+                                        int32_t *copies, int32_t *free_pages, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return el::plan(false, table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T, new_table, new_lengths, granted,
+                    slots, copies, free_pages, workspace, workspace_bytes, stream);
+}
+
+extern "C" el_status el_attn_plan_pages_exclusive(const int32_t *table, int64_t table_stride, int32_t columns, const int32_t *lengths, int32_t B_old,
+                                                  const int32_t *parents, const int32_t *counts, const uint8_t *reserved, int32_t pages, int32_t page_size,
+                                                  int32_t B, int32_t T, int32_t *new_table, int32_t *new_lengths, int32_t *granted, int64_t *slots,
+                                                  int32_t *copies, int32_t *free_pages, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return el::plan(true, table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T, new_table, new_lengths, granted,
+                    slots, copies, free_pages, workspace, workspace_bytes, stream);
 }

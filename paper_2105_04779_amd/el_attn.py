@@ -31,7 +31,7 @@ EXPORTED_SYMBOLS = (
     "el_attn_paged_workspace_bytes", "el_attn_paged_attend", "el_attn_paged_append", "el_attn_paged_copy",
     "el_attn_max_alternatives", "el_attn_score_workspace_bytes", "el_attn_score_tokens",
     "el_attn_quantized_workspace_bytes", "el_attn_quantized_attend", "el_attn_quantized_append", "el_attn_quantized_copy",
-    "el_attn_plan_workspace_bytes", "el_attn_plan_pages", "el_attn_sample_workspace_bytes", "el_attn_sample_tokens",
+    "el_attn_plan_workspace_bytes", "el_attn_plan_pages", "el_attn_plan_pages_exclusive", "el_attn_sample_workspace_bytes", "el_attn_sample_tokens",
     "el_attn_destroy", "el_attn_status_string", "el_attn_version",
 )
 
@@ -162,8 +162,9 @@ def _load():
     lib.el_attn_quantized_copy.restype = ctypes.c_int
     lib.el_attn_plan_workspace_bytes.argtypes = [i32, i32]
     lib.el_attn_plan_workspace_bytes.restype = sz
-    lib.el_attn_plan_pages.argtypes = [vp, i64, i32, vp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    lib.el_attn_plan_pages.restype = ctypes.c_int
+    for plan in (lib.el_attn_plan_pages, lib.el_attn_plan_pages_exclusive):
+        plan.argtypes = [vp, i64, i32, vp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        plan.restype = ctypes.c_int
     lib.el_attn_sample_workspace_bytes.argtypes = [ctypes.c_int, i32, i32]
     lib.el_attn_sample_workspace_bytes.restype = sz
     lib.el_attn_sample_tokens.argtypes = [ctypes.c_int, vp, i64, i32, i32, vp, ctypes.POINTER(ElAttnSampleRule), vp, vp, vp, sz, vp]
@@ -347,6 +348,12 @@ def el_attn_plan_workspace_bytes(B, pages) -> int:
 def el_attn_plan_pages(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
                        new_table, new_lengths, granted, slots, copies, free_pages, workspace=None, workspace_bytes=0, stream=None) -> int:
     return lib.el_attn_plan_pages(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
+                                  new_table, new_lengths, granted, slots, copies, free_pages, workspace, workspace_bytes, stream)
+
+
+def el_attn_plan_pages_exclusive(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
+                       new_table, new_lengths, granted, slots, copies, free_pages, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib.el_attn_plan_pages_exclusive(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
                                   new_table, new_lengths, granted, slots, copies, free_pages, workspace, workspace_bytes, stream)
 
 
@@ -719,7 +726,8 @@ class PagedCache8(_Pages):
 
     def append(self, k, v, table, lengths, counts=None):
         """New tokens as in PagedCache.append, rounded to codes: a block's scale is its largest value over the largest code, and grows (what the block
-        holds is rounded again) where a later token needs it.  No two sequences of a call may write into one block."""
+        holds is rounded again) where a later token needs it.  No other sequence may hold or write positions of a block that is written:
+        plan_pages with exclusive=True sees to that."""
         self._append("el_attn_quantized_append", lib.el_attn_quantized_append, (self._pages, _dtype_code(k)), k.dtype, k, v, table, lengths, counts)
 
     def _query_type(self, queries):
@@ -740,14 +748,16 @@ PagePlan.__doc__ = """The table of a step (see plan_pages): table [B, columns], 
 page * page_size + place, -1 for none), copies [3, B] (the operands of copy_pages), free [1] pages left; int32 where not said otherwise."""
 
 
-def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, parents=None, reserved=None, slots=True):
+def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, parents=None, reserved=None, slots=True, exclusive=False):
     """The next step's table from what every sequence holds and needs, on the device (see el_attn_plan_pages).
 
     table int32 [B_old, columns] (rows strided, a row contiguous) and lengths int32 [B_old]: what the sequences hold.  parents int32 [B] (None: each goes on
     from itself): whom sequence b goes on from; -1 starts a new one.  counts int32 [B] (None: `tokens` each): positions that it needs, up to `tokens`.
     pages, page_size: of the pool; reserved uint8 or bool [pages]: pages that others use.  A page that the new sequences do not name is free.
+    exclusive: a page that is written is kept only if nothing else names it.  A PagedCache8 needs that: what it holds of a block is rounded again when a larger token comes,
+    also for a sequence that shares the block and writes nothing.  A PagedCache does without: sequences may share what they have in common of a page.
 
-        plan = plan_pages(table, lengths, counts, pages=cache.K.shape[0], page_size=cache.page_size, parents=parents)
+        plan = plan_pages(table, lengths, counts, pages=cache.K.shape[0], page_size=cache.page_size, parents=parents, exclusive=isinstance(cache, PagedCache8))
         cache.copy_pages(*plan.copies)
         cache.append(k, v, plan.table, plan.lengths, plan.granted)
 
@@ -774,7 +784,8 @@ def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, paren
     nbytes = lib.el_attn_plan_workspace_bytes(B, pages)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     at = small.data_ptr()
-    _call("el_attn_plan_pages", device, lib.el_attn_plan_pages, table.data_ptr(), table.stride(0) if B_old > 1 else columns, columns, lengths.data_ptr(), B_old,
+    where, fn = ("el_attn_plan_pages_exclusive", lib.el_attn_plan_pages_exclusive) if exclusive else ("el_attn_plan_pages", lib.el_attn_plan_pages)
+    _call(where, device, fn, table.data_ptr(), table.stride(0) if B_old > 1 else columns, columns, lengths.data_ptr(), B_old,
           _ptr(parents), _ptr(counts), _ptr(reserved), pages, page_size, B, tokens, new_table.data_ptr(), at, at + 4 * B, _ptr(places), at + 8 * B, at + 20 * B,
           ws.data_ptr(), nbytes)
     new_lengths, granted, copies, free = torch.split_with_sizes(small, (B, B, 3 * B, 1))
