@@ -633,7 +633,7 @@ el_status el_attn_plan_pages_exclusive(const int32_t *table, int64_t table_strid
  *   top_p   of these the shortest beginning whose weights reach top_p times their sum
  *   min_p   of these those with w_v >= min_p (relative to the largest); the first in order always stays
  *   token   the first index v, in the order of the vocabulary, at which the sum of the weights left passes uniform times their total
- *   logprob log(w_token / total)
+ *   logprob log(w_token / total): w_token from its logit, total off by the roundings of its weights (2^-44 of the largest each), rounded to fp32
  *
  *   logits   as for el_attn_score_tokens: any row alignment, vocab up to 2^19
  *   uniform  [rows] float32, in [0, 1); below: the first token left; 1 or more, or NaN: the last

@@ -380,7 +380,11 @@ static __device__ __forceinline__ void run(const SampleArgs &a)
     }
     const Weight weight(a.powers, m, temperature);
     const double low = min_p > 0.f ? (double)min_p * (double)kOne : 0.0;                 // weights that min-p leaves
-    auto write = [&](int v, u64 wv, u64 total) { a.tokens[r] = v; if (a.logprob) a.logprob[r] = (float)log((double)wv / (double)total); };
+    // (from the logit: an unlikely token's weight is few units, which its logarithm would show.  The total is 1 or more and off by 2^-44 a token)
+    auto write = [&](int v, float x, u64 total) {
+        a.tokens[r] = v;
+        if (a.logprob) a.logprob[r] = (float)(((double)x - (double)m) / (double)temperature - log((double)total * (1.0 / (double)kOne)));
+    };
     const bool by_count = k > 0 && k < row.vocab, by_weight = top_p < 1.f;
 
     if (by_count && k <= kFewTokens) {
@@ -416,7 +420,7 @@ static __device__ __forceinline__ void run(const SampleArgs &a)
             }
             __syncthreads();
             const int chosen = s.token != 0x7fffffff ? s.token : s.cross;
-            if (kept && wv && v == chosen) write(v, wv, left);
+            if (kept && wv && v == chosen) write(v, value_of((unsigned)(key >> 32)), left);
             return;
         }
         __syncthreads();
@@ -688,16 +692,16 @@ static __device__ __forceinline__ void run(const SampleArgs &a)
     base += sum_before(s, sum, all);
     if (sum && !((double)base > target && base) && ((double)(base + sum) > target || base + sum == total)) {
         int chosen = 0;
-        u64 wv = 0;
+        float logit = m;
         walk([&](float x, int v) {
             if (!(x > least) && !(x == least && base_ties++ < equal)) return false;
             const u64 wx = weight(x);
             if (!wx) return false;
-            chosen = v; wv = wx;
+            chosen = v; logit = x;
             base += wx;
             return (double)base > target;
         });
-        write(chosen, wv, total);
+        write(chosen, logit, total);
     }
 }
 };

@@ -192,3 +192,30 @@ def test_refusals_and_no_rows():
         el_attn.sample_tokens(x, torch.zeros(5, device="cuda"))
     with pytest.raises(ValueError, match="gradient"):
         el_attn.sample_tokens(x.clone().requires_grad_(), u)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("copies", [1, 40])                          # (40: more rows than compute units)
+def test_log_probabilities_of_unlikely_tokens(dtype, copies):
+    """A random number of 0 draws the first token that has a weight, however small.  Its log-probability is off by the rounding to fp32, 2^-24 of itself, and by the total's: its
+    weights are off by 2^-44 and the exponential's 2^-44.6 of themselves, all of them at most 1, and the total is at least 1."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    g = np.random.default_rng(23)
+    V = 300
+    gaps = np.array([3.0, 11.0, 17.5, 20.75, 23.0, 25.5, 27.25, 29.0, 30.0])
+    for temperature in (1.0, 0.5, 1.75):
+        for rule, banned in ((dict(), 0.0), (dict(top_k=50), 0.9), (dict(top_k=200), 0.5), (dict(min_p=5e-14), 0.0), (dict(top_k=250, min_p=5e-14), 0.3)):
+            x = g.uniform(-9.0, -1.0, (len(gaps), V)) * temperature
+            x[g.random(x.shape) < banned] = -np.inf
+            x[:, 0], x[:, 5] = -gaps * temperature, 0.0
+            x = np.repeat(wl.round_to_storage(x.astype(np.float32), dtype), copies, 0)
+            assert (np.isfinite(x).sum(1) < rule.get("top_k", V + 1)).all()                # top-k leaves all
+            z = x.astype(np.float64) / temperature
+            want = z[:, 0] - np.log(np.exp(z).sum(1))
+            tokens, logprob = el_attn.sample_tokens(to_device(x, dtype), torch.zeros(len(x), device="cuda"), temperature=temperature, **rule)
+            torch.cuda.synchronize()
+            assert (tokens == 0).all(), (temperature, rule)
+            err = np.abs(logprob.cpu().numpy() - want) / (2.0 ** -24 * np.abs(want) + V * (2.0 ** -44 + 2.0 ** -44.6) + 2.0 ** -48)
+            record(f"unlikely tokens {dtype} T {temperature} {rule}: {err.max():.3f} of the bound")
+            assert err.max() <= 1.0, (temperature, rule, err.reshape(-1, copies)[:, 0])
