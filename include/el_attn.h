@@ -569,7 +569,7 @@ el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32_t dtype,
  * Earlier positions are those below lengths[b] - counts[b].  No other sequence, of this call or not, may hold or write positions of a block that is written: a larger
  * scale changes the earlier codes for all who read them, and of two that write, codes and scale would be lost.  Copy a shared page first
  * (el_attn_plan_pages_exclusive says which).
- * Errors: as el_attn_paged_append, UNSUPPORTED also for sizes whose grid passes 2^31 workgroups.
+ * Errors: as el_attn_paged_append, UNSUPPORTED also where G = ceil(kv_heads * (blocks that T positions may touch) / 2) reaches 2^24, or G * B passes 2^31 - 1.
  */
 el_status el_attn_quantized_append(const el_attn_pages8 *cache, int32_t dtype,
                                 const int32_t *table, int64_t table_stride, int32_t table_pages,

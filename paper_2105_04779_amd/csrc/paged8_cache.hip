@@ -222,7 +222,7 @@ extern "C" el_status el_attn_quantized_append(const el_attn_pages8 *cache, int32
                                               (int64_t)dtype_size(dtype), B, T); st != EL_OK) return st;
     const int64_t es = (int64_t)dtype_size(dtype), blocks = ((int64_t)T + cache->block - 2) / cache->block + 1;
     const int64_t groups = (blocks * cache->kv_heads * 2 + 3) / 4;
-    if (groups > INT32_MAX || groups * B > INT32_MAX) return EL_ERR_UNSUPPORTED;                     // (grid)
+    if (groups >= 1 << 24 || groups * B > INT32_MAX) return EL_ERR_UNSUPPORTED;                      // (a launch has fewer than 2^32 lanes a dimension)
     const int per_row = cache->d_head * (int)es / 16;
     const Append8Args a{page_view8(*cache, table, table_stride, table_pages), scale_view(*cache), lengths, counts, (const char *)K_new, (const char *)V_new,
                         batch_stride * es, token_stride * es, cache->kv_heads, cache->d_head, T, (int)blocks, per_row, 64 / per_row, 64 % per_row};

@@ -95,6 +95,14 @@ def test_append_and_copy_refuse_bad_operands(ea):
         assert call(c, **bad) == I, bad
 
 
+def test_append_refuses_what_a_launch_cannot_hold(ea):
+    """A workgroup of 256 lanes has four (block, head, K or V): 2^24 workgroups would be 2^32 lanes."""
+    call, wide = _calls(ea)["append"], dict(block=1, kv_heads=32, position_stride=32 * 128, page_stride=16 * 32 * 128)
+    token = dict(token_stride=32 * 128, batch_stride=1 << 36)
+    for B, T in ((1, 1 << 20), (1, (1 << 20) + 1), (3, 1 << 20), (1, 1 << 23)):          # T blocks, 16 T workgroups
+        assert call(_pages(ea, **wide), B=B, T=T, **token) == ea.EL_ERR_UNSUPPORTED, (B, T)
+
+
 def test_plan_refuses_bad_operands(ea):
     I = ea.EL_ERR_INVALID_ARG
 
