@@ -29,6 +29,7 @@ namespace {
 constexpr int kBins = 512;
 constexpr int kEach = 512;               // tokens that a wavefront collects
 constexpr int kComputeUnits = 256;
+constexpr int kRowsOfLaunch = 1 << 22;   // a launch has fewer than 2^32 lanes
 constexpr int kOrdered = 4096;           // rows up to which those that take longer are begun first
 constexpr int kFewTokens = 128;          // top-k up to which the bound from the lanes' maxima is used
 constexpr int32_t kMaxVocab = 1 << 19;
@@ -736,11 +737,17 @@ extern "C" el_status el_attn_sample_tokens(el_dtype dtype, const void *logits, i
          (uintptr_t)rule->row_top_p | (uintptr_t)rule->row_min_p) & 3) return EL_ERR_INVALID_ARG;
     if (!rule->row_temperature && !(rule->temperature >= 0.f && rule->temperature < INFINITY)) return EL_ERR_INVALID_ARG;
     (void)workspace; (void)workspace_bytes;
-    const SampleArgs a{(const char *)logits, row_stride * es, vocab, uniform, *rule, tokens, logprob, kPowers, rows,
-                       rows > kComputeUnits && rows <= kOrdered && (rule->row_top_k || rule->row_top_p)};
     const hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();      // errors other libraries left behind in this thread are not this launch's
-    if (rows > kComputeUnits) launch_sample<512>(a, dtype, rows, s);
-    else launch_sample<1024>(a, dtype, rows, s);
+    for (int32_t first = 0; first < rows; first += kRowsOfLaunch) {
+        const int32_t n = rows - first < kRowsOfLaunch ? rows - first : kRowsOfLaunch;
+        auto from = [&](auto *p) { return p ? p + first : nullptr; };
+        const el_attn_sample_rule here{rule->temperature, rule->top_k, rule->top_p, rule->min_p,
+                                       from(rule->row_temperature), from(rule->row_top_k), from(rule->row_top_p), from(rule->row_min_p)};
+        const SampleArgs a{(const char *)logits + first * (row_stride * es), row_stride * es, vocab, uniform + first, here, tokens + first, from(logprob), kPowers, n,
+                           n > kComputeUnits && n <= kOrdered && (rule->row_top_k || rule->row_top_p)};
+        if (n > kComputeUnits) launch_sample<512>(a, dtype, n, s);
+        else launch_sample<1024>(a, dtype, n, s);
+    }
     return hipGetLastError() == hipSuccess ? EL_OK : EL_ERR_HIP;
 }

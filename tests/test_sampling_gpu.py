@@ -219,3 +219,40 @@ def test_log_probabilities_of_unlikely_tokens(dtype, copies):
             err = np.abs(logprob.cpu().numpy() - want) / (2.0 ** -24 * np.abs(want) + V * (2.0 ** -44 + 2.0 ** -44.6) + 2.0 ** -48)
             record(f"unlikely tokens {dtype} T {temperature} {rule}: {err.max():.3f} of the bound")
             assert err.max() <= 1.0, (temperature, rule, err.reshape(-1, copies)[:, 0])
+
+
+@pytest.mark.parametrize("rows", [(1 << 22) + 5, (1 << 23) - 1, 1 << 23])
+def test_as_many_rows_as_there_may_be(rows):
+    """2^23 rows, workgroups of 512 lanes: more than one launch, each with its rows' settings."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    V = 3
+    x = torch.randint(-512, 513, (rows, V), generator=g, device="cuda").to(torch.float16) / 256      # (some ties)
+    way = torch.randint(0, 6, (rows,), generator=g, device="cuda")                        # which setting leaves the largest alone, if one does
+    off = torch.zeros(rows, device="cuda")
+    f = lambda i, value, other: torch.where(way == i, off + value, off + other)
+    tokens, logprob = el_attn.sample_tokens(x, off, temperature=f(1, 0.0, 1.0), top_k=f(2, 1, 0).to(torch.int32), top_p=f(3, 0.0, 1.0), min_p=f(4, 2.0, 0.0))
+    torch.cuda.synchronize()
+    z = x.double()
+    first = (z == z.amax(1, keepdim=True)).to(torch.uint8).argmax(1)                      # ties: the lowest index
+    alone = (way >= 1) & (way <= 4)
+    assert torch.equal(tokens.long(), torch.where(alone, first, 0))                        # a random number of 0 draws the first token
+    want = torch.where(alone, 0.0, z[:, 0] - torch.logsumexp(z, 1))
+    assert ((logprob.double() - want).abs() <= 2.0 ** -24 * want.abs() + V * 2.0 ** -43).all()
+
+
+def test_no_row_follows_from_another_launch():
+    """The first and the last row of 2^22 + 5, drawn alone."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows, V = (1 << 22) + 5, 9
+    x, u = torch.randn((rows, V), generator=g, device="cuda"), torch.rand(rows, generator=g, device="cuda")
+    p = torch.rand(rows, generator=g, device="cuda")
+    tokens, logprob = el_attn.sample_tokens(x, u, top_p=p)
+    for at in (0, 1, (1 << 22) - 2, (1 << 22) - 1, 1 << 22, rows - 2):
+        few = slice(at, at + 2)
+        t, l = el_attn.sample_tokens(x[few], u[few], top_p=p[few])
+        torch.cuda.synchronize()
+        assert torch.equal(tokens[few], t) and torch.equal(logprob[few], l), at
