@@ -256,3 +256,59 @@ def test_no_row_follows_from_another_launch():
         t, l = el_attn.sample_tokens(x[few], u[few], top_p=p[few])
         torch.cuda.synchronize()
         assert torch.equal(tokens[few], t) and torch.equal(logprob[few], l), at
+
+
+def _crowded(kind, rows, V):
+    """Rows most of whose logits fall into one of the 512 ranges that a bound is looked for in, more than a workgroup collects."""
+    g = np.random.default_rng(31)
+    normal = lambda *shape: g.standard_normal(shape)
+    if kind == "near":                                               # many values, few of them equal
+        x = 1.0 + 1e-3 * normal(rows, V)
+    elif kind == "ties":                                             # some dozens of neighbouring fp32 numbers
+        x = 1.0 + 2e-6 * normal(rows, V)
+    elif kind == "two":                                              # two of such clusters: a part of a range is a range of too many again
+        x = np.where(g.random((rows, V)) < 0.5, 1.0, 1.02) + 1e-6 * normal(rows, V)
+    elif kind == "few":                                              # one number among its neighbours, not too many in all
+        x = -9.0 + normal(rows, V)
+        for r in range(rows):
+            at = g.permutation(V)
+            x[r, at[:2500]] = 1.0
+            x[r, at[2500:2540]] = 1.0 + 2.0 ** -23 * (1 + np.arange(40) // 2)
+            x[r, at[2540:2580]] = 1.0 - 2.0 ** -24 * (1 + np.arange(40) // 2)
+            x[r, at[2580:2600]] = 1.0 + g.uniform(-8e-3, 8e-3, 20)
+    else:                                                            # a high temperature
+        x = 2.0 * normal(rows, V)
+    return x.astype(np.float32), g.random(rows, dtype=np.float32), 1000.0 if kind == "hot" else 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,V", [(3, 60000), (2, 200003), (259, 20011)])      # (the last: workgroups of 512 lanes)
+@pytest.mark.parametrize("kind", ["near", "ties", "two", "few", "hot"])
+def test_ranges_of_too_many_are_cut_again(kind, rows, V, dtype):
+    x, u, temperature = _crowded(kind, rows, V)
+    for rule in (dict(top_p=0.9), dict(top_p=0.03), dict(top_k=1501), dict(top_k=V // 2, top_p=0.7), dict(top_p=0.9, min_p=0.9985)):
+        _check(f"crowded {kind} {rows} of {V} {dtype} {rule}", x, dtype, u, temperature=temperature, **rule)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_vocabulary(dtype):
+    """2^19 tokens.  Weights are off by 2^-44 and 2^-44.6 of themselves, at most 1 each, so a sum of V of them by V (2^-44 + 2^-44.6), relative to the row's total."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    V = 1 << 19
+    g = np.random.default_rng(41)
+    x, u = wl.round_to_storage(g.standard_normal((4, V), dtype=np.float32) * np.float32(2), dtype), g.random(4, dtype=np.float32)
+    x[3, g.random(V) < 0.5] = -np.inf
+    full = lambda v, t: np.full(4, v, t)
+    for temperature, k, p, q in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (0.5, 300000, 0.99, 0.0), (1.0, 50, 1.0, 0.0), (1.5, 0, 1.0, 0.01)):
+        want, want_logprob, margin = oracle.sample_tokens_reference(x, u, full(temperature, np.float32), full(k, np.int32), full(p, np.float32), full(q, np.float32))
+        tokens, logprob = el_attn.sample_tokens(to_device(x, dtype), torch.from_numpy(u).cuda(), temperature=temperature, top_k=k, top_p=p, min_p=q)
+        torch.cuda.synchronize()
+        z = (x - x.max(1, keepdims=True)).astype(np.float64) / temperature
+        n = min(k, V) if k else V
+        off = V * (2.0 ** -44 + 2.0 ** -44.6) / np.sort(np.exp(z), 1)[:, V - n:].sum(1) / p
+        assert (margin > off).all(), (margin, off)
+        assert np.array_equal(tokens.cpu().numpy(), want), (temperature, k, p, q)
+        err = np.abs(logprob.cpu().numpy() - want_logprob) / (2.0 ** -24 * np.abs(want_logprob) + off)
+        record(f"vocabulary 2^19 {dtype} T {temperature} k {k} p {p} min-p {q}: {err.max():.3f} of the bound")
+        assert err.max() <= 1.0
