@@ -762,7 +762,7 @@ def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, paren
         cache.append(k, v, plan.table, plan.lengths, plan.granted)
 
     Returns a PagePlan of new tensors (slots=False: None in the place of its slots).  Where the free pages do not suffice, the first sequences
-    are served: granted is 0 for the others. """
+    are served: granted is 0 for the others.  No sequence, of the old or of the new, is no error."""
     import torch
     shape, device, i32 = table.shape, table.device, torch.int32
     if len(shape) != 2 or not table.is_cuda or table.dtype is not i32 or (shape[1] > 1 and table.stride(1) != 1):
@@ -776,8 +776,13 @@ def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, paren
         _check_index("counts", counts, device, (B,))
     if reserved is not None and (reserved.dtype not in (torch.uint8, torch.bool) or reserved.device != device or reserved.shape != (pages,) or not reserved.is_contiguous()):
         raise ValueError(f"reserved must be a contiguous uint8 or bool tensor [{pages}] on {device}")
-    if max(pages, page_size, tokens, columns, B, B_old) > _INT32_MAX or min(B, B_old, columns) < 1:
-        raise ValueError("sizes must be 32-bit numbers, with at least one sequence and one column")
+    if max(pages, page_size, tokens, columns, B, B_old) > _INT32_MAX or columns < 1:
+        raise ValueError("sizes must be 32-bit numbers, with at least one column")
+    if B_old == 0:                                                   # there is none to go on from
+        table, lengths, B_old, parents = table.new_zeros((1, columns)), lengths.new_zeros(1), 1, lengths.new_full((B,), -1)
+    none = B == 0
+    if none:                                                         # one that needs nothing tells of the free pages
+        parents, counts, B = lengths.new_full((1,), -1), lengths.new_zeros(1), 1
     new_table = torch.empty((B, columns), dtype=i32, device=device)
     small = torch.empty(5 * B + 1, dtype=i32, device=device)         # lengths, granted, copies, free
     places = torch.empty((B, tokens), dtype=torch.int64, device=device) if slots and tokens > 0 else None
@@ -789,7 +794,10 @@ def plan_pages(table, lengths, counts=None, *, pages, page_size, tokens=1, paren
           _ptr(parents), _ptr(counts), _ptr(reserved), pages, page_size, B, tokens, new_table.data_ptr(), at, at + 4 * B, _ptr(places), at + 8 * B, at + 20 * B,
           ws.data_ptr(), nbytes)
     new_lengths, granted, copies, free = torch.split_with_sizes(small, (B, B, 3 * B, 1))
-    return PagePlan(new_table, new_lengths, granted, places, copies.view(3, B), free)
+    copies = copies.view(3, B)
+    if none:
+        return PagePlan(new_table[:0], new_lengths[:0], granted[:0], None if places is None else places[:0], copies[:, :0], free)
+    return PagePlan(new_table, new_lengths, granted, places, copies, free)
 
 
 def _setting(name, value, rows, device, dtype):

@@ -115,3 +115,26 @@ def test_the_same_plan_again_and_on_another_stream():
             el_attn.plan_pages(t, l, c, **{**kw, **bad})
     with pytest.raises(el_attn.ElAttnError):
         el_attn.plan_pages(t.repeat(1, 1), l, None, pages=pages, page_size=1 << 30)
+
+
+@pytest.mark.parametrize("exclusive", [False, True])
+def test_no_sequences_are_no_error(exclusive):
+    import torch
+    from paper_2105_04779_amd import el_attn
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    reserved = torch.tensor([1, 0, 0, 1, 0, 0, 0], dtype=torch.uint8, device="cuda")
+    kw = dict(pages=7, page_size=4, exclusive=exclusive)
+    table, lengths = torch.empty((0, 3), dtype=torch.int32, device="cuda"), i32()
+    for t, n, p in ((table, lengths, None), (table, lengths, i32()), (i32(1, 2, 5).view(1, 3), i32(9), i32())):
+        for slots in (True, False):
+            for r, free in ((None, 7), (reserved, 5)):
+                plan = el_attn.plan_pages(t, n, tokens=2, parents=p, reserved=r, slots=slots, **kw)
+                assert plan.table.shape == (0, 3) and plan.lengths.shape == plan.granted.shape == (0,) and plan.copies.shape == (3, 0)
+                assert (plan.slots.shape == (0, 2)) if slots else plan.slots is None
+                assert plan.free.tolist() == [free] and plan.table.dtype == plan.copies.dtype == torch.int32
+    # the first sequences of all: whoever they name
+    plan = el_attn.plan_pages(table, lengths, i32(5, 0, 2), tokens=5, parents=i32(0, -1, 3), reserved=reserved, **kw)
+    want = oracle.plan_pages_reference(np.zeros((1, 3), int), [0], [5, 0, 2], [-1, -1, -1], [1, 0, 0, 1, 0, 0, 0], 7, 4, 5, exclusive=exclusive)
+    for name in ("table", "lengths", "granted", "slots", "copies"):
+        assert np.array_equal(getattr(plan, name).cpu().numpy(), want[name]), name
+    assert plan.table.tolist() == [[1, 2, -1], [-1, -1, -1], [4, -1, -1]] and plan.free.tolist() == [2]
