@@ -420,3 +420,35 @@ def test_results_in_16_bits_are_those_in_32_rounded_once(fmt, dtype):
         torch.cuda.synchronize()
         differ = int((got != want.to(element)).sum())
         assert got.dtype == element and differ == 0, f"case {k}: {differ} of {got.numel()}"
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page,block,kv,d", [(16, 8, 2, 64), (16, 16, 3, 32), (10, 5, 1, 48), (8, 1, 2, 16)])
+def test_tokens_one_at_a_time_are_the_definition_after_every_token(fmt, dtype, page, block, kv, d):
+    """Blocks whose scale grows with every token, now and then or never: codes are rounded again as the reference rounds them, token by token, to the last code."""
+    import torch
+    from paper_2105_04779_amd import el_attn
+    g = np.random.default_rng(100 + page + block)
+    B, T = 4, 2 * page + 3
+    size = np.stack([2.0 ** (np.arange(T) % block * 0.7), 2.0 ** (-np.arange(T) * 0.3), 2.0 ** g.uniform(-6, 6, T), np.ones(T)])
+    new = [wl.round_to_storage((g.standard_normal((B, T, kv, d)) * size[..., None, None]).astype(np.float32), dtype) for _ in range(2)]
+    pages = 3 * B + 1
+    table = g.permutation(pages)[:3 * B].reshape(B, 3).astype(np.int32)
+    pools = [(g.integers(0, 120, (pages, page, kv, d)).astype(np.int8 if fmt == "int8" else np.uint8), g.random((pages, kv, page // block), dtype=np.float32)) for _ in range(2)]
+    dev = [codes_to_device(c, fmt) for c, _ in pools] + [torch.from_numpy(s.copy()).cuda() for _, s in pools]
+    cache = el_attn.PagedCache8(*dev)
+    k, v = (to_device(x, dtype) for x in new)
+    table_d, again = torch.from_numpy(table).cuda(), 0
+    for t in range(T):
+        lengths = np.array([t + 1] * B)
+        cache.append(k[:, t:t + 1], v[:, t:t + 1], table_d, torch.from_numpy(lengths.astype(np.int32)).cuda())
+        torch.cuda.synchronize()
+        for i in range(2):
+            codes, scale = oracle.quantized_append_reference(*pools[i], table, lengths, None, new[i][:, t:t + 1], block, fmt)
+            again += int((codes != pools[i][0]).any((2, 3)).sum()) - B
+            pools[i] = codes, scale
+            assert np.array_equal(dev[2 + i].cpu().numpy(), scale), (t, i)
+            assert np.array_equal(codes_of(dev[i], fmt), codes), (t, i)
+    record(f"token by token {fmt} {dtype} page {page} block {block}: {again} positions rounded again")
+    assert block == 1 or again > 20
