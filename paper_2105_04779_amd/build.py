@@ -22,9 +22,10 @@ HIPCC_FLAGS = [
 
 
 # kernels that are built around what their wavefronts hold in registers.  (Vector registers: k_attend's instances keep 60 to 120 scalar ones in lanes of
-# vector registers, two or three of which are read back in the loop over tiles.)
+# vector registers, two or three of which are read back in the loop over tiles.  k_sample is not among them: a workgroup of 1024 lanes has 128 registers each, and 10 to
+# 18 numbers that it needs now and then wait in scratch memory, written outside its loops.)
 NO_SPILL_KERNELS = ("k_core_stream", "k_core_short", "k_qelq", "k_vproj", "k_oproj", "k_small_step", "k_gemm_f32",
-                    "k_attend", "k_coded_attend", "k_score_chunk")
+                    "k_attend", "k_coded_attend", "k_score_chunk", "k_append8")
 
 
 def sources():
