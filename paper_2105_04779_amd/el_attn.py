@@ -521,8 +521,8 @@ def _check_pools(K, V):
 
 
 class _Pages:
-    """What the paged caches share: tables, new tokens, queries, copies.  A cache sets _torch, device, page_size, kv_heads, d_head, _pages, and
-    says how its calls are made."""
+    """What the paged caches share: tables, new tokens, queries, copies.  A cache sets _torch, device, page_size, kv_heads, d_head, _pages, and _types: the type that
+    it takes, as a code and as torch's, or None where each call says (a cache in 8 bits).  The calls of the two are written out: the smallest ones are as long as this takes."""
 
     @property
     def K(self):
@@ -542,8 +542,9 @@ class _Pages:
             raise ValueError(f"table must be an int32 tensor on {self.device}")
         return table.data_ptr(), strides[0] if B > 1 else shape[1], shape[1]
 
-    def _append(self, where, fn, head, element, k, v, table, lengths, counts):
+    def _append(self, k, v, table, lengths, counts):
         shape, strides, device = k.shape, k.stride(), self.device
+        code, element = self._types or (_dtype_code(k), k.dtype)
         if len(shape) != 4 or shape != v.shape or shape[2] != self.kv_heads or shape[3] != self.d_head:
             raise ValueError(f"k and v must be [B, T, {self.kv_heads}, {self.d_head}]")
         if strides[3] != 1 or (self.kv_heads > 1 and strides[2] != self.d_head) or v.stride() != strides:
@@ -558,8 +559,12 @@ class _Pages:
         at, stride, columns = self._table(table, B)
         if B == 0 or T == 0:
             return
-        _call(where, device, fn, *head, at, stride, columns, lengths.data_ptr(),
-              _ptr(counts), k.data_ptr(), v.data_ptr(), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
+        if self._types:
+            _call("el_attn_paged_append", device, lib.el_attn_paged_append, self._pages, at, stride, columns, lengths.data_ptr(),
+                  _ptr(counts), k.data_ptr(), v.data_ptr(), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
+        else:
+            _call("el_attn_quantized_append", device, lib.el_attn_quantized_append, self._pages, code, at, stride, columns, lengths.data_ptr(),
+                  _ptr(counts), k.data_ptr(), v.data_ptr(), strides[0] if B > 1 else T * row, strides[1] if T > 1 else row, B, T)
 
     def _attend(self, queries, table, lengths, n, scale, softcap, window, slopes, out, out_code, lse):
         """`queries` has been found to be [B, beam, heads, d_head] of a type that this cache takes."""
@@ -582,20 +587,28 @@ class _Pages:
         if abs(n) > _INT32_MAX or abs(window) > _INT32_MAX:
             raise ValueError("n and window must be 32-bit numbers")
         rule = ElAttnScoreRule(d ** -0.5 if scale is None else scale, softcap, window, _ptr(slopes))
-        where, fn, head, nbytes = self._attend_call(queries, out_code, heads, B, beam, n)
-        ws = self._torch.empty(nbytes, dtype=self._torch.uint8, device=device) if nbytes else None
-        _call(where, device, fn, *head, at, stride, columns, _ptr(lengths),
-              queries.data_ptr(), strides[1] if beam > 1 else strides[0] if B > 1 else heads * d, heads, rule,
-              out.data_ptr(), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
+        if self._types:
+            nbytes = lib.el_attn_paged_workspace_bytes(self._pages, heads, B, beam, n)
+            ws = self._torch.empty(nbytes, dtype=self._torch.uint8, device=device) if nbytes else None
+            _call("el_attn_paged_attend", device, lib.el_attn_paged_attend, self._pages, at, stride, columns, _ptr(lengths),
+                  queries.data_ptr(), strides[1] if beam > 1 else strides[0] if B > 1 else heads * d, heads, rule,
+                  out.data_ptr(), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
+        else:
+            code = _dtype_code(queries)
+            nbytes = lib.el_attn_quantized_workspace_bytes(self._pages, code, out_code, heads, B, beam, n)
+            ws = self._torch.empty(nbytes, dtype=self._torch.uint8, device=device) if nbytes else None
+            _call("el_attn_quantized_attend", device, lib.el_attn_quantized_attend, self._pages, code, at, stride, columns, _ptr(lengths),
+                  queries.data_ptr(), strides[1] if beam > 1 else strides[0] if B > 1 else heads * d, heads, rule,
+                  out.data_ptr(), out_code, _ptr(lse), B, beam, n, _ptr(ws), nbytes)
 
     def _check_queries(self, queries):
         """The queries' type, as a code and as torch's."""
         shape = queries.shape
         if len(shape) != 4 or shape[3] != self.d_head or shape[2] % self.kv_heads != 0:
             raise ValueError(f"queries must be [B, beam, heads, {self.d_head}], heads a multiple of {self.kv_heads}")
-        code, element = self._query_type(queries)
-        _check_values("queries", queries, self.device, element)
-        return code, element
+        types = self._types or (_dtype_code(queries), queries.dtype)
+        _check_values("queries", queries, self.device, types[1])
+        return types
 
     def attend(self, queries, table, lengths, *, n=None, scale=None, softcap=0.0, window=0, slopes=None,
                out_dtype=None, out=None):
@@ -660,21 +673,14 @@ class PagedCache(_Pages):
         self.device = K.device
         pages, self.page_size, self.kv_heads, self.d_head = K.shape
         self.dtype = _dtype_code(K)
-        self._element = K.dtype
+        self._types = self.dtype, K.dtype
         self._pages = ElAttnPages(_ptr(K), _ptr(V), K.stride(0), K.stride(1), K.stride(2),
                                   pages, self.page_size, self.kv_heads, self.d_head, self.dtype)
 
     def append(self, k, v, table, lengths, counts=None):
         """New tokens k, v [B, T, kv_heads, d_head] (heads of a token contiguous, other strides free, the same for both) to
         the positions lengths[b] - counts[b] + i, i < counts[b] (default T): `lengths` counts them already.  B up to 65535."""
-        self._append("el_attn_paged_append", lib.el_attn_paged_append, (self._pages,), self._element, k, v, table, lengths, counts)
-
-    def _query_type(self, queries):
-        return self.dtype, self._element
-
-    def _attend_call(self, queries, out_code, heads, B, beam, n):
-        return ("el_attn_paged_attend", lib.el_attn_paged_attend, (self._pages,),
-                lib.el_attn_paged_workspace_bytes(self._pages, heads, B, beam, n))
+        self._append(k, v, table, lengths, counts)
 
     def copy_pages(self, src, dst, counts=None):
         """Positions [0, counts[i]) (default all) of page dst[i] become those of page src[i]; int32 device tensors.  No page
@@ -699,7 +705,7 @@ class PagedCache8(_Pages):
         if self.format is None:
             raise ValueError(f"unsupported dtype {K.dtype}: float8_e4m3fn or int8")
         pages, self.page_size, self.kv_heads, self.d_head = K.shape
-        self.device = K.device
+        self.device, self._types = K.device, None
         shape = K_scale.shape
         if len(shape) != 3 or tuple(shape[:2]) != (pages, self.kv_heads) or shape[2] < 1 or self.page_size % shape[2] != 0 or V_scale.shape != shape:
             raise ValueError("K_scale and V_scale must be [pages, kv_heads, blocks of a page], the blocks all of one size")
@@ -728,15 +734,7 @@ class PagedCache8(_Pages):
         """New tokens as in PagedCache.append, rounded to codes: a block's scale is its largest value over the largest code, and grows (what the block
         holds is rounded again) where a later token needs it.  No other sequence may hold or write positions of a block that is written:
         plan_pages with exclusive=True sees to that."""
-        self._append("el_attn_quantized_append", lib.el_attn_quantized_append, (self._pages, _dtype_code(k)), k.dtype, k, v, table, lengths, counts)
-
-    def _query_type(self, queries):
-        return _dtype_code(queries), queries.dtype
-
-    def _attend_call(self, queries, out_code, heads, B, beam, n):
-        code = _dtype_code(queries)
-        return ("el_attn_quantized_attend", lib.el_attn_quantized_attend, (self._pages, code),
-                lib.el_attn_quantized_workspace_bytes(self._pages, code, out_code, heads, B, beam, n))
+        self._append(k, v, table, lengths, counts)
 
     def copy_pages(self, src, dst, counts=None):
         """Positions [0, counts[i]) (default all) of page dst[i], and the scales of their blocks, become those of page src[i]; as PagedCache.copy_pages."""
