@@ -34,6 +34,7 @@ constexpr int kRor8 = 0x128;             // 16 lanes rotated by 8
 
 struct Attend8Args : AttendArgs {
     ScaleView s;
+    int dtype;                           // of the queries
     int step_slots, step_rest;           // pages and positions that 32 positions are
 };
 
@@ -656,6 +657,7 @@ extern "C" el_status el_attn_quantized_attend(const el_attn_pages8 *cache, int32
     Attend8Args a{};
     (AttendArgs &)a = attend_args(o, page_view8(*cache, table, table_stride, table_pages), cache->kv_heads, cache->d_head, lse, out, p, workspace);
     a.s = scale_view(*cache);
+    a.dtype = dtype;
     a.step_slots = TP / cache->page_size;
     a.step_rest = TP % cache->page_size;
     const hipStream_t s = (hipStream_t)stream;

@@ -46,7 +46,7 @@ struct AttendArgs {
     // and kept in natural units.  `unit` > 0: powers of two in one of theirs, `natural`: e's.
     bool shaped;
     float product, softcap, unit, natural;
-    int window, n, B, beam, heads, kv_heads, d, dtype;               // dtype: of the queries
+    int window, n, B, beam, heads, kv_heads, d;
     int group, R, row_blocks, rows;          // heads / kv_heads; query rows of a key head; blocks of them; rows of a block, at most
     bool near;                               // key heads that are neighbours in memory on one die
     int waves;                               // of a workgroup: a power of 2; more than one only where they share a whole sequence
@@ -336,7 +336,7 @@ inline AttendArgs attend_args(const AttendOperands &o, const PageView &view, int
     a.unit = a.shaped ? kLog2e : rule.scale * kLog2e;
     a.natural = a.shaped ? 1.f : rule.scale;
     a.n = o.n; a.B = o.B; a.beam = o.beam; a.heads = o.heads; a.kv_heads = kv_heads; a.d = d_head;
-    a.dtype = o.dtype; a.group = o.heads / kv_heads; a.R = o.beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
+    a.group = o.heads / kv_heads; a.R = o.beam * a.group; a.row_blocks = p.row_blocks; a.rows = p.rows;
     a.near = p.near; a.waves = p.waves; a.spans = p.spans;
     a.out = out; a.out_dtype = o.out_dtype; a.lse = lse;
     if (p.workspace) {
