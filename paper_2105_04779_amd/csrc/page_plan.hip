@@ -2,7 +2,7 @@
 //
 // Pages in use are those that the new sequences name, so nothing is kept between calls.  Bound by latency at the sizes of a serving batch: one launch of one
 // workgroup where little is to be done (k_plan_small), else four: marks cleared; rows copied and their pages marked; the unmarked pages of each chunk listed, and
-// every sequence's need added up; entries, slots.  512 requests of up to 8192 positions on 1.5 times the pages they need: 2.6 + 8.0 + 6.0 + 6.3 us.
+// every sequence's need added up; entries, slots.  512 requests of up to 8192 positions on 1.5 times the pages they need: 2.5 + 8.4 + 5.8 + 6.2 us.
 //
 // A mark is the largest of the keys (positions of the page in use, written?, lowest sequence first) of those that name it: a page is its writer's to keep if the
 // mark is the writer's own key.  Where a write changes more than the positions written (a cache in 8 bits), it is the number of entries that name the page, and a page is
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kLanes) k_plan_assign(const PlanArgs a)
 }
 
 // All of it by one workgroup, marks and free pages in LDS: pools of kSmallPages at most, where few entries and slots are to be gone through.  us on the device, four
-// launches / one: 32 sequences of 10 pages 15.2 / 10.0, 128 of 32 15.3 / 12.3, 64 of 128 16.3 / 15.3 (8256 entries and slots), 256 of 32 16.3 / 16.7, 64 of 119 and 128
+// launches / one: 32 sequences of 10 pages 15.2 / 8.8, 128 of 32 15.3 / 12.3, 64 of 128 16.3 / 15.3 (8256 entries and slots), 256 of 32 16.3 / 16.7, 64 of 119 and 128
 // new positions each 16.3 / 22.3.  Outside a graph three launches less save the host as much again.
 constexpr int kSmallPages = 8192, kSmallLanes = 1024;
 constexpr int64_t kSmallWork = 1 << 13;

@@ -18,9 +18,12 @@
 //   - V^T's operand needs 8 positions of a column in a lane: a lane loads d / 16 bytes of each of its 8 rows and pairs the bytes of two rows (v_perm)
 //     before they are converted.
 //   - ks multiplies a score in the subtraction of the running maximum, vs multiplies p before that is split into bf16 parts, which have fp32's range.
-// us in captured graphs, inputs in no cache: 64 sequences of 1024 to 4096 positions, 32 heads on 8 key heads of 128, e4m3, 337 MB, 86 (first 112: half lines, waits
-// for all that was under way, and twelve wavefronts a compute unit: 91); two of 100000 to 131072 in int8, 473 MB, 118 (143); 16 heads of 64 on as many, 111; 16 of up to
-// 8192 at 256 columns 77; 512 continuations of up to 256, 16 heads of 64, 53; one sequence of 613, 12.7.
+// us with the join, twelve passes a captured graph, inputs in no cache: 64 sequences of 1024 to 4096 positions, 32 heads on 8 key heads of 128, e4m3, 337 MB, 79 (4.2 TB/s);
+// two of 100000 to 131072 in int8, 473 MB, 101 (4.7); 16 of up to 8192, 8 key heads of 256, 337 MB, 72 to 75.  64 columns, half a line a request: 16 heads, 64 of 1024 to 4096, 337 MB,
+// 105 (3.2 TB/s); two of 100000 to 131072, 474 MB, 138 (3.4); 512 continuations of up to 256, 152 MB, 55 to 57; one sequence of 613, 11.9.  (Three passes a graph, which
+// leaves some 6 more on each: the first 112 with half lines and waits for all that was under way, 91 with twelve wavefronts a compute unit, 86; the second 143, 118.)
+// Of the first in other forms: fp32 queries 85; cap, window and slopes 87; a scale for every position or pages of 10 (not FAST) 103 and 104.  32 rows on each of 8 key heads, 32 of
+// 1024 to 4096, 168 MB, 68; 40 rows, which read and convert the codes twice, 102; 32 rows at 256 columns 142.
 // Work: paged_spans.h.
 #include <type_traits>
 #include "paged8.h"
@@ -47,7 +50,7 @@ template <int FMT_, int DP_, int RG_, int QT_, bool FAST_> struct Form8 {
     static constexpr int FMT = FMT_, DP = DP_, RG = RG_, QT = QT_, NP = 3, QP = QT == EL_F32 ? 3 : 1;
     static constexpr bool FAST = FAST_;
     static constexpr int LDS = RG * DP * 64 + 256;                   // of a wavefront that shares its sequence: results, (m, l)
-    // wavefronts that a compute unit holds, by registers (twelve of 128 columns would fit: 91 us for 86 with eight, 64 sequences of 1024 to 4096 on 8 key heads)
+    // wavefronts that a compute unit holds, by registers (twelve of 128 columns would fit, and take 6 % longer: 64 sequences of 1024 to 4096 on 8 key heads)
     static constexpr int PER_CU = DP == 256 || (DP == 128 && RG * QP == 6) ? 4 : DP == 128 || RG * QP > 2 ? 8 : RG == 2 ? 12 : 16;
     static constexpr int ROOM = 163840 / LDS, WAVES = ROOM >= 8 && PER_CU >= 8 ? 8 : 4;
 };

@@ -11,13 +11,14 @@
 // range that it falls into are ranked; a range of too many is cut into 512 again.  The sums of the ranges above are then each wavefront's share of what is left, so
 // the token's share is known without another look at the row, and only that is gone through in order.
 //
-// Bound by the vector ALU, 23 operations a logit for its weight, 16 of them of 64 bits (HBM alone would allow a row in 11 us on each compute unit).  us of a row in
+// Bound by the vector ALU, 23 operations a logit for its weight, 16 of them of 64 bits (HBM alone would allow a row in 11 us on each compute unit), and for rows in
+// fp32 as much by HBM, from which they come 2.6 times: 688 MB in 140 to 150 us for 512 of 128003.  us of a row in
 // bf16, one on each compute unit, 128003 logits: maxima 11 (HBM's rate), all weights 30, or 43 with their histogram (the rest is atomics in LDS, 11 to 18 clocks
-// each), tokens of the range 17, ranked 5, the share and the token 6.  256 rows with settings of their own 79 (97 when rows with top-p and min-p were
+// each), tokens of the range 17, ranked 5, the share and the token 6.  256 rows with settings of their own 80 (97 when rows with top-p and min-p were
 // always cut by the one before the other), 4 rows of 50265 with top-k 50 and all filters 17, three looks at the row.
 // More rows than compute units: workgroups of 512 lanes, two of which share one, so that a row computes while the other waits.  us with 1024 / 512: 512 rows of 128003 in bf16,
 // top-p 0.9 170 / 157, top-k 40 70 / 59, nothing 100 / 101; of 32000, top-p 72 / 53; 2000 of 32000, top-k and top-p of their own 182 / 123.  Rows that take longer are
-// begun first: 512 in fp32, half of them with top-p, 178 in their order (176 with 512 lanes), 160.
+// begun first: 512 in fp32, half of them with top-p, 178 in their order (176 with 512 lanes), 160 (three passes a captured graph; 133 to 154 among others, by the rows' luck).
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
