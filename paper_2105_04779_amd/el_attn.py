@@ -352,9 +352,9 @@ def el_attn_plan_pages(table, table_stride, columns, lengths, B_old, parents, co
 
 
 def el_attn_plan_pages_exclusive(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
-                       new_table, new_lengths, granted, slots, copies, free_pages, workspace=None, workspace_bytes=0, stream=None) -> int:
+                                 new_table, new_lengths, granted, slots, copies, free_pages, workspace=None, workspace_bytes=0, stream=None) -> int:
     return lib.el_attn_plan_pages_exclusive(table, table_stride, columns, lengths, B_old, parents, counts, reserved, pages, page_size, B, T,
-                                  new_table, new_lengths, granted, slots, copies, free_pages, workspace, workspace_bytes, stream)
+                                            new_table, new_lengths, granted, slots, copies, free_pages, workspace, workspace_bytes, stream)
 
 
 def el_attn_sample_workspace_bytes(dtype, rows, vocab) -> int:
